@@ -18,9 +18,8 @@
 //
 // Every wait on an mbarrier is bounded: when one gives up, the CTA raises a flag that all
 // roles poll, drains, frees its TMEM and returns, and a status word in global memory is set.
-#include <cuda.h>
-
 #include "common.cuh"
+#include "tc.cuh"
 
 // fp32 mode: A_hi = x with the low 13 mantissa bits cleared (what the tensor core keeps of a tf32 operand),
 // A_lo = x - A_hi, exact in fp32.  (Were the hi part rounded instead while the lo part assumed truncation,
@@ -28,8 +27,6 @@
 
 namespace {
 
-constexpr int TC_BM = 128;          // rows per tile (UMMA M)
-constexpr int TC_KBLOCK_BYTES = 128;  // one swizzle row of K per k-block
 constexpr int TC_EPI_WARPS = 16;      // four warps per TMEM lane quarter, each takes every fourth 16-column group
 constexpr int TC_THREADS_BF16 = 64 + 32 * TC_EPI_WARPS;   // warp 0 TMA, warp 1 MMA + TMEM, warps 2-17 epilogue
 #ifndef IT_TC_EPI_BACKOFF
@@ -44,9 +41,6 @@ constexpr int TC_THREADS_BF16 = 64 + 32 * TC_EPI_WARPS;   // warp 0 TMA, warp 1 
 #ifndef IT_TC_TMA_STORE
 #define IT_TC_TMA_STORE 1   // 0: always store the results straight from registers
 #endif
-#ifndef IT_TC_MAX_STAGES
-#define IT_TC_MAX_STAGES 8   // operand stages in shared memory (as many as fit, up to this)
-#endif
 #ifndef IT_TC_SPLIT_GROUPS
 #define IT_TC_SPLIT_GROUPS 1   // groups of four split warps; group g takes every k-block c with c % groups == g (measured: a second group gains nothing)
 #endif
@@ -57,98 +51,7 @@ constexpr int TC_THREADS_TF32 = TC_THREADS_BF16 + 128 * TC_SPLIT_GROUPS;   // ..
 #endif
 constexpr int TC_TSTAGES_MAX = IT_TC_TSTAGES_MAX;     // fp32 mode: split A tiles in flight in TMEM
 constexpr int TC_TSTAGE_COLS = 64;    // TMEM columns of one split A k-block: 32 of hi, 32 of lo
-constexpr uint32_t TC_SPIN_LIMIT = 1u << 22;
 
-// ----------------------------------------------------------------------------- PTX wrappers
-__device__ __forceinline__ uint32_t smem_u32(const void *p) { return (uint32_t)__cvta_generic_to_shared(p); }
-
-__device__ __forceinline__ void mbar_init(uint64_t *bar, uint32_t count) {
-  asm volatile("mbarrier.init.shared::cta.b64 [%0], %1;" ::"r"(smem_u32(bar)), "r"(count));
-}
-__device__ __forceinline__ void mbar_arrive(uint64_t *bar) {
-  asm volatile("mbarrier.arrive.shared::cta.b64 _, [%0];" ::"r"(smem_u32(bar)) : "memory");
-}
-__device__ __forceinline__ void mbar_arrive_expect_tx(uint64_t *bar, uint32_t bytes) {
-  asm volatile("mbarrier.arrive.expect_tx.shared::cta.b64 _, [%0], %1;" ::"r"(smem_u32(bar)), "r"(bytes) : "memory");
-}
-__device__ __forceinline__ bool mbar_try_wait(uint64_t *bar, uint32_t parity) {
-  uint32_t ok;
-  asm volatile(
-      "{\n\t.reg .pred p;\n\t"
-      "mbarrier.try_wait.parity.shared::cta.b64 p, [%1], %2;\n\t"
-      "selp.u32 %0, 1, 0, p;\n\t}"
-      : "=r"(ok)
-      : "r"(smem_u32(bar)), "r"(parity)
-      : "memory");
-  return ok != 0;
-}
-// Bounded wait.  Returns false if the CTA is aborting (or this wait ran out and started the abort).
-// `backoff_ns` > 0: sleep between polls, for roles whose waits are long and off the critical path (their polling
-// would otherwise take issue slots from the warps that feed the tensor core).
-// `limit`: the number of polls after which the wait gives up.
-__device__ __forceinline__ bool mbar_wait(uint64_t *bar, uint32_t parity, volatile int *abort_flag, uint32_t limit, uint32_t backoff_ns = 0) {
-  for (uint32_t it = 0; it < limit; ++it) {
-    if (mbar_try_wait(bar, parity)) return true;
-    if (backoff_ns) __nanosleep(backoff_ns);
-    if ((it & 63u) == 63u && *abort_flag) return false;
-  }
-  *abort_flag = 1;
-  return false;
-}
-// Before a CTA may leave, what it set off has to be over, also where a role gave up a wait: copies would still write its shared memory,
-// and MMAs read it and write its TMEM, when both belong to another CTA.  A barrier's wait for one parity is always true (that of the
-// phase before the present one), so it has to be the parity of the phase that was armed last.  Bounded, and apart from the abort flag.
-__device__ __forceinline__ void mbar_drain(uint64_t *bar, uint32_t parity) {
-  for (uint32_t it = 0; it < TC_SPIN_LIMIT; ++it)
-    if (mbar_try_wait(bar, parity)) return;
-}
-// A ring whose position (`next`, `phase`: the stage and parity that the next copy would have) has come round from (0, 0): whether stage
-// s was armed at all, and the parity of its last time.
-struct RingStage { bool armed; uint32_t parity; };
-__host__ __device__ constexpr RingStage ring_last(uint32_t s, uint32_t next, uint32_t phase, bool came_round) {
-  return s < next ? RingStage{true, phase} : RingStage{came_round, phase ^ 1u};
-}
-constexpr bool ring_last_holds() {   // against every copy made in turn
-  for (uint32_t stages = 1; stages <= IT_TC_MAX_STAGES; ++stages)
-    for (uint32_t copies = 0; copies <= 3 * stages + 1; ++copies) {
-      uint32_t next = 0, phase = 0, parity[IT_TC_MAX_STAGES] = {};
-      bool armed[IT_TC_MAX_STAGES] = {}, came_round = false;
-      for (uint32_t i = 0; i < copies; ++i) {
-        armed[next] = true;
-        parity[next] = phase;
-        if (++next == stages) { next = 0; phase ^= 1u; came_round = true; }
-      }
-      for (uint32_t s = 0; s < stages; ++s) {
-        const RingStage r = ring_last(s, next, phase, came_round);
-        if (r.armed != armed[s] || (r.armed && r.parity != parity[s])) return false;
-      }
-    }
-  return true;
-}
-static_assert(ring_last_holds(), "the last copy into every stage of a ring");
-__device__ __forceinline__ void ring_drain(uint64_t *full, uint32_t stages, uint32_t next, uint32_t phase, bool came_round) {
-  for (uint32_t s = 0; s < stages; ++s) {
-    const RingStage r = ring_last(s, next, phase, came_round);
-    if (r.armed) mbar_drain(&full[s], r.parity);
-  }
-}
-__device__ __forceinline__ void tma_load_2d(void *dst, const CUtensorMap *map, int c0, int c1, uint64_t *bar) {
-  asm volatile(
-      "cp.async.bulk.tensor.2d.shared::cluster.global.tile.mbarrier::complete_tx::bytes [%0], [%1, {%3, %4}], [%2];"
-      ::"r"(smem_u32(dst)), "l"(map), "r"(smem_u32(bar)), "r"(c0), "r"(c1)
-      : "memory");
-}
-// TMA store of one 128-byte-swizzled panel [128 rows x 128 bytes] from shared memory; rows past the end of the
-// tensor are clipped by the copy engine.
-__device__ __forceinline__ void tma_store_2d(const CUtensorMap *map, const void *src, int c0, int c1) {
-  asm volatile("cp.async.bulk.tensor.2d.global.shared::cta.tile.bulk_group [%0, {%2, %3}], [%1];"
-               ::"l"(map), "r"(smem_u32(src)), "r"(c0), "r"(c1)
-               : "memory");
-}
-__device__ __forceinline__ void tma_store_commit() { asm volatile("cp.async.bulk.commit_group;" ::: "memory"); }
-__device__ __forceinline__ void tma_store_wait_read() { asm volatile("cp.async.bulk.wait_group.read 0;" ::: "memory"); }
-__device__ __forceinline__ void tma_store_wait_read_but_last() { asm volatile("cp.async.bulk.wait_group.read 1;" ::: "memory"); }
-__device__ __forceinline__ void tma_store_wait_all() { asm volatile("cp.async.bulk.wait_group 0;" ::: "memory"); }
 // Named barriers of the epilogue warps: barrier 1 over all sixteen, or barriers 1 and 2 over the eight of a group, or 1 to 4 over the
 // four.  The reducing form also tells every thread whether any of them failed.
 __device__ __forceinline__ void epi_bar_sync(int groups, int group) {
@@ -170,72 +73,6 @@ __device__ __forceinline__ bool epi_bar_any(int groups, int group, bool flag) {
   else if (group == 0) IT_EPI_BAR_RED(1, 16 * TC_EPI_WARPS);
   else IT_EPI_BAR_RED(2, 16 * TC_EPI_WARPS);
   return r != 0;
-}
-__device__ __forceinline__ void st_shared_v4(uint32_t addr, uint32_t a, uint32_t b, uint32_t c, uint32_t d) {
-  asm volatile("st.shared.v4.b32 [%0], {%1, %2, %3, %4};" ::"r"(addr), "r"(a), "r"(b), "r"(c), "r"(d) : "memory");
-}
-__device__ __forceinline__ void tmem_alloc(uint32_t *dst_smem, uint32_t ncols) {
-  asm volatile("tcgen05.alloc.cta_group::1.sync.aligned.shared::cta.b32 [%0], %1;" ::"r"(smem_u32(dst_smem)), "r"(ncols));
-}
-__device__ __forceinline__ void tmem_relinquish() {
-  asm volatile("tcgen05.relinquish_alloc_permit.cta_group::1.sync.aligned;" ::);
-}
-__device__ __forceinline__ void tmem_dealloc(uint32_t taddr, uint32_t ncols) {
-  asm volatile("tcgen05.dealloc.cta_group::1.sync.aligned.b32 %0, %1;" ::"r"(taddr), "r"(ncols));
-}
-__device__ __forceinline__ void tc_fence_before() { asm volatile("tcgen05.fence::before_thread_sync;" ::: "memory"); }
-__device__ __forceinline__ void tc_fence_after() { asm volatile("tcgen05.fence::after_thread_sync;" ::: "memory"); }
-__device__ __forceinline__ void tc_commit(uint64_t *bar) {
-  asm volatile("tcgen05.commit.cta_group::1.mbarrier::arrive::one.shared::cluster.b64 [%0];" ::"r"(smem_u32(bar)) : "memory");
-}
-template <bool TF32>
-__device__ __forceinline__ void tc_mma(uint32_t d_tmem, uint64_t a_desc, uint64_t b_desc, uint32_t idesc, uint32_t accumulate) {
-  if (TF32) {
-    asm volatile(
-        "{\n\t.reg .pred p;\n\tsetp.ne.b32 p, %4, 0;\n\t"
-        "tcgen05.mma.cta_group::1.kind::tf32 [%0], %1, %2, %3, {%5, %5, %5, %5}, p;\n\t}"
-        ::"r"(d_tmem), "l"(a_desc), "l"(b_desc), "r"(idesc), "r"(accumulate), "r"(0u)
-        : "memory");
-  } else {
-    asm volatile(
-        "{\n\t.reg .pred p;\n\tsetp.ne.b32 p, %4, 0;\n\t"
-        "tcgen05.mma.cta_group::1.kind::f16 [%0], %1, %2, %3, {%5, %5, %5, %5}, p;\n\t}"
-        ::"r"(d_tmem), "l"(a_desc), "l"(b_desc), "r"(idesc), "r"(accumulate), "r"(0u)
-        : "memory");
-  }
-}
-// The same product with the A operand in tensor memory (lane = row of the tile, one 32-bit column per tf32 element).
-__device__ __forceinline__ void tc_mma_tf32_tmem_a(uint32_t d_tmem, uint32_t a_tmem, uint64_t b_desc, uint32_t idesc, uint32_t accumulate) {
-  asm volatile(
-      "{\n\t.reg .pred p;\n\tsetp.ne.b32 p, %4, 0;\n\t"
-      "tcgen05.mma.cta_group::1.kind::tf32 [%0], [%1], %2, %3, {%5, %5, %5, %5}, p;\n\t}"
-      ::"r"(d_tmem), "r"(a_tmem), "l"(b_desc), "r"(idesc), "r"(accumulate), "r"(0u)
-      : "memory");
-}
-// Lane i of the warp writes 16 consecutive 32-bit columns of TMEM lane (lane base of taddr) + i.
-__device__ __forceinline__ void tmem_st16(uint32_t taddr, const uint32_t (&r)[16]) {
-  asm volatile(
-      "tcgen05.st.sync.aligned.32x32b.x16.b32 [%0], {%1, %2, %3, %4, %5, %6, %7, %8, %9, %10, %11, %12, %13, %14, %15, %16};"
-      ::"r"(taddr), "r"(r[0]), "r"(r[1]), "r"(r[2]), "r"(r[3]), "r"(r[4]), "r"(r[5]), "r"(r[6]), "r"(r[7]), "r"(r[8]),
-        "r"(r[9]), "r"(r[10]), "r"(r[11]), "r"(r[12]), "r"(r[13]), "r"(r[14]), "r"(r[15])
-      : "memory");
-}
-__device__ __forceinline__ void tmem_st_wait() { asm volatile("tcgen05.wait::st.sync.aligned;" ::: "memory"); }
-__device__ __forceinline__ void tmem_ld16(uint32_t taddr, uint32_t (&r)[16]) {
-  asm volatile(
-      "tcgen05.ld.sync.aligned.32x32b.x16.b32 {%0, %1, %2, %3, %4, %5, %6, %7, %8, %9, %10, %11, %12, %13, %14, %15}, [%16];"
-      : "=r"(r[0]), "=r"(r[1]), "=r"(r[2]), "=r"(r[3]), "=r"(r[4]), "=r"(r[5]), "=r"(r[6]), "=r"(r[7]), "=r"(r[8]),
-        "=r"(r[9]), "=r"(r[10]), "=r"(r[11]), "=r"(r[12]), "=r"(r[13]), "=r"(r[14]), "=r"(r[15])
-      : "r"(taddr));
-}
-__device__ __forceinline__ void tmem_ld_wait() { asm volatile("tcgen05.wait::ld.sync.aligned;" ::: "memory"); }
-
-// Shared-memory matrix descriptor of a K-major tile whose rows are 128-byte swizzle rows:
-// start address, leading offset 16 B (unused for swizzled K-major), 1024 B between 8-row
-// groups, descriptor version 1, layout SWIZZLE_128B.
-__device__ __forceinline__ uint64_t make_desc(uint32_t smem_addr) {
-  return (uint64_t)((smem_addr & 0x3FFFFu) >> 4) | ((uint64_t)1 << 16) | ((uint64_t)(1024 >> 4) << 32) | ((uint64_t)1 << 46) |
-         ((uint64_t)2 << 61);
 }
 
 // ----------------------------------------------------------------------------- kernel
@@ -1411,21 +1248,6 @@ __global__ void __launch_bounds__(256) prep_weights_tc_kernel(const __grid_const
 }
 
 // ----------------------------------------------------------------------------- host side
-typedef CUresult (*EncodeTiledFn)(CUtensorMap *, CUtensorMapDataType, cuuint32_t, void *, const cuuint64_t *, const cuuint64_t *,
-                                  const cuuint32_t *, const cuuint32_t *, CUtensorMapInterleave, CUtensorMapSwizzle,
-                                  CUtensorMapL2promotion, CUtensorMapFloatOOBfill);
-
-EncodeTiledFn get_encode() {
-  static EncodeTiledFn fn = nullptr;
-  if (!fn) {
-    void *p = nullptr;
-    cudaDriverEntryPointQueryResult qres;
-    if (cudaGetDriverEntryPoint("cuTensorMapEncodeTiled", &p, cudaEnableDefault, &qres) == cudaSuccess && qres == cudaDriverEntryPointSuccess)
-      fn = reinterpret_cast<EncodeTiledFn>(p);
-  }
-  return fn;
-}
-
 // 2-D row-major matrix [rows, cols] of `elem` bytes; box = 128 bytes of a row x box_rows rows, 128-byte swizzle.
 it_status make_map(CUtensorMap *map, const void *ptr, int elem, int64_t rows, int64_t cols, int box_rows) {
   EncodeTiledFn enc = get_encode();
