@@ -43,14 +43,14 @@ typedef enum {
   IT_ERR_TIMEOUT = 7      /* a bounded device-side wait gave up */
 } it_status;
 
-typedef enum { IT_F32 = 0, IT_BF16 = 1 } it_dtype;
+typedef enum { IT_F32 = 0, IT_BF16 = 1, IT_E4M3 = 2 /* 8 bits: only where a call says so */ } it_dtype;
 typedef enum { IT_I32 = 0, IT_I64 = 1 } it_itype;
 typedef enum {
   IT_GATHER_SUM = 0, IT_GATHER_MEAN = 1, IT_GATHER_MAX = 2, IT_GATHER_GAT = 3, IT_GATHER_MIN = 4,
   IT_GATHER_NONE = 5,   /* no Gather stage: a dense layer */
   IT_GATHER_GCN = 6     /* sum aggregate, update on the aggregate alone */
 } it_gather_op;
-typedef enum { IT_ACT_NONE = 0, IT_ACT_RELU = 1, IT_ACT_ELU = 2 } it_act;
+typedef enum { IT_ACT_NONE = 0, IT_ACT_RELU = 1, IT_ACT_ELU = 2, IT_ACT_SILU = 3 /* experts only */ } it_act;
 
 #define IT_MAX_BUCKETS 8
 
@@ -296,6 +296,93 @@ it_status it_layer_update(const it_graph *g, const it_layer_desc *layer, const v
  */
 it_status it_aggregate_finish(int64_t n, int32_t dim, it_dtype dtype, const float *raw, const float *scale, void *out,
                               void *stream);
+
+/*
+ * A block of experts between two layers (no counterpart in the paper, whose layers have one apply_node for all vertices):
+ * it_residual_norm, a dense layer (op = IT_GATHER_NONE) for the logits, it_route, it_experts_forward.  Each call works on the
+ * rows of n vertices, whatever graph they belong to, from a single vertex on; none of them allocates or synchronises, and all of
+ * them can be captured into a CUDA graph.  Results are bit-identical from run to run.
+ *
+ * it_residual_norm - residual addition and root-mean-square norm of every row:
+ *       s = x + residual                                        (residual may be NULL: s = x)
+ *       y = s / sqrt( mean(s^2) + eps ) * weight                (weight fp32 [dim] or NULL: 1)
+ *   s and the mean are held in fp32 (so |s| beyond 1e19 overflows the mean, and an infinity or NaN in a row makes the row NaN).
+ *   sum_out [n, dim] feat_dtype, or NULL: s, rounded; the next block's residual.  y is taken from the unrounded s.
+ *   out [n, dim]: out_dtype = feat_dtype, or IT_E4M3 (dim a multiple of 16): y / scales[v] rounded to nearest even, with one fp32 scale
+ *   per row, scales[v] = max( max|y| / 448, 2^-126 ).  scales must be NULL otherwise.
+ *   sum_out and an out of feat_dtype may be x or residual themselves (not both the same matrix); other overlaps are refused.
+ */
+typedef struct {
+  int32_t dim;
+  it_dtype feat_dtype, out_dtype;
+  float eps;                            /* >= 0 */
+  const float *weight;                  /* [dim], may be NULL */
+} it_norm_desc;
+it_status it_residual_norm(const it_norm_desc *d, int64_t n, const void *x, const void *residual, void *sum_out, void *out,
+                           float *scales, void *stream);
+
+/*
+ * it_route - which experts every vertex goes to, and with which weights.  logits [n, n_experts] of logit_dtype, rows dense, of any length.
+ *   score_e  softmax over the row, or 1 / (1 + exp(-logit)).  A logit of -inf or NaN closes the expert to the vertex (score 0, never
+ *            chosen); +inf counts as the largest finite fp32 value.
+ *   key_e    score_e + balance_bias[e]; without a bias the logit itself (the same order).  A key of -inf or NaN closes the expert too.
+ *   groups   n_groups > 1: the experts fall into n_groups runs of equal length.  A group is worth the sum of its group_best (1 or 2) largest
+ *            keys (scores without a bias); only the group_k best groups that have an open expert stay open.
+ *   choice   the top_k largest keys in descending order.  The order is that of exact arithmetic as far as 64 bits resolve it; equal keys
+ *            (and groups) go to the lowest index.
+ *   ids      [n, top_k] int32; -1 where no open expert is left (weight 0).
+ *   weights  [n, top_k] fp32: the scores of the chosen (without the bias), with renormalise divided by their sum (0 where that is 0),
+ *            times weight_scale.
+ *   n_experts <= 1024, top_k <= min(n_experts, 32); n_groups divides n_experts; ids and weights overlap neither each other nor logits.
+ */
+typedef enum { IT_SCORE_SOFTMAX = 0, IT_SCORE_SIGMOID = 1 } it_score;
+typedef struct {
+  int32_t n_experts, top_k;
+  it_dtype logit_dtype;                 /* IT_F32 or IT_BF16 */
+  it_score score;
+  const float *balance_bias;            /* [n_experts], may be NULL */
+  int32_t n_groups, group_k, group_best;   /* 1, 1, 1: no groups */
+  int32_t renormalise;                  /* 0/1 */
+  float weight_scale;
+} it_route_desc;
+it_status it_route(const it_route_desc *d, int64_t n, const void *logits, int32_t *ids, float *weights, void *stream);
+
+/*
+ * it_experts_forward - the products of the experts that every vertex was sent to:
+ *       out[v] = sum_j weights[v, j] * F_{ids[v, j]}( x[v] )                        (0 where a vertex has no expert)
+ *       hidden_dim = 0:         F_e(x) = act( x * W1[e] + b1[e] )                    W1 [n_experts, in_dim, out_dim]
+ *       hidden_dim > 0:         F_e(x) = act( x * W1[e] + b1[e] ) * W2[e] + b2[e]    W1 [n_experts, in_dim, hidden_dim], W2 [n_experts, hidden_dim, out_dim]
+ *       ... and gated:          F_e(x) = ( act(g) . u ) * W2[e] + b2[e],  [g | u] = x * W1[e] + b1[e]    W1 [n_experts, in_dim, 2 * hidden_dim]
+ *   (top_k = 1, weights 1 and ids = a type per vertex: one weight matrix per vertex type.)
+ *   x [n, in_dim] of in_dtype, out [n, out_dim] of feat_dtype; in_dtype = feat_dtype, or IT_E4M3 with feat_dtype = IT_BF16: then x and W1 are
+ *   e4m3, x stands for x * x_scale[v] (fp32 [n], as it_residual_norm writes it) and W1[e, :, c] for W1[e, :, c] * w1_scale[e, c]
+ *   (fp32, one per column of W1).  W2 is feat_dtype; b1, b2, weights are fp32.
+ *   An id outside [0, n_experts) is no expert, whatever its weight; an expert may be named twice.
+ *   Widths: every row of x, W1, W2 and out is a multiple of 16 bytes (gated: a row of hidden_dim of them too).  n * top_k and the padded places of the
+ *   experts' rows are counted in 32 bits: n * top_k + 128 * n_experts < 2^31 (fp32: a third of that).
+ *   The products run on the tensor cores with fp32 accumulators (fp32 operands as three bf16 parts, six products); the hidden row between the
+ *   two products is stored in feat_dtype, the places of a vertex are added in fp32, in their order, and rounded once.
+ *   workspace: device, 256-byte aligned, >= it_experts_workspace_bytes; calls that can overlap on the GPU need one each.
+ *   x, ids, weights and the expert arrays may not overlap out or the workspace.
+ * it_experts_check - waits for `stream` and reports whether the last it_experts_forward with this workspace gave up one of its bounded
+ *   device-side waits: IT_ERR_TIMEOUT (out is then not valid), else IT_OK.
+ */
+typedef struct {
+  int32_t n_experts, top_k;
+  int32_t in_dim, hidden_dim, out_dim;  /* hidden_dim = 0: one product */
+  it_dtype feat_dtype, in_dtype;
+  it_act act;
+  int32_t gated;                        /* 0/1, needs hidden_dim > 0 */
+  const void *W1;
+  const float *b1;                      /* [n_experts, columns of W1], may be NULL */
+  const void *W2;                       /* NULL with hidden_dim = 0 */
+  const float *b2;                      /* [n_experts, out_dim], may be NULL; NULL with hidden_dim = 0 */
+  const float *w1_scale;                /* in_dtype IT_E4M3: [n_experts, columns of W1], else NULL */
+} it_experts_desc;
+it_status it_experts_workspace_bytes(const it_experts_desc *d, int64_t n, size_t *out_bytes);
+it_status it_experts_forward(const it_experts_desc *d, int64_t n, const void *x, const float *x_scale, const int32_t *ids,
+                             const float *weights, void *out, void *workspace, size_t workspace_bytes, void *stream);
+it_status it_experts_check(void *workspace, void *stream);
 
 /*
  * it_layer_forward_static — it_layer_forward for callers that must not allocate device

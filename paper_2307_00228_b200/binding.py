@@ -17,17 +17,20 @@ LIB_PATH = os.environ.get("INFERTURBO_LIB") or os.path.join(_PKG, "libinferturbo
 IT_OK = 0
 STATUS_NAMES = ["IT_OK", "IT_ERR_INVALID_ARG", "IT_ERR_BAD_GRAPH", "IT_ERR_UNSUPPORTED", "IT_ERR_WORKSPACE",
                 "IT_ERR_OOM", "IT_ERR_CUDA", "IT_ERR_TIMEOUT"]
-IT_F32, IT_BF16 = 0, 1
+IT_F32, IT_BF16, IT_E4M3 = 0, 1, 2
 IT_I32, IT_I64 = 0, 1
 GATHER_OPS = {"sum": 0, "mean": 1, "max": 2, "gat": 3, "min": 4, "dense": 5, "gcn": 6}
 ACTS = {"none": 0, "relu": 1, "elu": 2}
+EXPERT_ACTS = {**ACTS, "silu": 3}
+SCORES = {"softmax": 0, "sigmoid": 1}
 IT_MAX_BUCKETS = 8
 EXPORTS = ["it_graph_create", "it_split_hubs", "it_graph_get_split", "it_workspace_bytes", "it_layer_forward",
            "it_infer", "it_graph_destroy", "it_status_string", "it_last_error_message", "it_profile_begin",
            "it_profile_end", "it_kernel_launch_count", "it_layer_forward_static", "it_graph_check",
            "it_graph_set_edge_features", "it_debug_expire_wait", "it_graph_create_part", "it_layer_stages",
            "it_layer_transform", "it_layer_gather", "it_layer_update", "it_aggregate_finish", "it_debug_expire_wait_fused",
-           "it_debug_expire_wait_form"]
+           "it_debug_expire_wait_form", "it_residual_norm", "it_route", "it_experts_workspace_bytes", "it_experts_forward",
+           "it_experts_check"]
 
 
 class ItError(RuntimeError):
@@ -45,6 +48,21 @@ class it_layer_desc(C.Structure):
                 ("leaky_slope", C.c_float), ("use_edge_weights", C.c_int32), ("allow_reorder", C.c_int32),
                 ("edge_dim", C.c_int32), ("msg_dim", C.c_int32), ("act_edge", C.c_int),
                 ("W_edge", C.c_void_p), ("bias_edge", C.c_void_p), ("att_edge", C.c_void_p)]
+
+
+class it_norm_desc(C.Structure):
+    _fields_ = [("dim", C.c_int32), ("feat_dtype", C.c_int), ("out_dtype", C.c_int), ("eps", C.c_float), ("weight", C.c_void_p)]
+
+
+class it_route_desc(C.Structure):
+    _fields_ = [("n_experts", C.c_int32), ("top_k", C.c_int32), ("logit_dtype", C.c_int), ("score", C.c_int), ("balance_bias", C.c_void_p),
+                ("n_groups", C.c_int32), ("group_k", C.c_int32), ("group_best", C.c_int32), ("renormalise", C.c_int32), ("weight_scale", C.c_float)]
+
+
+class it_experts_desc(C.Structure):
+    _fields_ = [("n_experts", C.c_int32), ("top_k", C.c_int32), ("in_dim", C.c_int32), ("hidden_dim", C.c_int32), ("out_dim", C.c_int32),
+                ("feat_dtype", C.c_int), ("in_dtype", C.c_int), ("act", C.c_int), ("gated", C.c_int32),
+                ("W1", C.c_void_p), ("b1", C.c_void_p), ("W2", C.c_void_p), ("b2", C.c_void_p), ("w1_scale", C.c_void_p)]
 
 
 class it_stage_desc(C.Structure):
@@ -81,6 +99,13 @@ def lib() -> C.CDLL:
                      "it_aggregate_finish"):
             getattr(L, name).restype = C.c_int
         for name in EXPORTS[:7]:
+            getattr(L, name).restype = C.c_int
+        L.it_residual_norm.argtypes = [C.POINTER(it_norm_desc), i64, vp, vp, vp, vp, vp, vp]
+        L.it_route.argtypes = [C.POINTER(it_route_desc), i64, vp, vp, vp, vp]
+        L.it_experts_workspace_bytes.argtypes = [C.POINTER(it_experts_desc), i64, C.POINTER(C.c_size_t)]
+        L.it_experts_forward.argtypes = [C.POINTER(it_experts_desc), i64, vp, vp, vp, vp, vp, vp, C.c_size_t, vp]
+        L.it_experts_check.argtypes = [vp, vp]
+        for name in ("it_residual_norm", "it_route", "it_experts_workspace_bytes", "it_experts_forward", "it_experts_check"):
             getattr(L, name).restype = C.c_int
         L.it_status_string.argtypes = [C.c_int]
         L.it_status_string.restype = C.c_char_p
@@ -370,6 +395,133 @@ def it_debug_expire_wait_form(g: Graph, form: int, buffer: torch.Tensor, stream=
     L.it_debug_expire_wait_form.restype = C.c_int
     L.it_debug_expire_wait_form.argtypes = [C.c_void_p, C.c_int, C.c_void_p, C.c_size_t, C.c_void_p]
     _check(L.it_debug_expire_wait_form(g.handle, form, _ptr(buffer), buffer.numel() * buffer.element_size(), _stream(stream)))
+
+
+# ----------------------------------------------------------------------------- a block of experts between two layers
+_DTYPES = {torch.float32: IT_F32, torch.bfloat16: IT_BF16, torch.float8_e4m3fn: IT_E4M3}
+
+
+def _dtype_code(t: torch.dtype) -> int:
+    if t not in _DTYPES:
+        raise TypeError(f"unsupported dtype {t}")
+    return _DTYPES[t]
+
+
+def _addr(name, t, dtype, shape, optional=False):
+    """Address of a dense tensor on the current device, its type and shape checked (the library sees addresses only)."""
+    if t is None:
+        if not optional:
+            raise ValueError(f"{name} is None")
+        return None
+    if t.dtype != dtype or tuple(t.shape) != tuple(shape):
+        raise ValueError(f"{name} is {t.dtype} {tuple(t.shape)}, expected {dtype} {tuple(shape)}")
+    if not t.is_cuda or not t.is_contiguous() or t.device.index != torch.cuda.current_device():
+        raise ValueError(f"{name} must be a contiguous tensor on the current CUDA device")
+    return t.data_ptr()
+
+
+@dataclass(frozen=True)
+class NormDesc:
+    """it_norm_desc; out_dtype None: feat_dtype.  The C form is made once: the fields do not change."""
+    dim: int
+    feat_dtype: torch.dtype
+    weight: torch.Tensor | None = None
+    eps: float = 1e-5
+    out_dtype: torch.dtype | None = None
+
+    def __post_init__(self):
+        out = self.feat_dtype if self.out_dtype is None else self.out_dtype
+        object.__setattr__(self, "out_dtype", out)
+        object.__setattr__(self, "_c", it_norm_desc(self.dim, _dtype_code(self.feat_dtype), _dtype_code(out), self.eps,
+                                                    _addr("weight", self.weight, torch.float32, (self.dim,), optional=True)))
+
+
+def it_residual_norm(d: NormDesc, x, out, residual=None, sum_out=None, scales=None, stream=None):
+    """s = x + residual; out = s / sqrt(mean(s^2) + eps) * weight, in feat_dtype or in e4m3 with scales [n]; sum_out = s.  Returns out."""
+    shape = (x.shape[0], d.dim)
+    _check(lib().it_residual_norm(C.byref(d._c), shape[0], _addr("x", x, d.feat_dtype, shape), _addr("residual", residual, d.feat_dtype, shape, True),
+                                  _addr("sum_out", sum_out, d.feat_dtype, shape, True), _addr("out", out, d.out_dtype, shape),
+                                  _addr("scales", scales, torch.float32, shape[:1], True), _stream(stream)))
+    return out
+
+
+@dataclass(frozen=True)
+class RouteDesc:
+    """it_route_desc; the C form is made once."""
+    n_experts: int
+    top_k: int
+    logit_dtype: torch.dtype
+    score: str = "softmax"
+    balance_bias: torch.Tensor | None = None
+    n_groups: int = 1
+    group_k: int = 1
+    group_best: int = 1
+    renormalise: bool = True
+    weight_scale: float = 1.0
+
+    def __post_init__(self):
+        bias = _addr("balance_bias", self.balance_bias, torch.float32, (self.n_experts,), optional=True)
+        object.__setattr__(self, "_c", it_route_desc(self.n_experts, self.top_k, _dtype_code(self.logit_dtype), SCORES[self.score], bias, self.n_groups,
+                                                     self.group_k, self.group_best, int(self.renormalise), self.weight_scale))
+
+
+def it_route(d: RouteDesc, logits, ids, weights, stream=None):
+    """logits [n, n_experts] -> ids int32 [n, top_k] (-1: none left), weights fp32 [n, top_k].  Returns (ids, weights)."""
+    n = logits.shape[0]
+    _check(lib().it_route(C.byref(d._c), n, _addr("logits", logits, d.logit_dtype, (n, d.n_experts)), _addr("ids", ids, torch.int32, (n, d.top_k)),
+                          _addr("weights", weights, torch.float32, (n, d.top_k)), _stream(stream)))
+    return ids, weights
+
+
+@dataclass(frozen=True)
+class ExpertsDesc:
+    """it_experts_desc; states are e4m3 where W1 is.  The C form is made once."""
+    n_experts: int
+    top_k: int
+    in_dim: int
+    out_dim: int
+    feat_dtype: torch.dtype
+    W1: torch.Tensor
+    hidden_dim: int = 0
+    b1: torch.Tensor | None = None
+    W2: torch.Tensor | None = None
+    b2: torch.Tensor | None = None
+    act: str = "none"
+    gated: bool = False
+    w1_scale: torch.Tensor | None = None
+
+    def __post_init__(self):
+        e, h, o = self.n_experts, self.hidden_dim, self.out_dim
+        n1 = h * (2 if self.gated else 1) if h > 0 else o
+        eight = self.W1.dtype == torch.float8_e4m3fn
+        object.__setattr__(self, "in_dtype", torch.float8_e4m3fn if eight else self.feat_dtype)
+        f32 = torch.float32
+        c = it_experts_desc(e, self.top_k, self.in_dim, h, o, _dtype_code(self.feat_dtype), _dtype_code(self.in_dtype), EXPERT_ACTS[self.act], int(self.gated),
+                            _addr("W1", self.W1, self.in_dtype, (e, self.in_dim, n1)), _addr("b1", self.b1, f32, (e, n1), True),
+                            _addr("W2", self.W2, self.feat_dtype, (e, h, o), True), _addr("b2", self.b2, f32, (e, o), True),
+                            _addr("w1_scale", self.w1_scale, f32, (e, n1), True))
+        object.__setattr__(self, "_c", c)
+
+
+def it_experts_workspace_bytes(d: ExpertsDesc, n: int) -> int:
+    out = C.c_size_t()
+    _check(lib().it_experts_workspace_bytes(C.byref(d._c), n, C.byref(out)))
+    return out.value
+
+
+def it_experts_forward(d: ExpertsDesc, x, ids, weights, out, workspace, x_scale=None, stream=None):
+    """out[v] = sum_j weights[v, j] * expert ids[v, j] of x[v] (an id outside the experts: none).  Returns out."""
+    n = x.shape[0]
+    f32 = torch.float32
+    _check(lib().it_experts_forward(C.byref(d._c), n, _addr("x", x, d.in_dtype, (n, d.in_dim)), _addr("x_scale", x_scale, f32, (n,), True),
+                                    _addr("ids", ids, torch.int32, (n, d.top_k)), _addr("weights", weights, f32, (n, d.top_k)),
+                                    _addr("out", out, d.feat_dtype, (n, d.out_dim)), _ptr(workspace), _nbytes(workspace), _stream(stream)))
+    return out
+
+
+def it_experts_check(workspace, stream=None):
+    """Synchronise the stream; raises ItError(IT_ERR_TIMEOUT) if the last it_experts_forward with this workspace gave up a bounded wait."""
+    _check(lib().it_experts_check(_ptr(workspace), _stream(stream)))
 
 
 def it_graph_destroy(g: Graph):

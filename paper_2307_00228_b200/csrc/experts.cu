@@ -1,0 +1,346 @@
+// it_experts_forward: checks, scratch, the form for few places (a product per place), and the sum over the places of a vertex.
+#include <cooperative_groups.h>
+#include <cuda_fp8.h>
+#include <math.h>
+
+#include "experts.cuh"
+
+namespace cg = cooperative_groups;
+
+namespace {
+
+// ----------------------------------------------------------------------------- few places: a product per place
+// A place is one (vertex, expert).  With few of them every weight is read about once and nothing else counts, so this is a matter of
+// having many loads of W in flight at once: a block takes 128 bytes of a row of W (8 lanes x 16 bytes) and a share of its rows, the
+// blocks of a cluster share the rows between them and add up over distributed shared memory, in their order.  fp32 throughout: the hidden row is not rounded.
+constexpr int ROWS_THREADS = 256, ROWS_WARPS = ROWS_THREADS / 32, ROWS_COL_LANES = 8, ROWS_UNROLL = 4;
+constexpr int ROWS_STEP = ROWS_WARPS * (32 / ROWS_COL_LANES);   // rows of W that a block reads side by side
+
+struct RowsParams {
+  int64_t units;            // places (first product) or vertices (second)
+  int k, n_experts, K, cols, chunks, act, gated_at;   // gated_at: first column of the second half (0: not gated)
+  const void *x;            // rows that are multiplied: of x (first product) or fp32 hidden rows
+  const float *x_scale;
+  const int32_t *ids;
+  const float *weights;
+  const void *W;
+  const float *bias, *w_scale;
+  int w_cols;               // columns of W
+  float *hidden;            // first product: [places, cols]
+  void *out;                // second product
+  int *status;
+};
+
+__device__ __forceinline__ float elem_f32(const float *p) { return *p; }
+__device__ __forceinline__ float elem_f32(const __nv_bfloat16 *p) { return __bfloat162float(*p); }
+__device__ __forceinline__ float elem_f32(const __nv_fp8_e4m3 *p) { return float(*p); }
+
+template <typename TW> struct WVec { static constexpr int N = 16 / (int)sizeof(TW); };
+template <typename TW> __device__ __forceinline__ void w_to_f32(const uint4 &q, float (&v)[WVec<TW>::N]) {
+  if constexpr (sizeof(TW) == 1) {
+    const uint32_t w[4] = {q.x, q.y, q.z, q.w};
+#pragma unroll
+    for (int i = 0; i < 8; ++i) {
+      const __half2_raw h = __nv_cvt_fp8x2_to_halfraw2((__nv_fp8x2_storage_t)(w[i >> 1] >> (16 * (i & 1))), __NV_E4M3);
+      const float2 f = __half22float2(__half2(h));
+      v[2 * i] = f.x; v[2 * i + 1] = f.y;
+    }
+  } else {
+    vec_to_f32(q, v);
+  }
+}
+
+// SECOND: the rows of W follow one another place by place of the vertex: row i is row i % K of the place i / K.
+template <typename TX, typename TW, bool SECOND, bool GATED, typename TO>
+__global__ void __launch_bounds__(ROWS_THREADS) expert_rows_kernel(const RowsParams p) {
+  constexpr int N = WVec<TW>::N, CB = ROWS_COL_LANES * N, PARTS = GATED ? 2 : 1;
+  __shared__ float part[ROWS_WARPS][PARTS * CB];
+  __shared__ float total[PARTS * CB];
+  cg::cluster_group cluster = cg::this_cluster();
+  const int share = (int)cluster.block_rank(), shares = (int)cluster.num_blocks();
+  const int64_t id = blockIdx.x / shares, unit = id / p.chunks;
+  const int c0 = (int)(id % p.chunks) * CB;
+  const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31, cl = lane % ROWS_COL_LANES, rl = lane / ROWS_COL_LANES;
+  const int col = c0 + cl * N;
+  if (SECOND) {
+    it_allow_next();
+    it_wait_prior();   // the hidden rows
+  } else {
+    it_wait_prior();
+    it_allow_next();   // only now: what the next kernel reads besides the hidden rows is then there
+    if (blockIdx.x == 0 && threadIdx.x == 0) *p.status = 0;
+  }
+  const int64_t place0 = SECOND ? unit * p.k : unit;
+  if (!SECOND && (unsigned)p.ids[place0] >= (unsigned)p.n_experts) return;   // (all blocks of the cluster)
+
+  float acc[PARTS][N];
+#pragma unroll
+  for (int g = 0; g < PARTS; ++g)
+#pragma unroll
+    for (int i = 0; i < N; ++i) acc[g][i] = 0.f;
+  for (int j = 0; j < (SECOND ? p.k : 1); ++j) {
+    const int64_t place = place0 + j;
+    const int e = p.ids[place];
+    if ((unsigned)e >= (unsigned)p.n_experts) continue;
+    // this block's share of the K rows
+    const int lo = (int)((int64_t)p.K * share / shares), hi = (int)((int64_t)p.K * (share + 1) / shares);
+    const TX *x = reinterpret_cast<const TX *>(p.x) + (SECOND ? place : place / p.k) * p.K;
+    const TW *w = reinterpret_cast<const TW *>(p.W) + (int64_t)e * p.K * p.w_cols + col;
+    const float f = SECOND ? p.weights[place] : 1.f;
+    for (int r0 = lo + warp * (32 / ROWS_COL_LANES) + rl; r0 < hi; r0 += ROWS_STEP * ROWS_UNROLL) {
+      uint4 q[PARTS][ROWS_UNROLL];
+      float xv[ROWS_UNROLL];
+#pragma unroll
+      for (int u = 0; u < ROWS_UNROLL; ++u) {
+        const int r = r0 + u * ROWS_STEP;
+        const bool in = r < hi && col < p.cols;
+        xv[u] = in ? elem_f32(x + r) * f : 0.f;
+#pragma unroll
+        for (int g = 0; g < PARTS; ++g)
+          q[g][u] = in ? __ldg(reinterpret_cast<const uint4 *>(w + (int64_t)r * p.w_cols + g * p.gated_at)) : make_uint4(0, 0, 0, 0);
+      }
+#pragma unroll
+      for (int u = 0; u < ROWS_UNROLL; ++u) {
+        if (r0 + u * ROWS_STEP >= hi) break;
+#pragma unroll
+        for (int g = 0; g < PARTS; ++g) {
+          float v[N];
+          w_to_f32<TW>(q[g][u], v);
+#pragma unroll
+          for (int i = 0; i < N; ++i) acc[g][i] = fmaf(xv[u], v[i], acc[g][i]);
+        }
+      }
+    }
+    if (SECOND && p.bias && share == 0 && warp == 0 && rl == 0 && col < p.cols) {
+#pragma unroll
+      for (int i = 0; i < N; ++i) acc[0][i] = fmaf(f, p.bias[(int64_t)e * p.cols + col + i], acc[0][i]);
+    }
+  }
+#pragma unroll
+  for (int g = 0; g < PARTS; ++g)
+#pragma unroll
+    for (int i = 0; i < N; ++i) {
+#pragma unroll
+      for (int o = ROWS_COL_LANES; o < 32; o <<= 1) acc[g][i] += __shfl_xor_sync(0xffffffffu, acc[g][i], o);
+      if (rl == 0) part[warp][g * CB + cl * N + i] = acc[g][i];
+    }
+  __syncthreads();
+  for (int c = threadIdx.x; c < PARTS * CB; c += ROWS_THREADS) {
+    float s = 0.f;
+#pragma unroll
+    for (int w = 0; w < ROWS_WARPS; ++w) s += part[w][c];
+    total[c] = s;
+  }
+  cluster.sync();
+  if (share == 0) {
+    for (int c = threadIdx.x; c < CB && c0 + c < p.cols; c += ROWS_THREADS) {
+      float s[PARTS];
+#pragma unroll
+      for (int g = 0; g < PARTS; ++g) {
+        s[g] = 0.f;
+        for (int b = 0; b < shares; ++b) s[g] += cluster.map_shared_rank(total, b)[g * CB + c];
+      }
+      if constexpr (SECOND) {
+        reinterpret_cast<TO *>(p.out)[unit * p.cols + c0 + c] = TO(s[0]);
+      } else {
+        const int e = p.ids[place0];
+        const float xs = p.x_scale ? p.x_scale[place0 / p.k] : 1.f;
+#pragma unroll
+        for (int g = 0; g < PARTS; ++g) {
+          const int64_t at = (int64_t)e * p.w_cols + g * p.gated_at + c0 + c;
+          if (p.w_scale) s[g] *= xs * p.w_scale[at];
+          if (p.bias) s[g] += p.bias[at];
+        }
+        const float a = it_expert_act(s[0], p.act);
+        p.hidden[place0 * p.cols + c0 + c] = GATED ? a * s[PARTS - 1] : a;
+      }
+    }
+  }
+  cluster.sync();   // nobody's totals go before they are read
+}
+
+template <typename TX, typename TW, bool SECOND, bool GATED, typename TO>
+it_status launch_rows(RowsParams p, int sms, double bytes, double flops, cudaStream_t st) {
+  constexpr int CB = ROWS_COL_LANES * WVec<TW>::N;
+  p.chunks = (p.cols + CB - 1) / CB;
+  // shares of about 128 rows, as long as the blocks still run side by side (eight of 256 threads an SM)
+  const int64_t base = p.units * p.chunks, rows = (int64_t)p.K * (SECOND ? p.k : 1);
+  int shares = 1;
+  while (shares < 8 && rows > 128 * (int64_t)shares && base * shares * 2 <= (int64_t)sms * 8) shares *= 2;
+  IT_REQUIRE(base * shares <= INT32_MAX, IT_ERR_UNSUPPORTED, "too many places for one launch");
+  cudaLaunchAttribute attr[2] = {};
+  attr[0].id = cudaLaunchAttributeProgrammaticStreamSerialization;
+  attr[0].val.programmaticStreamSerializationAllowed = 1;
+  attr[1].id = cudaLaunchAttributeClusterDimension;
+  attr[1].val.clusterDim.x = (unsigned)shares; attr[1].val.clusterDim.y = 1; attr[1].val.clusterDim.z = 1;
+  cudaLaunchConfig_t cfg{};
+  cfg.gridDim = dim3((unsigned)(base * shares)); cfg.blockDim = dim3(ROWS_THREADS); cfg.stream = st; cfg.attrs = attr; cfg.numAttrs = 2;
+  IT_LAUNCH(IT_K_EXPERT_ROWS, bytes, flops, st, IT_CUDA_TRY((cudaLaunchKernelEx(&cfg, expert_rows_kernel<TX, TW, SECOND, GATED, TO>, p))));
+  return IT_OK;
+}
+
+// ----------------------------------------------------------------------------- the places of a vertex added up
+// out[v] = sum_j weights[v, j] * y[position of place (v, j)], in the order of j.  y: fp32 rows, by place (position NULL) or where the
+// product left them.  Bound by DRAM: a read of every fp32 row, a write of the result.
+struct CombineParams {
+  int64_t n;
+  int k, n_experts, dim;
+  const float *y;
+  const int32_t *position;
+  const int32_t *ids;
+  const float *weights;
+  void *out;
+};
+template <typename T>
+__global__ void __launch_bounds__(256) expert_combine_kernel(const CombineParams p) {
+  it_allow_next();
+  it_wait_prior();
+  constexpr int N = kVec<T>;
+  const int per = p.dim / N;
+  const int64_t total = p.n * per;
+  for (int64_t i = blockIdx.x * (int64_t)blockDim.x + threadIdx.x; i < total; i += (int64_t)gridDim.x * blockDim.x) {
+    const int64_t v = i / per;
+    const int c = (int)(i - v * per) * N;
+    float acc[N];
+#pragma unroll
+    for (int q = 0; q < N; ++q) acc[q] = 0.f;
+    for (int j = 0; j < p.k; ++j) {
+      const int64_t place = v * p.k + j;
+      if ((unsigned)p.ids[place] >= (unsigned)p.n_experts) continue;
+      const float w = p.weights[place];
+      const float4 *row = reinterpret_cast<const float4 *>(p.y + (p.position ? (int64_t)p.position[place] : place) * p.dim + c);
+#pragma unroll
+      for (int q = 0; q < N / 4; ++q) {
+        const float4 f = row[q];
+        acc[4 * q] = fmaf(w, f.x, acc[4 * q]); acc[4 * q + 1] = fmaf(w, f.y, acc[4 * q + 1]);
+        acc[4 * q + 2] = fmaf(w, f.z, acc[4 * q + 2]); acc[4 * q + 3] = fmaf(w, f.w, acc[4 * q + 3]);
+      }
+    }
+    *reinterpret_cast<uint4 *>(reinterpret_cast<T *>(p.out) + v * p.dim + c) = f32_to_vec(acc);
+  }
+}
+
+it_status launch_combine(const it_experts_args &a, const float *y, const int32_t *position, cudaStream_t st) {
+  const CombineParams p{a.n, a.d.top_k, a.d.n_experts, a.d.out_dim, y, position, a.ids, a.weights, a.out};
+  const bool f32 = a.d.feat_dtype == IT_F32;
+  const int64_t threads = a.n * (a.d.out_dim / (f32 ? 4 : 8)), blocks = (threads + 255) / 256, most = (int64_t)a.sms * 32;
+  const dim3 grid((unsigned)(blocks < most ? blocks : most));
+  const double bytes = (double)a.n * a.d.out_dim * (4.0 * a.d.top_k + it_dtype_size(a.d.feat_dtype));
+  if (f32) IT_LAUNCH(IT_K_EXPERT_COMBINE, bytes, 0, st, IT_CUDA_TRY(it_launch_pdl(expert_combine_kernel<float>, grid, dim3(256), 0, st, p)));
+  else IT_LAUNCH(IT_K_EXPERT_COMBINE, bytes, 0, st, IT_CUDA_TRY(it_launch_pdl(expert_combine_kernel<__nv_bfloat16>, grid, dim3(256), 0, st, p)));
+  return IT_OK;
+}
+
+it_status few_places(const it_experts_args &a, float *hidden, cudaStream_t st) {
+  const it_experts_desc &d = a.d;
+  const int64_t places = a.n * d.top_k;
+  RowsParams p{};
+  p.k = d.top_k; p.n_experts = d.n_experts; p.ids = a.ids; p.weights = a.weights; p.act = d.act; p.status = a.status;
+  p.units = places; p.K = d.in_dim; p.cols = d.hidden_dim > 0 ? d.hidden_dim : d.out_dim; p.w_cols = a.n1; p.gated_at = d.gated ? d.hidden_dim : 0;
+  p.x = a.x; p.x_scale = a.x_scale; p.W = d.W1; p.bias = d.b1; p.w_scale = d.w1_scale; p.hidden = hidden;
+  const double f1 = 2.0 * places * d.in_dim * a.n1, f2 = 2.0 * places * d.hidden_dim * d.out_dim;
+  const bool f32 = d.feat_dtype == IT_F32;
+  if (d.in_dtype == IT_E4M3) {
+    if (d.gated) IT_TRY((launch_rows<__nv_fp8_e4m3, __nv_fp8_e4m3, false, true, float>(p, a.sms, 0, f1, st)));
+    else IT_TRY((launch_rows<__nv_fp8_e4m3, __nv_fp8_e4m3, false, false, float>(p, a.sms, 0, f1, st)));
+  } else if (f32) {
+    if (d.gated) IT_TRY((launch_rows<float, float, false, true, float>(p, a.sms, 0, f1, st)));
+    else IT_TRY((launch_rows<float, float, false, false, float>(p, a.sms, 0, f1, st)));
+  } else {
+    if (d.gated) IT_TRY((launch_rows<__nv_bfloat16, __nv_bfloat16, false, true, float>(p, a.sms, 0, f1, st)));
+    else IT_TRY((launch_rows<__nv_bfloat16, __nv_bfloat16, false, false, float>(p, a.sms, 0, f1, st)));
+  }
+  if (d.hidden_dim == 0) return launch_combine(a, hidden, nullptr, st);
+  p.units = a.n; p.K = d.hidden_dim; p.cols = p.w_cols = d.out_dim; p.gated_at = 0;
+  p.x = hidden; p.x_scale = nullptr; p.W = d.W2; p.bias = d.b2; p.w_scale = nullptr; p.out = a.out;
+  if (f32) return launch_rows<float, float, true, false, float>(p, a.sms, 0, f2, st);
+  return launch_rows<float, __nv_bfloat16, true, false, __nv_bfloat16>(p, a.sms, 0, f2, st);
+}
+
+// ----------------------------------------------------------------------------- checks and scratch
+it_status check(const it_experts_desc *d, int64_t n) {
+  IT_REQUIRE(d != nullptr, IT_ERR_INVALID_ARG, "description is NULL");
+  IT_REQUIRE(d->feat_dtype == IT_F32 || d->feat_dtype == IT_BF16, IT_ERR_INVALID_ARG, "bad feat_dtype");
+  IT_REQUIRE(d->in_dtype == d->feat_dtype || d->in_dtype == IT_E4M3, IT_ERR_INVALID_ARG, "in_dtype must be feat_dtype or IT_E4M3");
+  IT_REQUIRE(d->in_dtype != IT_E4M3 || d->feat_dtype == IT_BF16, IT_ERR_UNSUPPORTED, "states of IT_E4M3 go with feat_dtype IT_BF16");
+  IT_REQUIRE(d->act >= IT_ACT_NONE && d->act <= IT_ACT_SILU, IT_ERR_INVALID_ARG, "bad activation %d", (int)d->act);
+  IT_REQUIRE(n >= 0 && d->n_experts >= 1 && d->top_k >= 1, IT_ERR_INVALID_ARG, "bad shape (%lld vertices, %d experts, top_k %d)", (long long)n, d->n_experts, d->top_k);
+  IT_REQUIRE(d->in_dim > 0 && d->hidden_dim >= 0 && d->out_dim > 0, IT_ERR_INVALID_ARG, "dims must be positive");
+  IT_REQUIRE(!d->gated || d->hidden_dim > 0, IT_ERR_INVALID_ARG, "a gate needs hidden_dim > 0");
+  const int s = it_dtype_size(d->feat_dtype), s1 = d->in_dtype == IT_E4M3 ? 1 : s;
+  const int64_t first = d->hidden_dim > 0 ? d->hidden_dim : d->out_dim;
+  IT_REQUIRE((int64_t)d->in_dim * s1 % 16 == 0 && first * s1 % 16 == 0 && (int64_t)d->hidden_dim * s % 16 == 0 && (int64_t)d->out_dim * s % 16 == 0, IT_ERR_INVALID_ARG,
+             "rows must be a multiple of 16 bytes (in %d, hidden %d, out %d)", d->in_dim, d->hidden_dim, d->out_dim);
+  IT_REQUIRE(d->hidden_dim <= INT32_MAX / 2 && d->n_experts <= (1 << 20), IT_ERR_UNSUPPORTED, "too many experts or columns");
+  const int64_t places = INT32_MAX / (d->feat_dtype == IT_F32 ? 3 : 1) - 128 * (int64_t)d->n_experts;
+  IT_REQUIRE(places > 0 && n <= places / d->top_k, IT_ERR_UNSUPPORTED, "%lld vertices with %d places each: too many rows for 32 bits", (long long)n, d->top_k);
+  return IT_OK;
+}
+
+struct ExpertsWs { size_t off_hidden, bytes; };
+constexpr size_t kStatusBytes = 256;
+
+it_status plan(const it_experts_desc *d, int64_t n, ExpertsWs *w) {
+  IT_TRY(check(d, n));
+  const size_t places = (size_t)n * d->top_k;
+  w->off_hidden = kStatusBytes;
+  w->bytes = w->off_hidden + it_align_up(places * (size_t)(d->hidden_dim > 0 ? d->hidden_dim : d->out_dim) * 4);
+  return IT_OK;
+}
+
+}  // namespace
+
+extern "C" it_status it_experts_workspace_bytes(const it_experts_desc *d, int64_t n, size_t *out_bytes) {
+  IT_REQUIRE(out_bytes != nullptr, IT_ERR_INVALID_ARG, "out_bytes is NULL");
+  ExpertsWs w;
+  IT_TRY(plan(d, n, &w));
+  *out_bytes = w.bytes;
+  return IT_OK;
+}
+
+extern "C" it_status it_experts_forward(const it_experts_desc *d, int64_t n, const void *x, const float *x_scale, const int32_t *ids,
+                                        const float *weights, void *out, void *workspace, size_t workspace_bytes, void *stream) {
+  ExpertsWs w;
+  IT_TRY(plan(d, n, &w));
+  const bool eight = d->in_dtype == IT_E4M3;
+  IT_REQUIRE(d->W1 != nullptr, IT_ERR_INVALID_ARG, "W1 is NULL");
+  IT_REQUIRE((d->W2 != nullptr) == (d->hidden_dim > 0), IT_ERR_INVALID_ARG, "W2 goes with hidden_dim > 0, and only with it");
+  IT_REQUIRE(d->hidden_dim > 0 || d->b2 == nullptr, IT_ERR_INVALID_ARG, "b2 goes with hidden_dim > 0");
+  IT_REQUIRE(eight == (d->w1_scale != nullptr), IT_ERR_INVALID_ARG, "w1_scale goes with states of IT_E4M3, and only with them");
+  IT_REQUIRE(it_aligned(d->W1, 16) && it_aligned(d->W2, 16) && it_aligned(d->b1, 16) && it_aligned(d->b2, 16) && it_aligned(d->w1_scale, 16), IT_ERR_INVALID_ARG,
+             "the experts' arrays must be 16-byte aligned");
+  IT_REQUIRE(workspace != nullptr && it_aligned(workspace, 256), IT_ERR_WORKSPACE, "workspace is NULL or not 256-byte aligned");
+  IT_REQUIRE(workspace_bytes >= w.bytes, IT_ERR_WORKSPACE, "workspace has %zu bytes, it_experts_forward needs %zu", workspace_bytes, w.bytes);
+  cudaStream_t st = (cudaStream_t)stream;
+  if (n == 0) {   // nothing to do, and nothing that could have given up
+    IT_CUDA_TRY(cudaMemsetAsync(workspace, 0, sizeof(int), st));
+    return IT_OK;
+  }
+  IT_REQUIRE(x != nullptr && ids != nullptr && weights != nullptr && out != nullptr, IT_ERR_INVALID_ARG, "x / ids / weights / out is NULL");
+  IT_REQUIRE(eight == (x_scale != nullptr), IT_ERR_INVALID_ARG, "x_scale goes with states of IT_E4M3, and only with them");
+  IT_REQUIRE(it_aligned(x, 16) && it_aligned(out, 16) && it_aligned(ids, 4) && it_aligned(weights, 4) && it_aligned(x_scale, 4), IT_ERR_INVALID_ARG,
+             "x and out must be 16-byte aligned, ids, weights and x_scale 4-byte");
+  const int s = it_dtype_size(d->feat_dtype), s1 = eight ? 1 : s;
+  const int64_t n1 = d->hidden_dim > 0 ? (int64_t)d->hidden_dim * (d->gated ? 2 : 1) : d->out_dim;
+  const size_t E = (size_t)d->n_experts, ob = (size_t)n * d->out_dim * s, pb = (size_t)n * d->top_k * 4;
+  const struct { const void *p; size_t bytes; } in[] = {
+      {x, (size_t)n * d->in_dim * s1}, {x_scale, (size_t)n * 4}, {ids, pb}, {weights, pb}, {d->W1, E * d->in_dim * n1 * s1}, {d->b1, E * n1 * 4},
+      {d->W2, E * d->hidden_dim * d->out_dim * s}, {d->b2, E * d->out_dim * 4}, {d->w1_scale, E * n1 * 4}};
+  for (const auto &i : in)
+    IT_REQUIRE(!it_overlap(i.p, i.bytes, out, ob) && !it_overlap(i.p, i.bytes, workspace, workspace_bytes), IT_ERR_INVALID_ARG, "an input overlaps out or the workspace");
+  IT_REQUIRE(!it_overlap(out, ob, workspace, workspace_bytes), IT_ERR_INVALID_ARG, "out overlaps the workspace");
+  it_experts_args a{};
+  a.d = *d; a.n = n; a.n1 = (int)n1; a.x = x; a.x_scale = x_scale; a.ids = ids; a.weights = weights; a.out = out;
+  a.status = (int *)workspace; a.sms = it_current_sms();
+  return few_places(a, (float *)((char *)workspace + w.off_hidden), st);
+}
+
+extern "C" it_status it_experts_check(void *workspace, void *stream) {
+  IT_REQUIRE(workspace != nullptr && it_aligned(workspace, 256), IT_ERR_WORKSPACE, "workspace is NULL or not 256-byte aligned");
+  int word = 0;
+  cudaStream_t st = (cudaStream_t)stream;
+  IT_CUDA_TRY(cudaMemcpyAsync(&word, workspace, sizeof(int), cudaMemcpyDeviceToHost, st));
+  IT_CUDA_TRY(cudaStreamSynchronize(st));
+  IT_REQUIRE(word == 0, IT_ERR_TIMEOUT, "a kernel of it_experts_forward gave up a bounded wait: its output is not valid");
+  return IT_OK;
+}

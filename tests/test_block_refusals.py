@@ -1,0 +1,109 @@
+"""What the calls of an experts block refuse: checked on the host before anything is launched, so no GPU is needed."""
+import ctypes as C
+
+import pytest
+
+from paper_2307_00228_b200 import binding as B
+
+P = 1 << 20   # addresses that are never followed: a refused call launches nothing
+
+
+def _status(code, status):
+    assert status == B.STATUS_NAMES.index(code), (B.STATUS_NAMES[status], B.it_last_error_message())
+
+
+def norm(n=10, x=P, residual=None, sum_out=None, out=2 * P, scales=None, **kw):
+    d = B.it_norm_desc(**{**dict(dim=64, feat_dtype=1, out_dtype=1, eps=1e-5, weight=None), **kw})
+    return B.lib().it_residual_norm(C.byref(d), n, x, residual, sum_out, out, scales, None)
+
+
+@pytest.mark.parametrize("kw", [dict(feat_dtype=2), dict(feat_dtype=7), dict(out_dtype=0), dict(dim=0), dict(dim=-8), dict(dim=12), dict(n=-1), dict(eps=-1.0),
+                                dict(eps=float("nan")), dict(eps=float("inf")), dict(weight=P + 4), dict(x=None), dict(out=None), dict(x=P + 2), dict(out=2 * P + 8),
+                                dict(residual=3 * P + 8), dict(sum_out=3 * P + 8), dict(out_dtype=2), dict(scales=3 * P), dict(out_dtype=2, dim=24, scales=3 * P),
+                                dict(out=P + 16), dict(sum_out=P + 128), dict(sum_out=2 * P), dict(out_dtype=2, scales=3 * P, out=P), dict(out_dtype=2, scales=P),
+                                dict(out_dtype=2, scales=2 * P), dict(residual=3 * P, sum_out=3 * P + 64), dict(weight=2 * P), dict(n=1 << 62)], ids=str)
+def test_norm(kw):
+    _status("IT_ERR_INVALID_ARG", norm(**kw))
+
+
+def test_norm_null_description_and_no_rows():
+    _status("IT_ERR_INVALID_ARG", B.lib().it_residual_norm(None, 1, P, None, None, 2 * P, None, None))
+    _status("IT_OK", norm(n=0, x=None, out=None))
+
+
+def route(n=10, logits=P, ids=2 * P, weights=3 * P, **kw):
+    d = B.it_route_desc(**{**dict(n_experts=16, top_k=2, logit_dtype=0, score=0, balance_bias=None, n_groups=1, group_k=1, group_best=1, renormalise=1, weight_scale=1.0), **kw})
+    return B.lib().it_route(C.byref(d), n, logits, ids, weights, None)
+
+
+@pytest.mark.parametrize("kw", [dict(logit_dtype=2), dict(score=2), dict(score=-1), dict(n=-1), dict(n_experts=0), dict(top_k=0), dict(top_k=17), dict(n_groups=0), dict(n_groups=3),
+                                dict(group_k=0), dict(group_k=2), dict(group_best=0), dict(group_best=3), dict(weight_scale=float("inf")), dict(weight_scale=float("nan")),
+                                dict(logits=None), dict(ids=None), dict(weights=None), dict(logits=P + 2), dict(ids=2 * P + 1), dict(weights=3 * P + 2), dict(ids=P + 64),
+                                dict(weights=P), dict(ids=3 * P), dict(balance_bias=2 * P), dict(balance_bias=P + 1), dict(n=1 << 61)], ids=str)
+def test_route(kw):
+    _status("IT_ERR_INVALID_ARG", route(**kw))
+
+
+def test_route_limits():
+    _status("IT_ERR_UNSUPPORTED", route(n_experts=1025))
+    _status("IT_ERR_UNSUPPORTED", route(n_experts=64, top_k=33))
+    _status("IT_ERR_INVALID_ARG", B.lib().it_route(None, 1, P, 2 * P, 3 * P, None))
+    _status("IT_OK", route(n=0, logits=None, ids=None, weights=None))
+
+
+BIG = 1 << 30
+
+
+def experts(n=10, x=BIG, x_scale=None, ids=2 * BIG, weights=3 * BIG, out=4 * BIG, workspace=5 * BIG, bytes_=1 << 28, **kw):
+    d = B.it_experts_desc(**{**dict(n_experts=4, top_k=2, in_dim=64, hidden_dim=128, out_dim=64, feat_dtype=1, in_dtype=1, act=1, gated=0, W1=6 * BIG, b1=None, W2=7 * BIG, b2=None,
+                                    w1_scale=None), **kw})
+    return B.lib().it_experts_forward(C.byref(d), n, x, x_scale, ids, weights, out, workspace, bytes_, None)
+
+
+@pytest.mark.parametrize("kw", [dict(feat_dtype=2), dict(in_dtype=0), dict(act=4), dict(act=-1), dict(n=-1), dict(n_experts=0), dict(top_k=0), dict(in_dim=0), dict(hidden_dim=-8),
+                                dict(out_dim=0), dict(in_dim=60), dict(hidden_dim=60), dict(out_dim=60), dict(hidden_dim=0, gated=1, W2=None), dict(W2=None), dict(hidden_dim=0),
+                                dict(hidden_dim=0, W2=None, b2=8 * BIG), dict(W1=None), dict(x=None), dict(ids=None), dict(weights=None), dict(out=None), dict(x=BIG + 8),
+                                dict(out=4 * BIG + 8), dict(W1=6 * BIG + 8), dict(W2=7 * BIG + 2), dict(b1=8 * BIG + 4), dict(b2=8 * BIG + 8), dict(ids=2 * BIG + 2),
+                                dict(weights=3 * BIG + 1), dict(x_scale=9 * BIG), dict(w1_scale=9 * BIG), dict(in_dtype=2), dict(in_dtype=2, w1_scale=9 * BIG),
+                                dict(in_dtype=2, in_dim=72, w1_scale=9 * BIG, x_scale=10 * BIG), dict(out=BIG), dict(out=2 * BIG), dict(out=5 * BIG), dict(x=5 * BIG + 4096),
+                                dict(out=7 * BIG + 64), dict(W2=5 * BIG)], ids=str)
+def test_experts(kw):
+    _status("IT_ERR_INVALID_ARG", experts(**kw))
+
+
+def test_experts_limits():
+    _status("IT_ERR_UNSUPPORTED", experts(feat_dtype=0, in_dtype=2, w1_scale=9 * BIG, x_scale=10 * BIG))
+    _status("IT_ERR_UNSUPPORTED", experts(n=1 << 31))
+    _status("IT_ERR_UNSUPPORTED", experts(feat_dtype=0, in_dtype=0, n=400_000_000))
+    _status("IT_ERR_UNSUPPORTED", experts(n_experts=1 << 24))
+    _status("IT_ERR_WORKSPACE", experts(workspace=None))
+    _status("IT_ERR_WORKSPACE", experts(workspace=5 * BIG + 64))
+    _status("IT_ERR_WORKSPACE", experts(bytes_=300))
+    _status("IT_ERR_INVALID_ARG", B.lib().it_experts_forward(None, 1, P, None, P, P, P, P, 0, None))
+    _status("IT_ERR_INVALID_ARG", B.lib().it_experts_workspace_bytes(C.byref(B.it_experts_desc()), 1, None))
+    _status("IT_ERR_WORKSPACE", B.lib().it_experts_check(None, None))
+
+
+def test_layers_refuse_what_only_the_block_takes():
+    """8-bit states and SiLU belong to the block: a layer with them is refused by its checks, as it was."""
+    text = open(B.__file__.replace("binding.py", "csrc/api.cu")).read()
+    assert "L->act <= IT_ACT_ELU" in text and "L->feat_dtype == IT_F32 || L->feat_dtype == IT_BF16" in text
+
+
+def test_structures_match_the_header():
+    import os
+    import re
+    import subprocess
+    import tempfile
+    root = os.path.dirname(os.path.dirname(os.path.abspath(__file__)))
+    for s in (B.it_norm_desc, B.it_route_desc, B.it_experts_desc):
+        fields = [f[0] for f in s._fields_]
+        prog = "#include <stdio.h>\n#include <stddef.h>\n#include \"inferturbo.h\"\nint main(void){printf(\"%zu\", sizeof(" + s.__name__ + "));" + \
+            "".join(f'printf(" %zu", offsetof({s.__name__}, {f}));' for f in fields) + "return 0;}\n"
+        with tempfile.TemporaryDirectory() as d:
+            src, exe = os.path.join(d, "t.c"), os.path.join(d, "t")
+            open(src, "w").write(prog)
+            subprocess.check_call(["gcc", "-I", os.path.join(root, "include"), src, "-o", exe])
+            nums = [int(t) for t in subprocess.check_output([exe]).split()]
+        assert nums == [C.sizeof(s)] + [getattr(s, f).offset for f in fields]
+    assert re.search(r"IT_E4M3 = 2", open(os.path.join(root, "include", "inferturbo.h")).read())

@@ -1,0 +1,140 @@
+"""it_experts_forward against its formula in 64 bits."""
+import pytest
+import torch
+
+from paper_2307_00228_b200 import binding as B
+from block_util import BF16, F32, check_experts, experts_case, experts_desc, run_experts
+
+pytestmark = pytest.mark.gpu
+
+SHAPES = [  # n, experts, top_k, in, hidden, out
+    (1, 4, 2, 64, 128, 64), (1, 16, 2, 256, 1024, 256), (3, 8, 3, 48, 80, 112), (7, 3, 1, 128, 0, 128), (130, 4, 2, 64, 256, 64), (257, 5, 2, 96, 192, 32),
+    (1000, 16, 4, 128, 512, 128), (640, 1, 1, 16, 16, 16), (513, 7, 2, 272, 0, 528), (300, 40, 3, 512, 144, 256), (2000, 2, 2, 64, 64, 768)]
+
+
+@pytest.mark.parametrize("shape", SHAPES, ids=str)
+@pytest.mark.parametrize("kind", ["f32", "bf16", "eight"])
+@pytest.mark.parametrize("gated,act", [(False, "relu"), (True, "silu"), (False, "elu")])
+def test_against_formula(shape, kind, gated, act):
+    n, E, k, a, h, o = shape
+    c = experts_case(n + a, n, E, k, a, h, o, F32 if kind == "f32" else BF16, gated=gated and h > 0, act=act, eight=kind == "eight", masked=0.1 if n > 100 else 0.0)
+    check_experts(c, run_experts(c))
+
+
+@pytest.mark.parametrize("kind", ["f32", "bf16"])
+@pytest.mark.parametrize("n", [2, 5, 16, 31, 64, 100, 129, 500])
+def test_few_and_more_places(kind, n):
+    c = experts_case(n, n, 8, 2, 72, 136, 40, F32 if kind == "f32" else BF16, biased=False, act="none")
+    check_experts(c, run_experts(c))
+
+
+@pytest.mark.parametrize("n", [4, 900])
+@pytest.mark.parametrize("h", [0, 96])
+def test_places_without_an_expert(n, h):
+    c = experts_case(n, n, 6, 3, 64, h, 64, BF16, masked=0.5)
+    c["ids"][0] = -1
+    c["ids"][1] = torch.tensor([6, -2147483648, 2147483647], dtype=torch.int32)   # outside the experts: none
+    c["weights"][1] = float("nan")
+    got = run_experts(c)
+    assert (got[:2] == 0).all()
+    c["weights"][1] = 0
+    c["ids"][1] = -1
+    check_experts(c, got)
+    c["ids"][:] = -1
+    assert (run_experts(c) == 0).all()
+
+
+@pytest.mark.parametrize("n", [3, 700])
+def test_an_expert_named_twice(n):
+    c = experts_case(n, n, 3, 4, 64, 64, 64, BF16, repeat=True)
+    check_experts(c, run_experts(c))
+
+
+@pytest.mark.parametrize("skew", [0.9, 1.0])
+def test_one_expert_takes_nearly_all(skew):
+    c = experts_case(11, 3000, 32, 2, 64, 128, 64, BF16, skew=skew)
+    check_experts(c, run_experts(c))
+
+
+@pytest.mark.parametrize("kind", ["f32", "bf16", "eight"])
+def test_many_vertices(kind):
+    c = experts_case(12, 60_001, 16, 2, 128, 256, 128, F32 if kind == "f32" else BF16, eight=kind == "eight")
+    check_experts(c, run_experts(c), device="cuda")
+
+
+@pytest.mark.parametrize("E", [1, 300, 1500])
+def test_numbers_of_experts(E):
+    c = experts_case(13, 4000, E, 2, 32, 48, 32, BF16, repeat=True)
+    check_experts(c, run_experts(c))
+
+
+@pytest.mark.parametrize("n", [2, 800])
+def test_a_bad_row_stays_in_its_vertex(n):
+    c = experts_case(14, n, 4, 2, 64, 64, 64, BF16, act="silu")
+    want = run_experts(c)
+    c["x"][1, 3] = float("nan")
+    got = run_experts(c)
+    assert got[1].isnan().all()
+    keep = [i for i in range(n) if i != 1]
+    assert torch.equal(got[keep], want[keep])
+
+
+@pytest.mark.parametrize("kind", ["f32", "bf16", "eight"])
+@pytest.mark.parametrize("n", [2, 5000])
+def test_results_are_the_same_every_time(kind, n):
+    c = experts_case(15, n, 8, 3, 64, 128, 64, F32 if kind == "f32" else BF16, eight=kind == "eight")
+    d = experts_desc(c)
+    want = run_experts(c, desc=d)
+    for _ in range(3):
+        assert torch.equal(run_experts(c, desc=d), want)
+
+
+@pytest.mark.parametrize("n", [3, 2000])
+def test_captured_replays_take_new_inputs(n):
+    c = experts_case(16, n, 8, 2, 64, 128, 64, BF16)
+    other = experts_case(17, n, 8, 2, 64, 128, 64, BF16)
+    d = experts_desc(c)
+    x, ids, w = c["x"].cuda(), c["ids"].cuda(), c["weights"].cuda()
+    out = torch.zeros(n, 64, dtype=BF16, device="cuda")
+    ws = torch.empty(B.it_experts_workspace_bytes(d, n), dtype=torch.uint8, device="cuda")
+    graph = torch.cuda.CUDAGraph()
+    torch.cuda.synchronize()
+    with torch.cuda.graph(graph):
+        B.it_experts_forward(d, x, ids, w, out, ws)
+    for src in (c, other):
+        x.copy_(src["x"]); ids.copy_(src["ids"]); w.copy_(src["weights"])
+        graph.replay()
+        B.it_experts_check(ws)
+        assert torch.equal(out, run_experts({**c, "x": src["x"], "ids": src["ids"], "weights": src["weights"]}, desc=d))
+
+
+def test_two_streams_with_a_workspace_each():
+    cs = [experts_case(s, 3000, 8, 2, 64, 256, 64, BF16) for s in (18, 19)]
+    want = [run_experts(c) for c in cs]
+    streams = [torch.cuda.Stream(), torch.cuda.Stream()]
+    ds = [experts_desc(c) for c in cs]
+    args = [[c["x"].cuda(), c["ids"].cuda(), c["weights"].cuda(), torch.zeros(3000, 64, dtype=BF16, device="cuda"),
+             torch.empty(B.it_experts_workspace_bytes(d, 3000), dtype=torch.uint8, device="cuda")] for c, d in zip(cs, ds)]
+    torch.cuda.synchronize()
+    for _ in range(5):
+        for s, d, a in zip(streams, ds, args):
+            B.it_experts_forward(d, *a, stream=s)
+    torch.cuda.synchronize()
+    for a, w in zip(args, want):
+        assert torch.equal(a[3], w)
+
+
+def test_rows_and_bytes_behind_the_last_are_left():
+    c = experts_case(20, 1000, 8, 2, 64, 128, 64, BF16)
+    d = experts_desc(c)
+    need = B.it_experts_workspace_bytes(d, 1000)
+    ws = torch.full((need + 4096,), 0x5a, dtype=torch.uint8, device="cuda")
+    out = torch.full((1003, 64), 7.0, dtype=BF16, device="cuda")
+    B.it_experts_forward(d, c["x"].cuda(), c["ids"].cuda(), c["weights"].cuda(), out[:1000], ws[:need])
+    B.it_experts_check(ws)
+    assert (out[1000:] == 7).all() and (ws[need:] == 0x5a).all()
+
+
+def test_no_vertices():
+    c = experts_case(21, 0, 4, 2, 64, 64, 64, BF16)
+    assert run_experts(c).shape == (0, 64)

@@ -1,0 +1,155 @@
+"""it_route against its definition in 64 bits: the choice exactly, the weights to their rounding."""
+import numpy as np
+import pytest
+import torch
+
+from paper_2307_00228_b200 import binding as B
+from block_util import BF16, F32, route_reference
+
+pytestmark = pytest.mark.gpu
+
+# weights: expf 2 ulp, the rounded difference from the top (|x| < 20) 10 ulp, a sum of 8 to 32 experts a lane and 5 steps across lanes at half
+# an ulp each, two products and a division; twice where the sum of the chosen divides
+RTOL = 2 * (2 + 10 + 19 + 3) * 2.0 ** -23
+
+
+def _run(d, logits, stream=None):
+    n = logits.shape[0]
+    ids = torch.full((n + 1, d.top_k), 77, dtype=torch.int32, device="cuda")
+    w = torch.full((n + 1, d.top_k), 77.0, device="cuda")
+    B.it_route(d, logits, ids[:n], w[:n], stream=stream)
+    if stream is not None:
+        stream.synchronize()
+    assert (ids[n] == 77).all() and (w[n] == 77).all()   # rows behind the last are left
+    return ids[:n].cpu().numpy(), w[:n].cpu().numpy()
+
+
+def _check(d, logits, bias=None):
+    ids, w = _run(d, logits)
+    rid, rw = route_reference(d, logits.float().cpu().numpy(), None if bias is None else bias.cpu().numpy())
+    assert np.array_equal(ids, rid), np.argwhere(ids != rid)[:5]
+    assert np.allclose(w, rw, rtol=RTOL, atol=1e-30)
+
+
+def _logits(seed, n, e, dtype, masked=0.0):
+    g = torch.Generator(device="cuda").manual_seed(seed)
+    l = (1.5 * torch.randn(n, e, generator=g, device="cuda")).to(dtype)
+    if masked:
+        l[torch.rand(n, e, generator=g, device="cuda") < masked] = -float("inf")
+    return l
+
+
+EXPERTS = [1, 2, 5, 8, 9, 16, 17, 32, 33, 60, 64, 100, 128, 200, 256, 300, 512, 1000, 1024]
+
+
+@pytest.mark.parametrize("e", EXPERTS)
+@pytest.mark.parametrize("dtype", [F32, BF16])
+@pytest.mark.parametrize("score", ["softmax", "sigmoid"])
+@pytest.mark.parametrize("biased", [False, True])
+def test_choice_and_weights(e, dtype, score, biased):
+    for n, k, renorm in ((1, 1, True), (33, min(e, 2), False), (70, min(e, 8), True), (5, min(e, 32), True)):
+        l = _logits(e + n, n, e, dtype, masked=0.0 if n == 33 else 0.1)
+        bias = 0.1 * torch.randn(e, generator=torch.Generator().manual_seed(e)).cuda() if biased else None
+        _check(B.RouteDesc(n_experts=e, top_k=k, logit_dtype=dtype, score=score, balance_bias=bias, renormalise=renorm, weight_scale=1.0 if renorm else 2.5), l, bias)
+
+
+@pytest.mark.parametrize("e,groups,group_k", [(8, 2, 1), (16, 4, 2), (64, 8, 3), (60, 5, 2), (256, 8, 4), (96, 32, 7), (512, 16, 4), (1024, 1024, 9), (128, 64, 64)])
+@pytest.mark.parametrize("dtype", [F32, BF16])
+@pytest.mark.parametrize("score,biased", [("softmax", False), ("sigmoid", True), ("softmax", True)])
+def test_groups(e, groups, group_k, dtype, score, biased):
+    for best in (1, 2):
+        for masked in (0.0, 0.4):
+            l = _logits(e + best, 41, e, dtype, masked)
+            l[3] = -float("inf")
+            bias = 0.1 * torch.randn(e, generator=torch.Generator().manual_seed(e)).cuda() if biased else None
+            d = B.RouteDesc(n_experts=e, top_k=min(8, e // groups * group_k), logit_dtype=dtype, score=score, balance_bias=bias, n_groups=groups, group_k=group_k,
+                            group_best=best)
+            _check(d, l, bias)
+
+
+@pytest.mark.parametrize("e", [4, 16, 64, 256, 700])
+@pytest.mark.parametrize("biased", [False, True])
+def test_ties_go_to_the_lowest_index(e, biased):
+    l = torch.randint(0, 3, (50, e), generator=torch.Generator().manual_seed(e)).to(BF16).cuda()
+    bias = torch.zeros(e, device="cuda") if biased else None
+    _check(B.RouteDesc(n_experts=e, top_k=min(e, 6), logit_dtype=BF16, balance_bias=bias), l, bias)
+
+
+@pytest.mark.parametrize("score", ["softmax", "sigmoid"])
+@pytest.mark.parametrize("e", [12, 64, 256])
+def test_keys_closer_than_32_bits_resolve(score, e):
+    """A bias that makes all keys of the row nearly equal: they differ by its rounding to fp32 alone."""
+    for seed in range(12):
+        l = torch.randn(1, e, generator=torch.Generator().manual_seed(seed))
+        s = torch.softmax(l.double(), 1) if score == "softmax" else torch.sigmoid(l.double())
+        bias = (0.5 - s[0]).float()
+        d = B.RouteDesc(n_experts=e, top_k=5, logit_dtype=F32, score=score, balance_bias=bias.cuda())
+        _check(d, l.cuda(), bias)
+
+
+@pytest.mark.parametrize("e", [6, 48])
+def test_values_that_close_an_expert(e):
+    l = _logits(1, 12, e, F32)
+    l[0] = -float("inf")
+    l[1] = float("nan")
+    l[2, :] = float("nan"); l[2, 3] = 0.5
+    l[3, 2] = float("inf"); l[3, 4] = float("inf")
+    l[4, 1:] = -float("inf")
+    l[5] = 3e38; l[5, 1] = -3e38
+    l[6] = torch.finfo(F32).min
+    for score in ("softmax", "sigmoid"):
+        for renorm in (True, False):
+            d = B.RouteDesc(n_experts=e, top_k=3, logit_dtype=F32, score=score, renormalise=renorm)
+            _check(d, l)
+    bias = torch.zeros(e); bias[1] = -float("inf"); bias[2] = float("nan")
+    _check(B.RouteDesc(n_experts=e, top_k=3, logit_dtype=F32, score="sigmoid", balance_bias=bias.cuda()), l, bias)
+
+
+def test_peaked_rows():
+    """Scores far below the largest: their rounding comes from the difference of the logits."""
+    l = 25 * torch.randn(300, 64, generator=torch.Generator().manual_seed(2))
+    bias = torch.zeros(64)
+    d = B.RouteDesc(n_experts=64, top_k=8, logit_dtype=F32, balance_bias=bias.cuda())
+    ids, _ = _run(d, l.cuda())
+    rid, _ = route_reference(d, l.numpy(), bias.numpy())
+    assert np.array_equal(ids, rid)
+
+
+def test_unaligned_rows_and_views():
+    base = _logits(4, 3001, 24, BF16).flatten()
+    l = base[1:1 + 2000 * 24].view(2000, 24)   # rows that start at odd elements
+    _check(B.RouteDesc(n_experts=24, top_k=4, logit_dtype=BF16), l)
+
+
+def test_many_rows_are_the_same_every_time():
+    l = _logits(5, 300_001, 16, BF16)
+    d = B.RouteDesc(n_experts=16, top_k=2, logit_dtype=BF16)
+    a, b = _run(d, l), _run(d, l)
+    assert np.array_equal(a[0], b[0]) and np.array_equal(a[1], b[1])
+    rid, rw = route_reference(d, l[-700:].float().cpu().numpy(), None)
+    assert np.array_equal(a[0][-700:], rid) and np.allclose(a[1][-700:], rw, rtol=RTOL)
+
+
+def test_other_stream_and_captured_replays():
+    l = _logits(6, 500, 32, F32)
+    d = B.RouteDesc(n_experts=32, top_k=4, logit_dtype=F32)
+    want = _run(d, l)
+    s = torch.cuda.Stream()
+    s.wait_stream(torch.cuda.current_stream())
+    got = _run(d, l, stream=s)
+    assert np.array_equal(got[0], want[0]) and np.array_equal(got[1], want[1])
+    ids, w, lin = torch.zeros(500, 4, dtype=torch.int32, device="cuda"), torch.zeros(500, 4, device="cuda"), torch.zeros_like(l)
+    graph = torch.cuda.CUDAGraph()
+    torch.cuda.synchronize()
+    with torch.cuda.graph(graph):
+        B.it_route(d, lin, ids, w)
+    for sign in (1, -1):
+        lin.copy_(sign * l)
+        graph.replay()
+        want = _run(d, sign * l)
+        assert np.array_equal(ids.cpu().numpy(), want[0]) and np.array_equal(w.cpu().numpy(), want[1])
+
+
+def test_no_rows():
+    l = torch.empty(0, 8, device="cuda")
+    B.it_route(B.RouteDesc(n_experts=8, top_k=2, logit_dtype=F32), l, torch.empty(0, 2, dtype=torch.int32, device="cuda"), torch.empty(0, 2, device="cuda"))
