@@ -358,10 +358,11 @@ it_status it_route(const it_route_desc *d, int64_t n, const void *logits, int32_
  *   e4m3, x stands for x * x_scale[v] (fp32 [n], as it_residual_norm writes it) and W1[e, :, c] for W1[e, :, c] * w1_scale[e, c]
  *   (fp32, one per column of W1).  W2 is feat_dtype; b1, b2, weights are fp32.
  *   An id outside [0, n_experts) is no expert, whatever its weight; an expert may be named twice.
- *   Widths: every row of x, W1, W2 and out is a multiple of 16 bytes (gated: a row of hidden_dim of them too).  n * top_k and the padded places of the
- *   experts' rows are counted in 32 bits: n * top_k + 128 * n_experts < 2^31 (fp32: a third of that).
- *   The products run on the tensor cores with fp32 accumulators (fp32 operands as three bf16 parts, six products); the hidden row between the
- *   two products is stored in feat_dtype, the places of a vertex are added in fp32, in their order, and rounded once.
+ *   in_dim, hidden_dim and out_dim are multiples of 8 (in_dim and the width of F's first product of 16 with IT_E4M3), n_experts <= 4096.  The
+ *   places of all vertices, padded for every expert, are counted in 32 bits: n * top_k + 128 * n_experts < 2^31 (fp32: a third of that).
+ *   The products run on the tensor cores with fp32 accumulators (fp32 operands as three bf16 parts, six products: an infinity in them gives
+ *   NaN); the hidden row between the two products is stored in feat_dtype, the places of a vertex are added in fp32, in their order, and
+ *   rounded once.  Few places take products of their own, in fp32 throughout.
  *   workspace: device, 256-byte aligned, >= it_experts_workspace_bytes; calls that can overlap on the GPU need one each.
  *   x, ids, weights and the expert arrays may not overlap out or the workspace.
  * it_experts_check - waits for `stream` and reports whether the last it_experts_forward with this workspace gave up one of its bounded
@@ -445,6 +446,11 @@ it_status it_debug_expire_wait_fused(it_graph *g, const void *x, void *out, void
 /* And for the other forms of the product: 0, 1 messages reduced by four and by eight warps a tile, 2 messages written, 3 bf16 and
  * 4 fp32 weights streamed beside the operand, 5 fp32 with one accumulator.  buffer: device, 256-byte aligned, at least 32 MB of zeros. */
 it_status it_debug_expire_wait_form(it_graph *g, int form, void *buffer, size_t bytes, void *stream);
+
+/* And for it_experts_forward, with its arguments: its products without their operand copies.  it_experts_check then reports IT_ERR_TIMEOUT until the
+ * next it_experts_forward with this workspace.  More than few places (those take a form that waits for nothing). */
+it_status it_debug_expire_wait_experts(const it_experts_desc *d, int64_t n, const void *x, const float *x_scale, const int32_t *ids,
+                                       const float *weights, void *out, void *workspace, size_t workspace_bytes, void *stream);
 
 /* Frees the library-owned arrays of the graph.  NULL is accepted. */
 it_status it_graph_destroy(it_graph *g);

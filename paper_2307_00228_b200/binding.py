@@ -30,7 +30,7 @@ EXPORTS = ["it_graph_create", "it_split_hubs", "it_graph_get_split", "it_workspa
            "it_graph_set_edge_features", "it_debug_expire_wait", "it_graph_create_part", "it_layer_stages",
            "it_layer_transform", "it_layer_gather", "it_layer_update", "it_aggregate_finish", "it_debug_expire_wait_fused",
            "it_debug_expire_wait_form", "it_residual_norm", "it_route", "it_experts_workspace_bytes", "it_experts_forward",
-           "it_experts_check"]
+           "it_experts_check", "it_debug_expire_wait_experts"]
 
 
 class ItError(RuntimeError):
@@ -105,7 +105,9 @@ def lib() -> C.CDLL:
         L.it_experts_workspace_bytes.argtypes = [C.POINTER(it_experts_desc), i64, C.POINTER(C.c_size_t)]
         L.it_experts_forward.argtypes = [C.POINTER(it_experts_desc), i64, vp, vp, vp, vp, vp, vp, C.c_size_t, vp]
         L.it_experts_check.argtypes = [vp, vp]
-        for name in ("it_residual_norm", "it_route", "it_experts_workspace_bytes", "it_experts_forward", "it_experts_check"):
+        L.it_debug_expire_wait_experts.argtypes = L.it_experts_forward.argtypes
+        for name in ("it_residual_norm", "it_route", "it_experts_workspace_bytes", "it_experts_forward", "it_experts_check",
+                     "it_debug_expire_wait_experts"):
             getattr(L, name).restype = C.c_int
         L.it_status_string.argtypes = [C.c_int]
         L.it_status_string.restype = C.c_char_p
@@ -511,9 +513,18 @@ def it_experts_workspace_bytes(d: ExpertsDesc, n: int) -> int:
 
 def it_experts_forward(d: ExpertsDesc, x, ids, weights, out, workspace, x_scale=None, stream=None):
     """out[v] = sum_j weights[v, j] * expert ids[v, j] of x[v] (an id outside the experts: none).  Returns out."""
+    return _experts(lib().it_experts_forward, d, x, ids, weights, out, workspace, x_scale, stream)
+
+
+def it_debug_expire_wait_experts(d: ExpertsDesc, x, ids, weights, out, workspace, x_scale=None, stream=None):
+    """Test hook: it_experts_forward with its operand copies switched off, so that its bounded waits run out."""
+    return _experts(lib().it_debug_expire_wait_experts, d, x, ids, weights, out, workspace, x_scale, stream)
+
+
+def _experts(call, d, x, ids, weights, out, workspace, x_scale, stream):
     n = x.shape[0]
     f32 = torch.float32
-    _check(lib().it_experts_forward(C.byref(d._c), n, _addr("x", x, d.in_dtype, (n, d.in_dim)), _addr("x_scale", x_scale, f32, (n,), True),
+    _check(call(C.byref(d._c), n, _addr("x", x, d.in_dtype, (n, d.in_dim)), _addr("x_scale", x_scale, f32, (n,), True),
                                     _addr("ids", ids, torch.int32, (n, d.top_k)), _addr("weights", weights, f32, (n, d.top_k)),
                                     _addr("out", out, d.feat_dtype, (n, d.out_dim)), _ptr(workspace), _nbytes(workspace), _stream(stream)))
     return out

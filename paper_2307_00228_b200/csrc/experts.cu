@@ -258,6 +258,8 @@ it_status few_places(const it_experts_args &a, float *hidden, cudaStream_t st) {
 }
 
 // ----------------------------------------------------------------------------- checks and scratch
+constexpr int kMaxDim = 1 << 20, kMaxExperts = 4096;
+
 it_status check(const it_experts_desc *d, int64_t n) {
   IT_REQUIRE(d != nullptr, IT_ERR_INVALID_ARG, "description is NULL");
   IT_REQUIRE(d->feat_dtype == IT_F32 || d->feat_dtype == IT_BF16, IT_ERR_INVALID_ARG, "bad feat_dtype");
@@ -267,25 +269,91 @@ it_status check(const it_experts_desc *d, int64_t n) {
   IT_REQUIRE(n >= 0 && d->n_experts >= 1 && d->top_k >= 1, IT_ERR_INVALID_ARG, "bad shape (%lld vertices, %d experts, top_k %d)", (long long)n, d->n_experts, d->top_k);
   IT_REQUIRE(d->in_dim > 0 && d->hidden_dim >= 0 && d->out_dim > 0, IT_ERR_INVALID_ARG, "dims must be positive");
   IT_REQUIRE(!d->gated || d->hidden_dim > 0, IT_ERR_INVALID_ARG, "a gate needs hidden_dim > 0");
-  const int s = it_dtype_size(d->feat_dtype), s1 = d->in_dtype == IT_E4M3 ? 1 : s;
-  const int64_t first = d->hidden_dim > 0 ? d->hidden_dim : d->out_dim;
-  IT_REQUIRE((int64_t)d->in_dim * s1 % 16 == 0 && first * s1 % 16 == 0 && (int64_t)d->hidden_dim * s % 16 == 0 && (int64_t)d->out_dim * s % 16 == 0, IT_ERR_INVALID_ARG,
-             "rows must be a multiple of 16 bytes (in %d, hidden %d, out %d)", d->in_dim, d->hidden_dim, d->out_dim);
-  IT_REQUIRE(d->hidden_dim <= INT32_MAX / 2 && d->n_experts <= (1 << 20), IT_ERR_UNSUPPORTED, "too many experts or columns");
+  const int step1 = d->in_dtype == IT_E4M3 ? 16 : 8, first = d->hidden_dim > 0 ? d->hidden_dim : d->out_dim;
+  IT_REQUIRE(d->in_dim % step1 == 0 && first % step1 == 0 && d->hidden_dim % 8 == 0 && d->out_dim % 8 == 0, IT_ERR_INVALID_ARG,
+             "widths must be multiples of 8, rows of e4m3 of 16 (in %d, hidden %d, out %d)", d->in_dim, d->hidden_dim, d->out_dim);
+  IT_REQUIRE(d->in_dim <= kMaxDim && d->hidden_dim <= kMaxDim && d->out_dim <= kMaxDim, IT_ERR_UNSUPPORTED, "more than %d columns", kMaxDim);
+  IT_REQUIRE(d->n_experts <= kMaxExperts, IT_ERR_UNSUPPORTED, "%d experts, at most %d", d->n_experts, kMaxExperts);
   const int64_t places = INT32_MAX / (d->feat_dtype == IT_F32 ? 3 : 1) - 128 * (int64_t)d->n_experts;
   IT_REQUIRE(places > 0 && n <= places / d->top_k, IT_ERR_UNSUPPORTED, "%lld vertices with %d places each: too many rows for 32 bits", (long long)n, d->top_k);
   return IT_OK;
 }
 
-struct ExpertsWs { size_t off_hidden, bytes; };
+// Few places keep the form by place.  FEW_PLACES
+constexpr int64_t kFewPlaces = 64;
+
+struct ExpertsWs {
+  bool few;
+  size_t off_rows;                                   // few: fp32 rows by place
+  size_t off_order, off_position, off_tiles, off_counts, off_hidden, off_sums, off_x, off_w1, off_w2;   // (tiles: the number of tiles, then their experts)
+  int64_t tiles_max;
+  size_t bytes;
+};
 constexpr size_t kStatusBytes = 256;
 
 it_status plan(const it_experts_desc *d, int64_t n, ExpertsWs *w) {
   IT_TRY(check(d, n));
-  const size_t places = (size_t)n * d->top_k;
-  w->off_hidden = kStatusBytes;
-  w->bytes = w->off_hidden + it_align_up(places * (size_t)(d->hidden_dim > 0 ? d->hidden_dim : d->out_dim) * 4);
+  *w = ExpertsWs{};
+  const int64_t places = n * d->top_k;
+  const size_t cols = (size_t)(d->hidden_dim > 0 ? d->hidden_dim : d->out_dim);
+  size_t off = kStatusBytes;
+  auto take = [&](size_t bytes) { const size_t o = off; off += it_align_up(bytes); return o; };
+  w->few = places <= kFewPlaces;
+  if (w->few) {
+    w->off_rows = take((size_t)places * cols * 4);
+  } else {
+    const bool f32 = d->feat_dtype == IT_F32;
+    w->tiles_max = it_experts_tiles_max(places, d->n_experts);
+    const size_t rows = (size_t)w->tiles_max * 128, E = (size_t)d->n_experts, n1 = cols * (d->gated ? 2 : 1);
+    w->off_order = take(rows * 4);
+    w->off_position = take((size_t)places * 4);
+    w->off_tiles = take(((size_t)w->tiles_max + 1) * 4);
+    w->off_counts = take(it_experts_count_words(places, d->n_experts) * 4);
+    w->off_hidden = take(d->hidden_dim > 0 ? rows * cols * (f32 ? 6 : 2) : 0);
+    w->off_sums = take(d->top_k > 1 ? rows * (size_t)d->out_dim * 4 : 0);
+    w->off_x = take(f32 ? (size_t)n * d->in_dim * 6 : 0);
+    w->off_w1 = take(f32 ? E * d->in_dim * n1 * 6 : 0);
+    w->off_w2 = take(f32 ? E * d->hidden_dim * d->out_dim * 6 : 0);
+  }
+  w->bytes = off;
   return IT_OK;
+}
+
+// Many places: sorted by expert, one product (or two) over tiles of 128 places, the places of a vertex added up.
+it_status many_places(const it_experts_args &a, const ExpertsWs &w, char *ws, uint32_t spin_limit, int no_loads, cudaStream_t st) {
+  const it_experts_desc &d = a.d;
+  const bool f32 = d.feat_dtype == IT_F32, two = d.hidden_dim > 0;
+  it_experts_plan q{};
+  q.order = (int32_t *)(ws + w.off_order); q.position = (int32_t *)(ws + w.off_position); q.n_tiles = (int32_t *)(ws + w.off_tiles);
+  q.tile_expert = q.n_tiles + 1; q.counts = (int32_t *)(ws + w.off_counts); q.tiles_max = w.tiles_max;
+  IT_TRY(it_launch_experts_plan(a, q, st));
+  const void *x = a.x, *W1 = d.W1, *W2 = d.W2;
+  if (f32) {
+    it_experts_parts parts{};
+    auto part = [&](const void *src, size_t off, int64_t elems) {
+      parts.src[parts.count] = (const float *)src; parts.dst[parts.count] = (__nv_bfloat16 *)(ws + off); parts.elems[parts.count++] = elems;
+      return (const void *)(ws + off);
+    };
+    x = part(a.x, w.off_x, a.n * d.in_dim);
+    W1 = part(d.W1, w.off_w1, (int64_t)d.n_experts * d.in_dim * a.n1);
+    if (two) W2 = part(d.W2, w.off_w2, (int64_t)d.n_experts * d.hidden_dim * d.out_dim);
+    IT_TRY(it_launch_experts_parts(parts, a.sms, st));
+  }
+  const it_expert_store last = d.top_k > 1 ? IT_EXPERT_SUMS : (f32 ? IT_EXPERT_OUT_F32 : IT_EXPERT_OUT_BF16);
+  void *result = d.top_k > 1 ? (void *)(ws + w.off_sums) : a.out;
+  it_expert_gemm g{};
+  g.parts = f32 ? 3 : 1; g.spin_limit = spin_limit; g.no_loads = no_loads;
+  g.A = x; g.gather = 1; g.a_rows = a.n; g.W = W1; g.K = d.in_dim; g.w_cols = a.n1; g.cols = two ? d.hidden_dim : d.out_dim;
+  g.eight = d.in_dtype == IT_E4M3; g.act = d.act; g.gated = d.gated != 0; g.bias = d.b1; g.w_scale = d.w1_scale; g.x_scale = a.x_scale;
+  g.store = two ? (f32 ? IT_EXPERT_PARTS : IT_EXPERT_HIDDEN) : last;
+  g.dst = two ? (void *)(ws + w.off_hidden) : result;
+  IT_TRY(it_launch_expert_gemm(a, q, g, st));
+  if (two) {
+    g.A = ws + w.off_hidden; g.gather = 0; g.a_rows = w.tiles_max * 128; g.W = W2; g.K = d.hidden_dim; g.w_cols = g.cols = d.out_dim;
+    g.eight = 0; g.act = IT_ACT_NONE; g.gated = 0; g.bias = d.b2; g.w_scale = nullptr; g.x_scale = nullptr; g.store = last; g.dst = result;
+    IT_TRY(it_launch_expert_gemm(a, q, g, st));
+  }
+  return d.top_k > 1 ? launch_combine(a, (const float *)(ws + w.off_sums), q.position, st) : IT_OK;
 }
 
 }  // namespace
@@ -298,8 +366,9 @@ extern "C" it_status it_experts_workspace_bytes(const it_experts_desc *d, int64_
   return IT_OK;
 }
 
-extern "C" it_status it_experts_forward(const it_experts_desc *d, int64_t n, const void *x, const float *x_scale, const int32_t *ids,
-                                        const float *weights, void *out, void *workspace, size_t workspace_bytes, void *stream) {
+namespace {
+it_status forward(const it_experts_desc *d, int64_t n, const void *x, const float *x_scale, const int32_t *ids, const float *weights, void *out, void *workspace,
+                  size_t workspace_bytes, uint32_t spin_limit, int no_loads, cudaStream_t st) {
   ExpertsWs w;
   IT_TRY(plan(d, n, &w));
   const bool eight = d->in_dtype == IT_E4M3;
@@ -311,7 +380,6 @@ extern "C" it_status it_experts_forward(const it_experts_desc *d, int64_t n, con
              "the experts' arrays must be 16-byte aligned");
   IT_REQUIRE(workspace != nullptr && it_aligned(workspace, 256), IT_ERR_WORKSPACE, "workspace is NULL or not 256-byte aligned");
   IT_REQUIRE(workspace_bytes >= w.bytes, IT_ERR_WORKSPACE, "workspace has %zu bytes, it_experts_forward needs %zu", workspace_bytes, w.bytes);
-  cudaStream_t st = (cudaStream_t)stream;
   if (n == 0) {   // nothing to do, and nothing that could have given up
     IT_CUDA_TRY(cudaMemsetAsync(workspace, 0, sizeof(int), st));
     return IT_OK;
@@ -332,7 +400,22 @@ extern "C" it_status it_experts_forward(const it_experts_desc *d, int64_t n, con
   it_experts_args a{};
   a.d = *d; a.n = n; a.n1 = (int)n1; a.x = x; a.x_scale = x_scale; a.ids = ids; a.weights = weights; a.out = out;
   a.status = (int *)workspace; a.sms = it_current_sms();
-  return few_places(a, (float *)((char *)workspace + w.off_hidden), st);
+  char *ws = (char *)workspace;
+  return w.few ? few_places(a, (float *)(ws + w.off_rows), st) : many_places(a, w, ws, spin_limit, no_loads, st);
+}
+}  // namespace
+
+extern "C" it_status it_experts_forward(const it_experts_desc *d, int64_t n, const void *x, const float *x_scale, const int32_t *ids,
+                                        const float *weights, void *out, void *workspace, size_t workspace_bytes, void *stream) {
+  return forward(d, n, x, x_scale, ids, weights, out, workspace, workspace_bytes, 0, 0, (cudaStream_t)stream);
+}
+
+extern "C" it_status it_debug_expire_wait_experts(const it_experts_desc *d, int64_t n, const void *x, const float *x_scale, const int32_t *ids,
+                                                  const float *weights, void *out, void *workspace, size_t workspace_bytes, void *stream) {
+  ExpertsWs w;
+  IT_TRY(plan(d, n, &w));
+  IT_REQUIRE(n > 0 && !w.few, IT_ERR_UNSUPPORTED, "the form for few places has no waits");
+  return forward(d, n, x, x_scale, ids, weights, out, workspace, workspace_bytes, 4096, 1, (cudaStream_t)stream);
 }
 
 extern "C" it_status it_experts_check(void *workspace, void *stream) {

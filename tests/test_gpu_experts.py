@@ -138,3 +138,17 @@ def test_rows_and_bytes_behind_the_last_are_left():
 def test_no_vertices():
     c = experts_case(21, 0, 4, 2, 64, 64, 64, BF16)
     assert run_experts(c).shape == (0, 64)
+
+
+@pytest.mark.parametrize("kind", ["f32", "bf16", "eight"])
+@pytest.mark.parametrize("h,k", [(128, 2), (0, 1)])
+def test_waits_that_run_out_are_reported_and_over(kind, h, k):
+    c = experts_case(22, 700, 4, k, 64, h, 64, F32 if kind == "f32" else BF16, eight=kind == "eight")
+    d = experts_desc(c)
+    dev = lambda t: None if t is None else t.cuda()   # noqa: E731
+    out = torch.empty(700, 64, dtype=c["dtype"], device="cuda")
+    ws = torch.empty(B.it_experts_workspace_bytes(d, 700), dtype=torch.uint8, device="cuda")
+    B.it_debug_expire_wait_experts(d, dev(c["x"]), dev(c["ids"]), dev(c["weights"]), out, ws, x_scale=dev(c["x_scale"]))
+    with pytest.raises(B.ItError, match="IT_ERR_TIMEOUT"):
+        B.it_experts_check(ws)
+    check_experts(c, run_experts(c, desc=d, workspace=ws))
