@@ -14,9 +14,12 @@
 namespace {
 
 constexpr int EX_EPI_WARPS = 8;   // two per TMEM lane quarter, each takes every other chunk of columns
-constexpr int EX_THREADS = 64 + 32 * EX_EPI_WARPS;   // warp 0 TMA, warp 1 MMA + TMEM, warps 2-9 epilogue
+constexpr int EX_TMA_WARPS = 4;   // each fetches a quarter of a tile's rows: a copy of four rows takes some 50 cycles to issue
+constexpr int EX_EPI_WARP0 = EX_TMA_WARPS + 1;
+constexpr int EX_THREADS = 32 * (EX_EPI_WARP0 + EX_EPI_WARPS);   // warps 0-3 TMA, warp 4 MMA + TMEM, warps 5-12 epilogue
 constexpr int EX_STAGE_A = TC_BM * TC_KBLOCK_BYTES;
-constexpr int EX_STAGING = 4096;   // per epilogue warp: 32 rows of 128 bytes
+constexpr int EX_STAGING = 2048;   // per epilogue warp: 32 rows of 64 bytes (of 128 bytes they would cost a stage of operands)
+constexpr int EX_CONSTS = 2 * 128 * 4;   // per epilogue warp: bias and scale of its columns
 constexpr int EX_MAX_STAGES = 8;
 constexpr int EX_EPI_BACKOFF = 64, EX_TMA_BACKOFF = 32;   // ns between polls
 
@@ -46,6 +49,16 @@ __device__ __forceinline__ void ex_mma(uint32_t d_tmem, uint64_t a_desc, uint64_
         : "memory");
   } else {
     tc_mma<false>(d_tmem, a_desc, b_desc, idesc, accumulate);
+  }
+}
+
+__device__ __forceinline__ void expert_act(float (&v)[16], int act) {
+  if (act == IT_ACT_RELU) {
+#pragma unroll
+    for (int i = 0; i < 16; ++i) v[i] = fmaxf(v[i], 0.f);
+  } else if (act != IT_ACT_NONE) {
+#pragma unroll
+    for (int i = 0; i < 16; ++i) v[i] = it_expert_act(v[i], act);
   }
 }
 
@@ -85,7 +98,8 @@ expert_gemm_kernel(const __grid_constant__ CUtensorMap map_a, const __grid_const
 
   unsigned char *base = reinterpret_cast<unsigned char *>((reinterpret_cast<uintptr_t>(smem_raw) + 1023) & ~(uintptr_t)1023);
   unsigned char *staging = base + (size_t)p.stages * stage_bytes;
-  uint64_t *full = reinterpret_cast<uint64_t *>(staging + (STORE == IT_EXPERT_PARTS ? 0 : EX_EPI_WARPS * EX_STAGING));   // [stages]
+  unsigned char *consts = staging + (STORE == IT_EXPERT_PARTS ? 0 : EX_EPI_WARPS * EX_STAGING);
+  uint64_t *full = reinterpret_cast<uint64_t *>(consts + EX_EPI_WARPS * EX_CONSTS);   // [stages]
   uint64_t *empty = full + EX_MAX_STAGES;      // [stages]
   uint64_t *acc_full = empty + EX_MAX_STAGES;  // [2]
   uint64_t *acc_empty = acc_full + 2;          // [2]
@@ -97,7 +111,7 @@ expert_gemm_kernel(const __grid_constant__ CUtensorMap map_a, const __grid_const
 
   if (threadIdx.x == 0) {
     for (int s = 0; s < p.stages; ++s) {
-      mbar_init(&full[s], 1);
+      mbar_init(&full[s], p.gather_div ? EX_TMA_WARPS : 1);
       mbar_init(&empty[s], 1);
     }
     for (int a = 0; a < 2; ++a) {
@@ -108,7 +122,7 @@ expert_gemm_kernel(const __grid_constant__ CUtensorMap map_a, const __grid_const
     *abort_flag = 0;
     asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");
   }
-  if (warp == 1) {
+  if (warp == EX_TMA_WARPS) {
     tmem_alloc(tmem_slot, tmem_cols);
     tmem_relinquish();
   }
@@ -123,16 +137,17 @@ expert_gemm_kernel(const __grid_constant__ CUtensorMap map_a, const __grid_const
   const int64_t n_tiles = (int64_t)m_tiles * p.n_splits;
   const int KB = p.kb * p.passes;
 
-  if (warp == 0) {
-    // ------------------------------------------------------------------ TMA producer: every lane four rows of A, lane 0 the weights
+  if (warp < EX_TMA_WARPS) {
+    // ------------------------------------------------------------------ TMA producers: eight lanes of a warp four rows of A each; warp 0 the weights
     uint32_t stage = 0, phase = 0;
-    bool ok = !p.no_loads, came_round = false;
+    bool ok = !p.no_loads && (warp == 0 || p.gather_div), came_round = false;
+    const uint32_t my_bytes = (p.gather_div ? EX_STAGE_A / EX_TMA_WARPS : EX_STAGE_A) + (warp == 0 ? b_bytes : 0);
     for (int64_t tile = blockIdx.x; tile < n_tiles && ok; tile += gridDim.x) {
       const int m = (int)(tile / p.n_splits), c0 = (int)(tile % p.n_splits) * p.cols_per_tile;
       const int e = p.tile_expert[m];
       int4 rows = make_int4(0, 0, 0, 0);
-      if (p.gather_div) {
-        const int4 at = *reinterpret_cast<const int4 *>(p.order + (int64_t)m * TC_BM + lane * 4);
+      if (p.gather_div && lane < 8) {
+        const int4 at = *reinterpret_cast<const int4 *>(p.order + (int64_t)m * TC_BM + warp * 32 + lane * 4);
         // positions of no place read the first row, and their products go nowhere
         rows.x = at.x < 0 ? 0 : at.x / p.gather_div; rows.y = at.y < 0 ? 0 : at.y / p.gather_div;
         rows.z = at.z < 0 ? 0 : at.z / p.gather_div; rows.w = at.w < 0 ? 0 : at.w / p.gather_div;
@@ -141,24 +156,22 @@ expert_gemm_kernel(const __grid_constant__ CUtensorMap map_a, const __grid_const
         int pa, pb;
         pass_parts(p.passes, pass, &pa, &pb);
         const int row0 = pa * p.a_rows;
+        const int4 r = make_int4(rows.x + row0, rows.y + row0, rows.z + row0, rows.w + row0);
         for (int kb = 0; kb < p.kb; ++kb) {
           if (lane == 0) {
             ok = mbar_wait(&empty[stage], phase ^ 1u, abort_flag, p.spin_limit, EX_TMA_BACKOFF);
-            if (ok) mbar_arrive_expect_tx(&full[stage], (uint32_t)stage_bytes);
+            if (ok) mbar_arrive_expect_tx(&full[stage], my_bytes);
           }
           ok = __shfl_sync(0xffffffffu, (int)ok, 0);
           if (!ok) break;
           unsigned char *to = base + (size_t)stage * stage_bytes;
-          if (p.gather_div) {
-            const int4 r = make_int4(rows.x + row0, rows.y + row0, rows.z + row0, rows.w + row0);
-            tma_gather4(to + lane * 4 * TC_KBLOCK_BYTES, &map_a, kb * BK, r, &full[stage]);
-          }
-          if (lane == 0) {
-            if (!p.gather_div) tma_load_2d(to, &map_a, kb * BK, row0 + m * TC_BM, &full[stage]);
-            for (int c = 0; c < p.bn / BK; ++c) {
+          if (p.gather_div && lane < 8) tma_gather4(to + (warp * 32 + lane * 4) * TC_KBLOCK_BYTES, &map_a, kb * BK, r, &full[stage]);
+          if (warp == 0) {
+            if (lane == 8 && !p.gather_div) tma_load_2d(to, &map_a, kb * BK, row0 + m * TC_BM, &full[stage]);
+            if (lane >= 16 && lane - 16 < p.bn / BK) {   // a panel of the weights a lane
               // gated: the first half of the panels are columns of the gate, the second of what it gates
-              const int half = p.gated && c * BK >= p.cols_per_tile, col = half ? p.cols + c0 + c * BK - p.cols_per_tile : c0 + c * BK;
-              tma_load_3d(to + EX_STAGE_A + c * PANEL, &map_w, col, kb * BK, pb * p.n_experts + e, &full[stage]);
+              const int c = (lane - 16) * BK, col = p.gated && c >= p.cols_per_tile ? p.cols + c0 + c - p.cols_per_tile : c0 + c;
+              tma_load_3d(to + EX_STAGE_A + (lane - 16) * PANEL, &map_w, col, kb * BK, pb * p.n_experts + e, &full[stage]);
             }
           }
           if (++stage == (uint32_t)p.stages) { stage = 0; phase ^= 1u; came_round = true; }
@@ -166,8 +179,9 @@ expert_gemm_kernel(const __grid_constant__ CUtensorMap map_a, const __grid_const
       }
     }
     __syncwarp();
+    // (after an abort a stage may be armed by some of the warps only: this wait is then one for the copies in flight by its limit)
     if (lane == 0) ring_drain(full, (uint32_t)p.stages, stage, phase, came_round);
-  } else if (warp == 1) {
+  } else if (warp == EX_TMA_WARPS) {
     // ------------------------------------------------------------------ MMA issuer
     if (lane == 0) {
       // D = fp32, A K-major, B MN-major (bit 16), N = bn, M = 128; operands bf16 (1) or e4m3 (0)
@@ -200,62 +214,77 @@ expert_gemm_kernel(const __grid_constant__ CUtensorMap map_a, const __grid_const
     }
   } else {
     // ------------------------------------------------------------------ epilogue: a thread per row of the tile, a warp per 32 rows and chunk
-    const int quarter = warp & 3, sub = (warp - 2) >> 2;   // a warp may only touch TMEM lanes [32 * (warp % 4), +32)
+    const int quarter = warp & 3, sub = (warp - EX_EPI_WARP0) >> 2;   // a warp may only touch TMEM lanes [32 * (warp % 4), +32)
     constexpr bool F32_OUT = STORE == IT_EXPERT_SUMS || STORE == IT_EXPERT_OUT_F32;
-    constexpr int CHUNK = F32_OUT ? 32 : 64;   // columns of a 128-byte row of the staging tile
-    const uint32_t stage_s = smem_u32(staging) + (uint32_t)(warp - 2) * EX_STAGING, swz = (uint32_t)lane & 7u;
+    constexpr int CHUNK = F32_OUT ? 32 : 64;   // columns that a warp takes at a time: 128 bytes of a row
+    const uint32_t stage_s = smem_u32(staging) + (uint32_t)(warp - EX_EPI_WARP0) * EX_STAGING, swz = ((uint32_t)lane >> 1) & 3u;
+    float *bias_s = reinterpret_cast<float *>(consts + (warp - EX_EPI_WARP0) * EX_CONSTS), *scale_s = bias_s + 128;
     uint32_t acc = 0, acc_phase = 0;
     for (int64_t tile = blockIdx.x; tile < n_tiles; tile += gridDim.x) {
       const int m = (int)(tile / p.n_splits), c_tile = (int)(tile % p.n_splits) * p.cols_per_tile;
       const int64_t pos0 = (int64_t)m * TC_BM + quarter * 32;
       const int place = p.order[pos0 + lane], e = p.tile_expert[m];
       const int64_t w_row = (int64_t)e * p.w_cols;
+      {
+        // constants of this warp's columns, four a lane, in the order in which it comes to them (gated: 64 of the gate, then 64 of what it
+        // gates); loaded while the product runs (by the epilogue itself, column by column, they took four times the rest of it)
+        const int l4 = lane * 4;
+        const int c = c_tile + (p.gated ? sub * CHUNK + (l4 & 63) : ((l4 / CHUNK) * 2 + sub) * CHUNK + l4 % CHUNK);
+        const int64_t at = w_row + c + (p.gated && l4 >= 64 ? p.cols : 0);
+        float4 b = make_float4(0.f, 0.f, 0.f, 0.f), s = make_float4(1.f, 1.f, 1.f, 1.f);
+        if (c < p.cols) {
+          if (p.bias) b = __ldg(reinterpret_cast<const float4 *>(p.bias + at));
+          if constexpr (EIGHT) s = __ldg(reinterpret_cast<const float4 *>(p.w_scale + at));
+        }
+        __syncwarp();   // the previous tile's have been read
+        *reinterpret_cast<float4 *>(bias_s + l4) = b;
+        if constexpr (EIGHT) *reinterpret_cast<float4 *>(scale_s + l4) = s;
+      }
       const float xs = EIGHT && place >= 0 ? p.x_scale[place / p.x_div] : 1.f;
       const float weight = (STORE == IT_EXPERT_OUT_BF16 || STORE == IT_EXPERT_OUT_F32) && place >= 0 ? p.weights[place] : 1.f;
       const bool ok = mbar_wait(&acc_full[acc], acc_phase, abort_flag, p.spin_limit, EX_EPI_BACKOFF);
       if (!__all_sync(0xffffffffu, ok)) break;
       tc_fence_after();
       const uint32_t taddr = tmem_base + ((uint32_t)(quarter * 32) << 16) + acc * (uint32_t)p.bn;
-      for (int ch = sub * CHUNK; ch < p.cols_per_tile && c_tile + ch < p.cols; ch += 2 * CHUNK) {
+      int lc = 0;   // column among this warp's
+      for (int ch = sub * CHUNK; ch < p.cols_per_tile && c_tile + ch < p.cols; ch += 2 * CHUNK, lc += CHUNK) {
 #pragma unroll
         for (int q = 0; q < CHUNK; q += 16) {
           const int c = c_tile + ch + q;   // first column of 16 (columns past the last are computed and not stored)
           float v[16];
-          auto finish = [&](int tmem_col, int wc) {   // accumulator -> scaled, with the bias
+          auto finish = [&](int tmem_col, int at) {   // accumulator -> scaled, with the bias
             uint32_t r[16];
             tmem_ld16(taddr + (uint32_t)tmem_col, r);
+            float4 b[4], s[4];
+#pragma unroll
+            for (int i = 0; i < 4; ++i) {
+              b[i] = *reinterpret_cast<const float4 *>(bias_s + at + 4 * i);
+              if constexpr (EIGHT) s[i] = *reinterpret_cast<const float4 *>(scale_s + at + 4 * i);
+            }
             tmem_ld_wait();
 #pragma unroll
-            for (int i = 0; i < 16; ++i) v[i] = __uint_as_float(r[i]);
-            if (c >= p.cols) return;
-            // (a run of 16 columns may be cut at a multiple of 4)
-#pragma unroll
-            for (int i = 0; i < 16; i += 4) {
-              if (c + i >= p.cols) break;
+            for (int i = 0; i < 4; ++i) {
               if constexpr (EIGHT) {
-                const float4 s = __ldg(reinterpret_cast<const float4 *>(p.w_scale + w_row + wc + i));
-                v[i] *= xs * s.x; v[i + 1] *= xs * s.y; v[i + 2] *= xs * s.z; v[i + 3] *= xs * s.w;
-              }
-              if (p.bias) {
-                const float4 b = __ldg(reinterpret_cast<const float4 *>(p.bias + w_row + wc + i));
-                v[i] += b.x; v[i + 1] += b.y; v[i + 2] += b.z; v[i + 3] += b.w;
+                v[4 * i] = fmaf(__uint_as_float(r[4 * i]) * xs, s[i].x, b[i].x); v[4 * i + 1] = fmaf(__uint_as_float(r[4 * i + 1]) * xs, s[i].y, b[i].y);
+                v[4 * i + 2] = fmaf(__uint_as_float(r[4 * i + 2]) * xs, s[i].z, b[i].z); v[4 * i + 3] = fmaf(__uint_as_float(r[4 * i + 3]) * xs, s[i].w, b[i].w);
+              } else {
+                v[4 * i] = __uint_as_float(r[4 * i]) + b[i].x; v[4 * i + 1] = __uint_as_float(r[4 * i + 1]) + b[i].y;
+                v[4 * i + 2] = __uint_as_float(r[4 * i + 2]) + b[i].z; v[4 * i + 3] = __uint_as_float(r[4 * i + 3]) + b[i].w;
               }
             }
           };
-          float gate[16];
           if (p.gated) {
-            finish(ch + q, c);
+            float gate[16];
+            finish(ch + q, q);
+            expert_act(v, p.act);
 #pragma unroll
-            for (int i = 0; i < 16; ++i) gate[i] = it_expert_act(v[i], p.act);
-            finish(p.cols_per_tile + ch + q, p.cols + c);
+            for (int i = 0; i < 16; ++i) gate[i] = v[i];
+            finish(p.cols_per_tile + ch + q, 64 + q);
 #pragma unroll
             for (int i = 0; i < 16; ++i) v[i] *= gate[i];
           } else {
-            finish(ch + q, c);
-            if (p.act != IT_ACT_NONE) {
-#pragma unroll
-              for (int i = 0; i < 16; ++i) v[i] = it_expert_act(v[i], p.act);
-            }
+            finish(ch + q, lc + q);
+            expert_act(v, p.act);
           }
           if constexpr (STORE == IT_EXPERT_PARTS) {
             uint32_t w[3][8];
@@ -282,7 +311,7 @@ expert_gemm_kernel(const __grid_constant__ CUtensorMap map_a, const __grid_const
             }
 #pragma unroll
             for (int i = 0; i < 4; ++i)
-              st_shared_v4(stage_s + (uint32_t)lane * 128u + ((((uint32_t)q / 4 + i) ^ swz) << 4), __float_as_uint(v[4 * i]), __float_as_uint(v[4 * i + 1]),
+              st_shared_v4(stage_s + (uint32_t)lane * 64u + (((uint32_t)i ^ swz) << 4), __float_as_uint(v[4 * i]), __float_as_uint(v[4 * i + 1]),
                            __float_as_uint(v[4 * i + 2]), __float_as_uint(v[4 * i + 3]));
           } else {
             uint32_t w[8];
@@ -292,27 +321,28 @@ expert_gemm_kernel(const __grid_constant__ CUtensorMap map_a, const __grid_const
               const __nv_bfloat162 h = __floats2bfloat162_rn(v[2 * i], v[2 * i + 1]);
               w[i] = *reinterpret_cast<const uint32_t *>(&h);
             }
-            st_shared_v4(stage_s + (uint32_t)lane * 128u + ((((uint32_t)q / 8) ^ swz) << 4), w[0], w[1], w[2], w[3]);
-            st_shared_v4(stage_s + (uint32_t)lane * 128u + ((((uint32_t)q / 8 + 1) ^ swz) << 4), w[4], w[5], w[6], w[7]);
+            st_shared_v4(stage_s + (uint32_t)lane * 64u + ((((uint32_t)(q & 31) / 8) ^ swz) << 4), w[0], w[1], w[2], w[3]);
+            st_shared_v4(stage_s + (uint32_t)lane * 64u + ((((uint32_t)(q & 31) / 8 + 1) ^ swz) << 4), w[4], w[5], w[6], w[7]);
           }
-        }
-        if constexpr (STORE != IT_EXPERT_PARTS) {
-          // rows of 128 bytes out of the staging tile: eight lanes a row, whole lines of memory
-          __syncwarp();
-          constexpr int ESIZE = F32_OUT ? 4 : 2;
-          const int piece = lane & 7, c = c_tile + ch + piece * (16 / ESIZE);
+          if (STORE != IT_EXPERT_PARTS && (F32_OUT || (q & 16))) {
+            // rows of 64 bytes out of the staging tile, four lanes a row
+            __syncwarp();
+            constexpr int ESIZE = F32_OUT ? 4 : 2;
+            const int piece = lane & 3, c64 = c_tile + ch + (F32_OUT ? q : q - 16) + piece * (16 / ESIZE);
 #pragma unroll
-          for (int r0 = 0; r0 < 32; r0 += 4) {
-            const int r = r0 + (lane >> 3);
-            const int at = __shfl_sync(0xffffffffu, place, r);
-            uint4 q;
-            asm volatile("ld.shared.v4.b32 {%0, %1, %2, %3}, [%4];" : "=r"(q.x), "=r"(q.y), "=r"(q.z), "=r"(q.w)
-                         : "r"(stage_s + (uint32_t)r * 128u + ((uint32_t)(piece ^ (r & 7)) << 4)) : "memory");
-            if (at < 0 || c >= p.cols) continue;
-            const int64_t row = STORE == IT_EXPERT_OUT_BF16 || STORE == IT_EXPERT_OUT_F32 ? (int64_t)at : pos0 + r;
-            *reinterpret_cast<uint4 *>(reinterpret_cast<unsigned char *>(p.dst) + (row * p.cols + c) * ESIZE) = q;
+            for (int r0 = 0; r0 < 32; r0 += 8) {
+              const int r = r0 + (lane >> 2);
+              const int at = __shfl_sync(0xffffffffu, place, r);
+              uint4 d;
+              asm volatile("ld.shared.v4.b32 {%0, %1, %2, %3}, [%4];" : "=r"(d.x), "=r"(d.y), "=r"(d.z), "=r"(d.w)
+                           : "r"(stage_s + (uint32_t)r * 64u + ((uint32_t)(piece ^ ((r >> 1) & 3)) << 4)) : "memory");
+              if (at >= 0 && c64 < p.cols) {
+                const int64_t row = STORE == IT_EXPERT_OUT_BF16 || STORE == IT_EXPERT_OUT_F32 ? (int64_t)at : pos0 + r;
+                *reinterpret_cast<uint4 *>(reinterpret_cast<unsigned char *>(p.dst) + (row * p.cols + c64) * ESIZE) = d;
+              }
+            }
+            __syncwarp();
           }
-          __syncwarp();
         }
       }
       tc_fence_before();
@@ -327,7 +357,7 @@ expert_gemm_kernel(const __grid_constant__ CUtensorMap map_a, const __grid_const
   tc_fence_before();
   __syncthreads();
   if (threadIdx.x == 0 && *abort_flag) atomicExch(p.status, 1);
-  if (warp == 1) {
+  if (warp == EX_TMA_WARPS) {
     tc_fence_after();
     tmem_dealloc(tmem_base, tmem_cols);
   }
@@ -379,7 +409,7 @@ it_status it_launch_expert_gemm(const it_experts_args &a, const it_experts_plan 
   IT_TRY(encode(&ma, g.eight, g.A, 2, da, sa, ba));
   IT_TRY(encode(&mw, g.eight, g.W, 3, dw, sw, bw));
 
-  const int stage = EX_STAGE_A + p.bn * TC_KBLOCK_BYTES, fixed = 1024 + (g.store == IT_EXPERT_PARTS ? 0 : EX_EPI_WARPS * EX_STAGING) + (2 * EX_MAX_STAGES + 8) * 8;
+  const int stage = EX_STAGE_A + p.bn * TC_KBLOCK_BYTES, fixed = 1024 + (g.store == IT_EXPERT_PARTS ? 0 : EX_EPI_WARPS * EX_STAGING) + EX_EPI_WARPS * EX_CONSTS + (2 * EX_MAX_STAGES + 8) * 8;
   p.stages = (227 * 1024 - fixed) / stage;
   if (p.stages > EX_MAX_STAGES) p.stages = EX_MAX_STAGES;
   const int smem = fixed + p.stages * stage;
