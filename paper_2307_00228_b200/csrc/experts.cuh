@@ -66,7 +66,7 @@ it_status it_launch_expert_gemm(const it_experts_args &a, const it_experts_plan 
 __device__ __forceinline__ float it_expert_act(float v, int act) {
   if (act == IT_ACT_RELU) return fmaxf(v, 0.f);
   if (act == IT_ACT_ELU) return it_elu(v);
-  if (act == IT_ACT_SILU) return v / (1.f + it_exp(-v));
+  if (act == IT_ACT_SILU) return __fdividef(v, 1.f + it_exp(-v));   // (off by a few ulp; 0 where the divisor passes 2^126)
   return v;
 }
 #endif

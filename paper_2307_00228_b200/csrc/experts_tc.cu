@@ -1,34 +1,43 @@
 // The products of it_experts_forward on the tensor cores: one persistent, warp-specialised kernel over tiles of 128 places of one expert,
 //   D[128, cols] = A[places, K] * W[expert][K, cols]
 // with tcgen05.mma (accumulators in TMEM, two of them, so that a tile's epilogue runs beside the next tile's products), operands
-// staged by TMA in 128-byte-swizzled k-blocks.  The rows of A are fetched where they lie, four to a copy (tile::gather4), by the place's
-// vertex; the weights are taken as they are, [K, columns], which makes B an MN-major operand, so nothing is transposed or prepared.
+// staged in 128-byte-swizzled k-blocks.  The rows of A are fetched where they lie, by the place's vertex, with 16-byte asynchronous copies of four
+// warps (TMA gathers of four rows took 52 cycles each, 1650 a k-block: 40k vertices, 4 of 32, 768-1024 gated 730 us); rows in order and the
+// weights come by TMA, the weights taken as they are, [K, columns], which makes B an MN-major operand, so nothing is transposed or prepared.
 // bf16 (kind::f16), e4m3 (kind::f8f6f4), and fp32 as three bf16 parts a value in six products per k-block, the smallest first
 // (what is left out is 2^-24 of a term).
 //
 // Every wait on an mbarrier is bounded: when one gives up, the CTA raises a flag that all roles poll, waits for its copies and products in
 // flight, frees its TMEM and returns, and a status word in global memory is set.
+#include <type_traits>
+
 #include "experts.cuh"
 #include "tc.cuh"
 
 namespace {
 
-constexpr int EX_EPI_WARPS = 8;   // two per TMEM lane quarter, each takes every other chunk of columns
-constexpr int EX_TMA_WARPS = 4;   // each fetches a quarter of a tile's rows: a copy of four rows takes some 50 cycles to issue
-constexpr int EX_EPI_WARP0 = EX_TMA_WARPS + 1;
-constexpr int EX_THREADS = 32 * (EX_EPI_WARP0 + EX_EPI_WARPS);   // warps 0-3 TMA, warp 4 MMA + TMEM, warps 5-12 epilogue
+constexpr int EX_FETCH_WARPS = 4;  // rows found by place: each fetches a quarter of a tile's rows; the weights and rows in order: the first, by TMA
+constexpr int EX_MMA_WARP = 4, EX_META_WARP = 5, EX_EPI_WARP0 = 6;
+constexpr int EX_EPI_WARPS = 8;    // two per TMEM lane quarter, each takes every other 64 bytes of a row
+constexpr int EX_EPI_SUBS = EX_EPI_WARPS / 4;
+constexpr int EX_THREADS = 32 * (EX_EPI_WARP0 + EX_EPI_WARPS);
 constexpr int EX_STAGE_A = TC_BM * TC_KBLOCK_BYTES;
 constexpr int EX_STAGING = 2048;   // per epilogue warp: 32 rows of 64 bytes (of 128 bytes they would cost a stage of operands)
-constexpr int EX_CONSTS = 2 * 128 * 4;   // per epilogue warp: bias and scale of its columns
+// What the epilogue of a tile needs besides the product: places of the rows, their weights and scales, bias and scale of the columns.
+struct ExMeta { int32_t place[TC_BM]; float weight[TC_BM]; float bias[256]; };
+struct ExMetaEight : ExMeta { float xs[TC_BM]; float scale[256]; };
 constexpr int EX_MAX_STAGES = 8;
 constexpr int EX_EPI_BACKOFF = 64, EX_TMA_BACKOFF = 32;   // ns between polls
 
-__device__ __forceinline__ void tma_gather4(void *dst, const CUtensorMap *map, int c, const int4 &rows, uint64_t *bar) {
-  asm volatile(
-      "cp.async.bulk.tensor.2d.shared::cluster.global.tile::gather4.mbarrier::complete_tx::bytes [%0], [%1, {%3, %4, %5, %6, %7}], [%2];"
-      ::"r"(smem_u32(dst)), "l"(map), "r"(smem_u32(bar)), "r"(c), "r"(rows.x), "r"(rows.y), "r"(rows.z), "r"(rows.w)
-      : "memory");
+// 16 bytes of a row into shared memory, asynchronously; `bytes` 0: zeros.
+__device__ __forceinline__ void cp_async16(uint32_t dst, const void *src, uint32_t bytes) {
+  asm volatile("cp.async.cg.shared.global [%0], [%1], 16, %2;" ::"r"(dst), "l"(src), "r"(bytes) : "memory");
 }
+// One arrival (of those that the barrier was set up for) once all of this thread's copies so far are in.
+__device__ __forceinline__ void cp_async_arrive(uint64_t *bar) {
+  asm volatile("cp.async.mbarrier.arrive.noinc.shared::cta.b64 [%0];" ::"r"(smem_u32(bar)) : "memory");
+}
+__device__ __forceinline__ void cp_async_wait_all() { asm volatile("cp.async.wait_all;" ::: "memory"); }
 __device__ __forceinline__ void tma_load_3d(void *dst, const CUtensorMap *map, int c0, int c1, int c2, uint64_t *bar) {
   asm volatile(
       "cp.async.bulk.tensor.3d.shared::cluster.global.tile.mbarrier::complete_tx::bytes [%0], [%1, {%3, %4, %5}], [%2];"
@@ -52,18 +61,19 @@ __device__ __forceinline__ void ex_mma(uint32_t d_tmem, uint64_t a_desc, uint64_
   }
 }
 
-__device__ __forceinline__ void expert_act(float (&v)[16], int act) {
+template <int N> __device__ __forceinline__ void expert_act(float (&v)[N], int act) {
   if (act == IT_ACT_RELU) {
 #pragma unroll
-    for (int i = 0; i < 16; ++i) v[i] = fmaxf(v[i], 0.f);
+    for (int i = 0; i < N; ++i) v[i] = fmaxf(v[i], 0.f);
   } else if (act != IT_ACT_NONE) {
 #pragma unroll
-    for (int i = 0; i < 16; ++i) v[i] = it_expert_act(v[i], act);
+    for (int i = 0; i < N; ++i) v[i] = it_expert_act(v[i], act);
   }
 }
 
 struct ExParams {
   const int32_t *order, *tile_expert, *n_tiles;
+  const void *A;
   int tiles_max;
   int n_splits, bn, cols_per_tile;   // column tiles; columns of an accumulator; columns of the result in a tile (gated: bn / 2)
   int K, kb, passes;                 // k-blocks of a pass; passes: 1, or the six products of fp32 parts
@@ -87,23 +97,24 @@ __device__ __forceinline__ void pass_parts(int passes, int i, int *pa, int *pb) 
   *pb = passes == 1 ? 0 : (int)((B >> (4 * i)) & 15u);
 }
 
-template <bool EIGHT, it_expert_store STORE>
+template <bool EIGHT, it_expert_store STORE, bool GATED>
 __global__ void __launch_bounds__(EX_THREADS, 1)
 expert_gemm_kernel(const __grid_constant__ CUtensorMap map_a, const __grid_constant__ CUtensorMap map_w, const ExParams p) {
-  extern __shared__ unsigned char smem_raw[];
+  extern __shared__ __align__(1024) unsigned char base[];   // (the swizzle goes by addresses: stages start at multiples of 1024)
   const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
   constexpr int BK = EIGHT ? 128 : 64;                  // elements of a k-block, and columns of a panel
   constexpr int PANEL = BK * TC_KBLOCK_BYTES;           // bytes of a panel of W: BK rows x 128 bytes
   const int b_bytes = p.bn * TC_KBLOCK_BYTES, stage_bytes = EX_STAGE_A + b_bytes;
 
-  unsigned char *base = reinterpret_cast<unsigned char *>((reinterpret_cast<uintptr_t>(smem_raw) + 1023) & ~(uintptr_t)1023);
   unsigned char *staging = base + (size_t)p.stages * stage_bytes;
-  unsigned char *consts = staging + (STORE == IT_EXPERT_PARTS ? 0 : EX_EPI_WARPS * EX_STAGING);
-  uint64_t *full = reinterpret_cast<uint64_t *>(consts + EX_EPI_WARPS * EX_CONSTS);   // [stages]
+  using Meta = std::conditional_t<EIGHT, ExMetaEight, ExMeta>;
+  Meta *meta = reinterpret_cast<Meta *>(staging + EX_EPI_WARPS * EX_STAGING);   // [2], one per accumulator
+  uint64_t *full = reinterpret_cast<uint64_t *>(meta + 2);   // [stages]
   uint64_t *empty = full + EX_MAX_STAGES;      // [stages]
   uint64_t *acc_full = empty + EX_MAX_STAGES;  // [2]
   uint64_t *acc_empty = acc_full + 2;          // [2]
-  uint64_t *mma_done = acc_empty + 2;          // [1]
+  uint64_t *meta_full = acc_empty + 2;         // [2]
+  uint64_t *mma_done = meta_full + 2;          // [1]
   uint32_t *tmem_slot = reinterpret_cast<uint32_t *>(mma_done + 1);
   volatile int *abort_flag = reinterpret_cast<volatile int *>(tmem_slot + 1);
   uint32_t tmem_cols = 32;
@@ -111,18 +122,19 @@ expert_gemm_kernel(const __grid_constant__ CUtensorMap map_a, const __grid_const
 
   if (threadIdx.x == 0) {
     for (int s = 0; s < p.stages; ++s) {
-      mbar_init(&full[s], p.gather_div ? EX_TMA_WARPS : 1);
+      mbar_init(&full[s], p.gather_div ? 32 * EX_FETCH_WARPS + 1 : 1);
       mbar_init(&empty[s], 1);
     }
     for (int a = 0; a < 2; ++a) {
       mbar_init(&acc_full[a], 1);
+      mbar_init(&meta_full[a], 1);
       mbar_init(&acc_empty[a], EX_EPI_WARPS);
     }
     mbar_init(mma_done, 1);
     *abort_flag = 0;
     asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");
   }
-  if (warp == EX_TMA_WARPS) {
+  if (warp == EX_MMA_WARP) {
     tmem_alloc(tmem_slot, tmem_cols);
     tmem_relinquish();
   }
@@ -134,54 +146,84 @@ expert_gemm_kernel(const __grid_constant__ CUtensorMap map_a, const __grid_const
   const uint32_t tmem_base = *tmem_slot;
   int m_tiles = *p.n_tiles;
   m_tiles = m_tiles < p.tiles_max ? m_tiles : p.tiles_max;
-  const int64_t n_tiles = (int64_t)m_tiles * p.n_splits;
+  const uint32_t splits = (uint32_t)p.n_splits, n_tiles = (uint32_t)m_tiles * splits;   // (below 2^31)
   const int KB = p.kb * p.passes;
 
-  if (warp < EX_TMA_WARPS) {
-    // ------------------------------------------------------------------ TMA producers: eight lanes of a warp four rows of A each; warp 0 the weights
+  if (warp < EX_FETCH_WARPS) {
+    // ------------------------------------------------------------------ producers: rows found by place by all four warps, 16 bytes a lane;
+    // weights, and rows in order, by TMA from the first
     uint32_t stage = 0, phase = 0;
-    bool ok = !p.no_loads && (warp == 0 || p.gather_div), came_round = false;
-    const uint32_t my_bytes = (p.gather_div ? EX_STAGE_A / EX_TMA_WARPS : EX_STAGE_A) + (warp == 0 ? b_bytes : 0);
-    for (int64_t tile = blockIdx.x; tile < n_tiles && ok; tile += gridDim.x) {
-      const int m = (int)(tile / p.n_splits), c0 = (int)(tile % p.n_splits) * p.cols_per_tile;
-      const int e = p.tile_expert[m];
-      int4 rows = make_int4(0, 0, 0, 0);
-      if (p.gather_div && lane < 8) {
-        const int4 at = *reinterpret_cast<const int4 *>(p.order + (int64_t)m * TC_BM + warp * 32 + lane * 4);
-        // positions of no place read the first row, and their products go nowhere
-        rows.x = at.x < 0 ? 0 : at.x / p.gather_div; rows.y = at.y < 0 ? 0 : at.y / p.gather_div;
-        rows.z = at.z < 0 ? 0 : at.z / p.gather_div; rows.w = at.w < 0 ? 0 : at.w / p.gather_div;
+    const bool gather = p.gather_div > 0;
+    bool ok = !p.no_loads && (warp == 0 || gather), came_round = false;
+    const uint32_t tma_bytes = (gather ? 0 : EX_STAGE_A) + b_bytes;
+    const int chunk = lane & 7;
+    uint32_t dst[8];   // where this lane's 16 bytes of its eight rows go in a stage (128-byte swizzle)
+#pragma unroll
+    for (int i = 0; i < 8; ++i) {
+      const int r = warp * 32 + i * 4 + (lane >> 3);
+      dst[i] = (uint32_t)r * TC_KBLOCK_BYTES + (uint32_t)((chunk ^ (r & 7)) << 4);
+    }
+    // (what a tile is about is looked up while the tile before it is fetched)
+    auto lookup = [&](uint32_t tile, int &e, int &place) {
+      if (tile >= n_tiles) return;
+      const uint32_t m = tile / splits;
+      e = p.tile_expert[m];
+      if (gather) place = p.order[(int64_t)m * TC_BM + warp * 32 + lane];
+    };
+    int e_next = 0, place_next = -1;
+    lookup(blockIdx.x, e_next, place_next);
+    for (uint32_t tile = blockIdx.x; tile < n_tiles && ok; tile += gridDim.x) {
+      const int m = (int)(tile / splits), c0 = (int)(tile % splits) * p.cols_per_tile;
+      const int e = e_next, place = place_next;
+      lookup(tile + gridDim.x, e_next, place_next);
+      const unsigned char *src[8];
+      uint32_t real = 0;   // bit i: row i of this lane's has a place
+      if (gather) {
+        const int row = place < 0 ? -1 : place / p.gather_div;
+#pragma unroll
+        for (int i = 0; i < 8; ++i) {
+          const int r = __shfl_sync(0xffffffffu, row, i * 4 + (lane >> 3));
+          src[i] = reinterpret_cast<const unsigned char *>(p.A) + ((int64_t)(r < 0 ? 0 : r) * p.K) * (EIGHT ? 1 : 2) + chunk * 16;
+          real |= (r >= 0 ? 1u : 0u) << i;
+        }
       }
       for (int pass = 0; pass < p.passes && ok; ++pass) {
         int pa, pb;
         pass_parts(p.passes, pass, &pa, &pb);
-        const int row0 = pa * p.a_rows;
-        const int4 r = make_int4(rows.x + row0, rows.y + row0, rows.z + row0, rows.w + row0);
+        const int64_t part = (int64_t)pa * p.a_rows * p.K * 2;   // (more than one pass: bf16)
         for (int kb = 0; kb < p.kb; ++kb) {
           if (lane == 0) {
             ok = mbar_wait(&empty[stage], phase ^ 1u, abort_flag, p.spin_limit, EX_TMA_BACKOFF);
-            if (ok) mbar_arrive_expect_tx(&full[stage], my_bytes);
+            if (ok && warp == 0) mbar_arrive_expect_tx(&full[stage], tma_bytes);
           }
           ok = __shfl_sync(0xffffffffu, (int)ok, 0);
           if (!ok) break;
           unsigned char *to = base + (size_t)stage * stage_bytes;
-          if (p.gather_div && lane < 8) tma_gather4(to + (warp * 32 + lane * 4) * TC_KBLOCK_BYTES, &map_a, kb * BK, r, &full[stage]);
           if (warp == 0) {
-            if (lane == 8 && !p.gather_div) tma_load_2d(to, &map_a, kb * BK, row0 + m * TC_BM, &full[stage]);
+            if (lane == 8 && !gather) tma_load_2d(to, &map_a, kb * BK, pa * p.a_rows + m * TC_BM, &full[stage]);
             if (lane >= 16 && lane - 16 < p.bn / BK) {   // a panel of the weights a lane
               // gated: the first half of the panels are columns of the gate, the second of what it gates
-              const int c = (lane - 16) * BK, col = p.gated && c >= p.cols_per_tile ? p.cols + c0 + c - p.cols_per_tile : c0 + c;
+              const int c = (lane - 16) * BK, col = GATED && c >= p.cols_per_tile ? p.cols + c0 + c - p.cols_per_tile : c0 + c;
               tma_load_3d(to + EX_STAGE_A + (lane - 16) * PANEL, &map_w, col, kb * BK, pb * p.n_experts + e, &full[stage]);
             }
+            __syncwarp();
+          }
+          if (gather) {
+            const uint32_t to_s = smem_u32(to);
+            const bool in = kb * TC_KBLOCK_BYTES + chunk * 16 < p.K * (EIGHT ? 1 : 2);   // (rows are multiples of 16 bytes)
+#pragma unroll
+            for (int i = 0; i < 8; ++i) cp_async16(to_s + dst[i], in ? src[i] + part + (int64_t)kb * TC_KBLOCK_BYTES : p.A, in && ((real >> i) & 1u) ? 16u : 0u);
+            cp_async_arrive(&full[stage]);
           }
           if (++stage == (uint32_t)p.stages) { stage = 0; phase ^= 1u; came_round = true; }
         }
       }
     }
     __syncwarp();
-    // (after an abort a stage may be armed by some of the warps only: this wait is then one for the copies in flight by its limit)
-    if (lane == 0) ring_drain(full, (uint32_t)p.stages, stage, phase, came_round);
-  } else if (warp == EX_TMA_WARPS) {
+    cp_async_wait_all();
+    // (after an abort a stage may lack another warp's arrivals: the wait for the copies in flight then ends by its limit)
+    if (lane == 0 && warp == 0) ring_drain(full, (uint32_t)p.stages, stage, phase, came_round);
+  } else if (warp == EX_MMA_WARP) {
     // ------------------------------------------------------------------ MMA issuer
     if (lane == 0) {
       // D = fp32, A K-major, B MN-major (bit 16), N = bn, M = 128; operands bf16 (1) or e4m3 (0)
@@ -189,7 +231,7 @@ expert_gemm_kernel(const __grid_constant__ CUtensorMap map_a, const __grid_const
       const uint32_t idesc = (1u << 4) | (fmt << 7) | (fmt << 10) | (1u << 16) | ((uint32_t)(p.bn >> 3) << 17) | ((uint32_t)(TC_BM >> 4) << 24);
       uint32_t stage = 0, phase = 0, acc = 0, acc_phase = 0;
       bool ok = true;
-      for (int64_t tile = blockIdx.x; tile < n_tiles && ok; tile += gridDim.x) {
+      for (uint32_t tile = blockIdx.x; tile < n_tiles && ok; tile += gridDim.x) {
         ok = mbar_wait(&acc_empty[acc], acc_phase ^ 1u, abort_flag, p.spin_limit);
         if (!ok) break;
         tc_fence_after();
@@ -197,6 +239,8 @@ expert_gemm_kernel(const __grid_constant__ CUtensorMap map_a, const __grid_const
         for (int kb = 0; kb < KB; ++kb) {
           ok = mbar_wait(&full[stage], phase, abort_flag, p.spin_limit);
           if (!ok) break;
+          // gathered rows were written by the threads of the other warps: what follows reads them through the tensor core's path
+          if (p.gather_div) asm volatile("fence.proxy.async.shared::cta;" ::: "memory");
           tc_fence_after();
           const uint32_t a_s = smem_u32(base + (size_t)stage * stage_bytes), b_s = a_s + EX_STAGE_A;
 #pragma unroll
@@ -212,137 +256,168 @@ expert_gemm_kernel(const __grid_constant__ CUtensorMap map_a, const __grid_const
       tc_commit(mma_done);
       mbar_drain(mma_done, 0);
     }
-  } else {
-    // ------------------------------------------------------------------ epilogue: a thread per row of the tile, a warp per 32 rows and chunk
-    const int quarter = warp & 3, sub = (warp - EX_EPI_WARP0) >> 2;   // a warp may only touch TMEM lanes [32 * (warp % 4), +32)
-    constexpr bool F32_OUT = STORE == IT_EXPERT_SUMS || STORE == IT_EXPERT_OUT_F32;
-    constexpr int CHUNK = F32_OUT ? 32 : 64;   // columns that a warp takes at a time: 128 bytes of a row
-    const uint32_t stage_s = smem_u32(staging) + (uint32_t)(warp - EX_EPI_WARP0) * EX_STAGING, swz = ((uint32_t)lane >> 1) & 3u;
-    float *bias_s = reinterpret_cast<float *>(consts + (warp - EX_EPI_WARP0) * EX_CONSTS), *scale_s = bias_s + 128;
+  } else if (warp == EX_META_WARP) {
+    // ------------------------------------------------------------------ what the epilogue needs, ahead of it: two loads, one behind the other, for
+    // every tile, and four rows and columns a lane.  (Made by the epilogue where it needs them, these waits took most of its time.)
     uint32_t acc = 0, acc_phase = 0;
-    for (int64_t tile = blockIdx.x; tile < n_tiles; tile += gridDim.x) {
-      const int m = (int)(tile / p.n_splits), c_tile = (int)(tile % p.n_splits) * p.cols_per_tile;
-      const int64_t pos0 = (int64_t)m * TC_BM + quarter * 32;
-      const int place = p.order[pos0 + lane], e = p.tile_expert[m];
-      const int64_t w_row = (int64_t)e * p.w_cols;
-      {
-        // constants of this warp's columns, four a lane, in the order in which it comes to them (gated: 64 of the gate, then 64 of what it
-        // gates); loaded while the product runs (by the epilogue itself, column by column, they took four times the rest of it)
-        const int l4 = lane * 4;
-        const int c = c_tile + (p.gated ? sub * CHUNK + (l4 & 63) : ((l4 / CHUNK) * 2 + sub) * CHUNK + l4 % CHUNK);
-        const int64_t at = w_row + c + (p.gated && l4 >= 64 ? p.cols : 0);
-        float4 b = make_float4(0.f, 0.f, 0.f, 0.f), s = make_float4(1.f, 1.f, 1.f, 1.f);
-        if (c < p.cols) {
-          if (p.bias) b = __ldg(reinterpret_cast<const float4 *>(p.bias + at));
-          if constexpr (EIGHT) s = __ldg(reinterpret_cast<const float4 *>(p.w_scale + at));
-        }
-        __syncwarp();   // the previous tile's have been read
-        *reinterpret_cast<float4 *>(bias_s + l4) = b;
-        if constexpr (EIGHT) *reinterpret_cast<float4 *>(scale_s + l4) = s;
+    int4 place_next = make_int4(-1, -1, -1, -1);
+    int e_next = 0;
+    auto look = [&](uint32_t tile) {
+      if (tile >= n_tiles) return;
+      const uint32_t m = tile / splits;
+      place_next = *reinterpret_cast<const int4 *>(p.order + (int64_t)m * TC_BM + lane * 4);
+      e_next = p.tile_expert[m];
+    };
+    look(blockIdx.x);
+    for (uint32_t tile = blockIdx.x; tile < n_tiles; tile += gridDim.x) {
+      const int4 place = place_next;
+      const int64_t w_row = (int64_t)e_next * p.w_cols;
+      const int c_tile = (int)(tile % splits) * p.cols_per_tile;
+      look(tile + gridDim.x);
+      float4 weight = make_float4(1.f, 1.f, 1.f, 1.f), xs = weight, bias[2], scale[2];
+      if (STORE == IT_EXPERT_OUT_BF16 || STORE == IT_EXPERT_OUT_F32) {
+        weight.x = place.x < 0 ? 0.f : p.weights[place.x]; weight.y = place.y < 0 ? 0.f : p.weights[place.y];
+        weight.z = place.z < 0 ? 0.f : p.weights[place.z]; weight.w = place.w < 0 ? 0.f : p.weights[place.w];
       }
-      const float xs = EIGHT && place >= 0 ? p.x_scale[place / p.x_div] : 1.f;
-      const float weight = (STORE == IT_EXPERT_OUT_BF16 || STORE == IT_EXPERT_OUT_F32) && place >= 0 ? p.weights[place] : 1.f;
-      const bool ok = mbar_wait(&acc_full[acc], acc_phase, abort_flag, p.spin_limit, EX_EPI_BACKOFF);
+      if constexpr (EIGHT) {
+        xs.x = place.x < 0 ? 0.f : p.x_scale[place.x / p.x_div]; xs.y = place.y < 0 ? 0.f : p.x_scale[place.y / p.x_div];
+        xs.z = place.z < 0 ? 0.f : p.x_scale[place.z / p.x_div]; xs.w = place.w < 0 ? 0.f : p.x_scale[place.w / p.x_div];
+      }
+#pragma unroll
+      for (int i = 0; i < 2; ++i) {   // columns of the accumulator, four a lane (gated: the second half of them belongs to columns p.cols and on)
+        bias[i] = make_float4(0.f, 0.f, 0.f, 0.f);
+        scale[i] = make_float4(1.f, 1.f, 1.f, 1.f);
+        const int ac = i * 128 + lane * 4, second = GATED && ac >= p.cols_per_tile, c = c_tile + ac - (second ? p.cols_per_tile : 0);
+        if (ac >= p.bn || c >= p.cols) continue;
+        const int64_t at = w_row + c + (second ? p.cols : 0);
+        if (p.bias) bias[i] = __ldg(reinterpret_cast<const float4 *>(p.bias + at));
+        if constexpr (EIGHT) scale[i] = __ldg(reinterpret_cast<const float4 *>(p.w_scale + at));
+      }
+      bool ok = lane == 0 ? mbar_wait(&acc_empty[acc], acc_phase ^ 1u, abort_flag, p.spin_limit, EX_EPI_BACKOFF) : true;
+      if (!__shfl_sync(0xffffffffu, (int)ok, 0)) break;
+      Meta &k = meta[acc];
+      *reinterpret_cast<int4 *>(k.place + lane * 4) = place;
+      *reinterpret_cast<float4 *>(k.weight + lane * 4) = weight;
+#pragma unroll
+      for (int i = 0; i < 2; ++i) *reinterpret_cast<float4 *>(k.bias + i * 128 + lane * 4) = bias[i];
+      if constexpr (EIGHT) {
+        *reinterpret_cast<float4 *>(k.xs + lane * 4) = xs;
+#pragma unroll
+        for (int i = 0; i < 2; ++i) *reinterpret_cast<float4 *>(k.scale + i * 128 + lane * 4) = scale[i];
+      }
+      __syncwarp();
+      if (lane == 0) mbar_arrive(&meta_full[acc]);
+      if (++acc == 2) { acc = 0; acc_phase ^= 1u; }
+    }
+  } else {
+    // ------------------------------------------------------------------ epilogue: a thread per row of the tile, a warp per 32 rows and step of columns
+    const int quarter = warp & 3, sub = (warp - EX_EPI_WARP0) >> 2;   // a warp may only touch TMEM lanes [32 * (warp % 4), +32)
+    constexpr bool F32_OUT = STORE == IT_EXPERT_SUMS || STORE == IT_EXPERT_OUT_F32, DIRECT = STORE == IT_EXPERT_OUT_BF16 || STORE == IT_EXPERT_OUT_F32;
+    constexpr int STEP = F32_OUT ? 16 : 32;   // columns that a warp takes at a time: 64 bytes of a row, written
+    constexpr int PLANES = STORE == IT_EXPERT_PARTS ? 3 : 1;
+    const uint32_t stage_s = smem_u32(staging) + (uint32_t)(warp - EX_EPI_WARP0) * EX_STAGING, swz = ((uint32_t)lane >> 1) & 3u;
+    uint32_t acc = 0, acc_phase = 0;
+    for (uint32_t tile = blockIdx.x; tile < n_tiles; tile += gridDim.x) {
+      const int m = (int)(tile / splits), c_tile = (int)(tile % splits) * p.cols_per_tile;
+      const int64_t pos0 = (int64_t)m * TC_BM + quarter * 32;
+      const bool ok = mbar_wait(&meta_full[acc], acc_phase, abort_flag, p.spin_limit, EX_EPI_BACKOFF) &&
+                      mbar_wait(&acc_full[acc], acc_phase, abort_flag, p.spin_limit, EX_EPI_BACKOFF);
       if (!__all_sync(0xffffffffu, ok)) break;
       tc_fence_after();
+      const Meta &k = meta[acc];
+      float xs = 1.f, weight = 1.f;
+      if constexpr (EIGHT) xs = k.xs[quarter * 32 + lane];
+      if constexpr (DIRECT) weight = k.weight[quarter * 32 + lane];
       const uint32_t taddr = tmem_base + ((uint32_t)(quarter * 32) << 16) + acc * (uint32_t)p.bn;
-      int lc = 0;   // column among this warp's
-      for (int ch = sub * CHUNK; ch < p.cols_per_tile && c_tile + ch < p.cols; ch += 2 * CHUNK, lc += CHUNK) {
+      const int width = p.cols - c_tile < p.cols_per_tile ? p.cols - c_tile : p.cols_per_tile;
+      const int steps = width > sub * STEP ? (width - sub * STEP + EX_EPI_SUBS * STEP - 1) / (EX_EPI_SUBS * STEP) : 0;   // of this warp
+      uint32_t r[16], r2[16];   // 16 columns of the accumulator; gated: and of what they gate
+      auto fetch = [&](int col) {
+        tmem_ld16(taddr + (uint32_t)col, r);
+        if constexpr (GATED) tmem_ld16(taddr + (uint32_t)(p.cols_per_tile + col), r2);
+      };
+      if (steps > 0) fetch(sub * STEP);
+      for (int s = 0; s < steps; ++s) {
+        const int ch = (s * EX_EPI_SUBS + sub) * STEP;   // first column of the step in the tile
+        uint32_t w[PLANES][16];
 #pragma unroll
-        for (int q = 0; q < CHUNK; q += 16) {
-          const int c = c_tile + ch + q;   // first column of 16 (columns past the last are computed and not stored)
+        for (int q = 0; q < STEP; q += 16) {
           float v[16];
-          auto finish = [&](int tmem_col, int at) {   // accumulator -> scaled, with the bias
-            uint32_t r[16];
-            tmem_ld16(taddr + (uint32_t)tmem_col, r);
-            float4 b[4], s[4];
+          tmem_ld_wait();
+          auto finish = [&](const uint32_t (&acc_r)[16], int at_c) {   // accumulator -> scaled, with the bias
 #pragma unroll
             for (int i = 0; i < 4; ++i) {
-              b[i] = *reinterpret_cast<const float4 *>(bias_s + at + 4 * i);
-              if constexpr (EIGHT) s[i] = *reinterpret_cast<const float4 *>(scale_s + at + 4 * i);
-            }
-            tmem_ld_wait();
-#pragma unroll
-            for (int i = 0; i < 4; ++i) {
+              const float4 b = *reinterpret_cast<const float4 *>(k.bias + at_c + 4 * i);
               if constexpr (EIGHT) {
-                v[4 * i] = fmaf(__uint_as_float(r[4 * i]) * xs, s[i].x, b[i].x); v[4 * i + 1] = fmaf(__uint_as_float(r[4 * i + 1]) * xs, s[i].y, b[i].y);
-                v[4 * i + 2] = fmaf(__uint_as_float(r[4 * i + 2]) * xs, s[i].z, b[i].z); v[4 * i + 3] = fmaf(__uint_as_float(r[4 * i + 3]) * xs, s[i].w, b[i].w);
+                const float4 f = *reinterpret_cast<const float4 *>(k.scale + at_c + 4 * i);
+                v[4 * i] = fmaf(__uint_as_float(acc_r[4 * i]) * xs, f.x, b.x); v[4 * i + 1] = fmaf(__uint_as_float(acc_r[4 * i + 1]) * xs, f.y, b.y);
+                v[4 * i + 2] = fmaf(__uint_as_float(acc_r[4 * i + 2]) * xs, f.z, b.z); v[4 * i + 3] = fmaf(__uint_as_float(acc_r[4 * i + 3]) * xs, f.w, b.w);
               } else {
-                v[4 * i] = __uint_as_float(r[4 * i]) + b[i].x; v[4 * i + 1] = __uint_as_float(r[4 * i + 1]) + b[i].y;
-                v[4 * i + 2] = __uint_as_float(r[4 * i + 2]) + b[i].z; v[4 * i + 3] = __uint_as_float(r[4 * i + 3]) + b[i].w;
+                v[4 * i] = __uint_as_float(acc_r[4 * i]) + b.x; v[4 * i + 1] = __uint_as_float(acc_r[4 * i + 1]) + b.y;
+                v[4 * i + 2] = __uint_as_float(acc_r[4 * i + 2]) + b.z; v[4 * i + 3] = __uint_as_float(acc_r[4 * i + 3]) + b.w;
               }
             }
           };
-          if (p.gated) {
-            float gate[16];
-            finish(ch + q, q);
-            expert_act(v, p.act);
+          float gate[GATED ? 16 : 1];
+          finish(r, ch + q);
+          if constexpr (GATED) {
 #pragma unroll
             for (int i = 0; i < 16; ++i) gate[i] = v[i];
-            finish(p.cols_per_tile + ch + q, 64 + q);
+            finish(r2, p.cols_per_tile + ch + q);
+          }
+          // the next 16 columns are fetched while these are finished
+          if (q + 16 < STEP) fetch(ch + q + 16);
+          else if (s + 1 < steps) fetch(ch + EX_EPI_SUBS * STEP);
+          if constexpr (GATED) {
+            expert_act(gate, p.act);
 #pragma unroll
             for (int i = 0; i < 16; ++i) v[i] *= gate[i];
           } else {
-            finish(ch + q, lc + q);
             expert_act(v, p.act);
           }
-          if constexpr (STORE == IT_EXPERT_PARTS) {
-            uint32_t w[3][8];
+          if constexpr (DIRECT) {
 #pragma unroll
-            for (int i = 0; i < 16; ++i) {
-              const uint32_t u = __float_as_uint(v[i]);
-              const float r1 = v[i] - __uint_as_float(u & 0xffff0000u);
-              const uint32_t u1 = __float_as_uint(r1), u2 = __float_as_uint(r1 - __uint_as_float(u1 & 0xffff0000u));
-              if (i & 1) { w[0][i >> 1] |= u & 0xffff0000u; w[1][i >> 1] |= u1 & 0xffff0000u; w[2][i >> 1] |= u2 & 0xffff0000u; }
-              else { w[0][i >> 1] = u >> 16; w[1][i >> 1] = u1 >> 16; w[2][i >> 1] = u2 >> 16; }
+            for (int i = 0; i < 16; ++i) v[i] *= weight;
+          }
+          if constexpr (F32_OUT) {
+#pragma unroll
+            for (int i = 0; i < 16; ++i) w[0][i] = __float_as_uint(v[i]);
+          } else if constexpr (STORE == IT_EXPERT_PARTS) {
+#pragma unroll
+            for (int i = 0; i < 16; i += 2) {
+              const float2 x1 = make_float2(v[i] - __uint_as_float(__float_as_uint(v[i]) & 0xffff0000u), v[i + 1] - __uint_as_float(__float_as_uint(v[i + 1]) & 0xffff0000u));
+              const float2 x2 = make_float2(x1.x - __uint_as_float(__float_as_uint(x1.x) & 0xffff0000u), x1.y - __uint_as_float(__float_as_uint(x1.y) & 0xffff0000u));
+              w[0][(q + i) / 2] = __byte_perm(__float_as_uint(v[i]), __float_as_uint(v[i + 1]), 0x7632);
+              w[1][(q + i) / 2] = __byte_perm(__float_as_uint(x1.x), __float_as_uint(x1.y), 0x7632);
+              w[2][(q + i) / 2] = __byte_perm(__float_as_uint(x2.x), __float_as_uint(x2.y), 0x7632);
             }
-#pragma unroll
-            for (int k = 0; k < 3; ++k) {
-              uint2 *to = reinterpret_cast<uint2 *>(reinterpret_cast<__nv_bfloat16 *>(p.dst) + k * p.part_stride + (pos0 + lane) * p.cols + c);
-#pragma unroll
-              for (int i = 0; i < 4; ++i)
-                if (place >= 0 && c + 4 * i < p.cols) to[i] = make_uint2(w[k][2 * i], w[k][2 * i + 1]);
-            }
-            __syncwarp();   // (the loads from TMEM are taken by whole warps)
-          } else if constexpr (F32_OUT) {
-            if constexpr (STORE == IT_EXPERT_OUT_F32) {
-#pragma unroll
-              for (int i = 0; i < 16; ++i) v[i] *= weight;
-            }
-#pragma unroll
-            for (int i = 0; i < 4; ++i)
-              st_shared_v4(stage_s + (uint32_t)lane * 64u + (((uint32_t)i ^ swz) << 4), __float_as_uint(v[4 * i]), __float_as_uint(v[4 * i + 1]),
-                           __float_as_uint(v[4 * i + 2]), __float_as_uint(v[4 * i + 3]));
           } else {
-            uint32_t w[8];
 #pragma unroll
-            for (int i = 0; i < 8; ++i) {
-              if (STORE == IT_EXPERT_OUT_BF16) { v[2 * i] *= weight; v[2 * i + 1] *= weight; }
-              const __nv_bfloat162 h = __floats2bfloat162_rn(v[2 * i], v[2 * i + 1]);
-              w[i] = *reinterpret_cast<const uint32_t *>(&h);
+            for (int i = 0; i < 16; i += 2) {
+              const __nv_bfloat162 h = __floats2bfloat162_rn(v[i], v[i + 1]);
+              w[0][(q + i) / 2] = *reinterpret_cast<const uint32_t *>(&h);
             }
-            st_shared_v4(stage_s + (uint32_t)lane * 64u + ((((uint32_t)(q & 31) / 8) ^ swz) << 4), w[0], w[1], w[2], w[3]);
-            st_shared_v4(stage_s + (uint32_t)lane * 64u + ((((uint32_t)(q & 31) / 8 + 1) ^ swz) << 4), w[4], w[5], w[6], w[7]);
           }
-          if (STORE != IT_EXPERT_PARTS && (F32_OUT || (q & 16))) {
-            // rows of 64 bytes out of the staging tile, four lanes a row
-            __syncwarp();
-            constexpr int ESIZE = F32_OUT ? 4 : 2;
-            const int piece = lane & 3, c64 = c_tile + ch + (F32_OUT ? q : q - 16) + piece * (16 / ESIZE);
+        }
+        // rows of 64 bytes through the staging tile, four lanes a row
+        constexpr int ESIZE = F32_OUT ? 4 : 2;
+        const int piece = lane & 3, c64 = c_tile + ch + piece * (16 / ESIZE);
 #pragma unroll
-            for (int r0 = 0; r0 < 32; r0 += 8) {
-              const int r = r0 + (lane >> 2);
-              const int at = __shfl_sync(0xffffffffu, place, r);
-              uint4 d;
-              asm volatile("ld.shared.v4.b32 {%0, %1, %2, %3}, [%4];" : "=r"(d.x), "=r"(d.y), "=r"(d.z), "=r"(d.w)
-                           : "r"(stage_s + (uint32_t)r * 64u + ((uint32_t)(piece ^ ((r >> 1) & 3)) << 4)) : "memory");
-              if (at >= 0 && c64 < p.cols) {
-                const int64_t row = STORE == IT_EXPERT_OUT_BF16 || STORE == IT_EXPERT_OUT_F32 ? (int64_t)at : pos0 + r;
-                *reinterpret_cast<uint4 *>(reinterpret_cast<unsigned char *>(p.dst) + (row * p.cols + c64) * ESIZE) = d;
-              }
-            }
-            __syncwarp();
+        for (int pl = 0; pl < PLANES; ++pl) {
+#pragma unroll
+          for (int i = 0; i < 4; ++i)
+            st_shared_v4(stage_s + (uint32_t)lane * 64u + (((uint32_t)i ^ swz) << 4), w[pl][4 * i], w[pl][4 * i + 1], w[pl][4 * i + 2], w[pl][4 * i + 3]);
+          __syncwarp();
+#pragma unroll
+          for (int r0 = 0; r0 < 32; r0 += 8) {
+            const int row = r0 + (lane >> 2), at = k.place[quarter * 32 + row];
+            uint4 d;
+            asm volatile("ld.shared.v4.b32 {%0, %1, %2, %3}, [%4];" : "=r"(d.x), "=r"(d.y), "=r"(d.z), "=r"(d.w)
+                         : "r"(stage_s + (uint32_t)row * 64u + ((uint32_t)(piece ^ ((row >> 1) & 3)) << 4)) : "memory");
+            if (at >= 0 && c64 < p.cols)
+              *reinterpret_cast<uint4 *>(reinterpret_cast<unsigned char *>(p.dst) + (pl * p.part_stride + (DIRECT ? (int64_t)at : pos0 + row) * p.cols + c64) * ESIZE) = d;
           }
+          __syncwarp();
         }
       }
       tc_fence_before();
@@ -357,7 +432,7 @@ expert_gemm_kernel(const __grid_constant__ CUtensorMap map_a, const __grid_const
   tc_fence_before();
   __syncthreads();
   if (threadIdx.x == 0 && *abort_flag) atomicExch(p.status, 1);
-  if (warp == EX_TMA_WARPS) {
+  if (warp == EX_MMA_WARP) {
     tc_fence_after();
     tmem_dealloc(tmem_base, tmem_cols);
   }
@@ -374,10 +449,10 @@ it_status encode(CUtensorMap *map, bool eight, const void *ptr, int rank, const 
   return IT_OK;
 }
 
-template <bool EIGHT, it_expert_store STORE>
+template <bool EIGHT, it_expert_store STORE, bool GATED>
 it_status launch(const CUtensorMap &ma, const CUtensorMap &mw, const ExParams &p, int grid, int smem, double bytes, double flops, cudaStream_t st) {
-  IT_CUDA_TRY(cudaFuncSetAttribute(expert_gemm_kernel<EIGHT, STORE>, cudaFuncAttributeMaxDynamicSharedMemorySize, smem));
-  IT_LAUNCH(IT_K_EXPERT_GEMM, bytes, flops, st, IT_CUDA_TRY(it_launch_pdl(expert_gemm_kernel<EIGHT, STORE>, dim3((unsigned)grid), dim3(EX_THREADS), smem, st, ma, mw, p)));
+  IT_CUDA_TRY(cudaFuncSetAttribute(expert_gemm_kernel<EIGHT, STORE, GATED>, cudaFuncAttributeMaxDynamicSharedMemorySize, smem));
+  IT_LAUNCH(IT_K_EXPERT_GEMM, bytes, flops, st, IT_CUDA_TRY(it_launch_pdl(expert_gemm_kernel<EIGHT, STORE, GATED>, dim3((unsigned)grid), dim3(EX_THREADS), smem, st, ma, mw, p)));
   return IT_OK;
 }
 
@@ -388,7 +463,7 @@ it_status it_launch_expert_gemm(const it_experts_args &a, const it_experts_plan 
   ExParams p{};
   p.order = q.order; p.tile_expert = q.tile_expert; p.n_tiles = q.n_tiles; p.tiles_max = (int)q.tiles_max;
   p.K = g.K; p.kb = (g.K + BK - 1) / BK; p.passes = g.parts == 3 ? 6 : 1;
-  p.gather_div = g.gather ? a.d.top_k : 0; p.a_rows = (int)g.a_rows;
+  p.A = g.A; p.gather_div = g.gather ? a.d.top_k : 0; p.a_rows = (int)g.a_rows;
   p.n_experts = a.d.n_experts; p.w_cols = g.w_cols; p.cols = g.cols; p.act = g.act; p.gated = g.gated;
   p.bias = g.bias; p.w_scale = g.w_scale; p.x_scale = g.x_scale; p.weights = a.weights; p.x_div = a.d.top_k;
   p.dst = g.dst; p.part_stride = q.tiles_max * TC_BM * (int64_t)g.cols; p.status = a.status;
@@ -401,7 +476,7 @@ it_status it_launch_expert_gemm(const it_experts_args &a, const it_experts_plan 
   p.bn = g.gated ? 2 * p.cols_per_tile : p.cols_per_tile;
 
   const cuuint64_t da[2] = {(cuuint64_t)g.K, (cuuint64_t)(g.a_rows * g.parts)}, sa[1] = {(cuuint64_t)g.K * elem};
-  const cuuint32_t ba[2] = {(cuuint32_t)BK, (cuuint32_t)(g.gather ? 1 : TC_BM)};
+  const cuuint32_t ba[2] = {(cuuint32_t)BK, (cuuint32_t)TC_BM};
   const cuuint64_t dw[3] = {(cuuint64_t)g.w_cols, (cuuint64_t)g.K, (cuuint64_t)a.d.n_experts * g.parts};
   const cuuint64_t sw[2] = {(cuuint64_t)g.w_cols * elem, (cuuint64_t)g.w_cols * elem * (cuuint64_t)g.K};
   const cuuint32_t bw[3] = {(cuuint32_t)BK, (cuuint32_t)BK, 1};
@@ -409,19 +484,31 @@ it_status it_launch_expert_gemm(const it_experts_args &a, const it_experts_plan 
   IT_TRY(encode(&ma, g.eight, g.A, 2, da, sa, ba));
   IT_TRY(encode(&mw, g.eight, g.W, 3, dw, sw, bw));
 
-  const int stage = EX_STAGE_A + p.bn * TC_KBLOCK_BYTES, fixed = 1024 + (g.store == IT_EXPERT_PARTS ? 0 : EX_EPI_WARPS * EX_STAGING) + EX_EPI_WARPS * EX_CONSTS + (2 * EX_MAX_STAGES + 8) * 8;
+  const int stage = EX_STAGE_A + p.bn * TC_KBLOCK_BYTES, fixed = EX_EPI_WARPS * EX_STAGING + 2 * (int)(g.eight ? sizeof(ExMetaEight) : sizeof(ExMeta)) + (2 * EX_MAX_STAGES + 9) * 8;
   p.stages = (227 * 1024 - fixed) / stage;
   if (p.stages > EX_MAX_STAGES) p.stages = EX_MAX_STAGES;
   const int smem = fixed + p.stages * stage;
   const int64_t tiles = q.tiles_max * p.n_splits;
+  IT_REQUIRE(tiles + 3 * (int64_t)a.sms <= INT32_MAX, IT_ERR_UNSUPPORTED, "too many places and columns for one launch");
   const int grid = (int)(tiles < a.sms ? tiles : a.sms);
   const int64_t places = a.n * a.d.top_k;
   const double flops = 2.0 * places * g.K * (double)g.w_cols, bytes = (double)places * (g.K * elem * g.parts + g.cols * 4.0);
+#define IT_EX_LAUNCH(EIGHT, STORE, GATED) return launch<EIGHT, STORE, GATED>(ma, mw, p, grid, smem, bytes, flops, st)
   switch (g.store) {
-    case IT_EXPERT_HIDDEN: return g.eight ? launch<true, IT_EXPERT_HIDDEN>(ma, mw, p, grid, smem, bytes, flops, st) : launch<false, IT_EXPERT_HIDDEN>(ma, mw, p, grid, smem, bytes, flops, st);
-    case IT_EXPERT_PARTS: return launch<false, IT_EXPERT_PARTS>(ma, mw, p, grid, smem, bytes, flops, st);
-    case IT_EXPERT_SUMS: return g.eight ? launch<true, IT_EXPERT_SUMS>(ma, mw, p, grid, smem, bytes, flops, st) : launch<false, IT_EXPERT_SUMS>(ma, mw, p, grid, smem, bytes, flops, st);
-    case IT_EXPERT_OUT_BF16: return g.eight ? launch<true, IT_EXPERT_OUT_BF16>(ma, mw, p, grid, smem, bytes, flops, st) : launch<false, IT_EXPERT_OUT_BF16>(ma, mw, p, grid, smem, bytes, flops, st);
-    default: return launch<false, IT_EXPERT_OUT_F32>(ma, mw, p, grid, smem, bytes, flops, st);
+    case IT_EXPERT_HIDDEN:
+      if (g.eight) { if (g.gated) IT_EX_LAUNCH(true, IT_EXPERT_HIDDEN, true); else IT_EX_LAUNCH(true, IT_EXPERT_HIDDEN, false); }
+      if (g.gated) IT_EX_LAUNCH(false, IT_EXPERT_HIDDEN, true);
+      IT_EX_LAUNCH(false, IT_EXPERT_HIDDEN, false);
+    case IT_EXPERT_PARTS:
+      if (g.gated) IT_EX_LAUNCH(false, IT_EXPERT_PARTS, true);
+      IT_EX_LAUNCH(false, IT_EXPERT_PARTS, false);
+    case IT_EXPERT_SUMS:
+      if (g.eight) IT_EX_LAUNCH(true, IT_EXPERT_SUMS, false);
+      IT_EX_LAUNCH(false, IT_EXPERT_SUMS, false);
+    case IT_EXPERT_OUT_BF16:
+      if (g.eight) IT_EX_LAUNCH(true, IT_EXPERT_OUT_BF16, false);
+      IT_EX_LAUNCH(false, IT_EXPERT_OUT_BF16, false);
+    default: IT_EX_LAUNCH(false, IT_EXPERT_OUT_F32, false);
   }
+#undef IT_EX_LAUNCH
 }

@@ -5,8 +5,8 @@
 // looks at the gap between every two neighbours of the choice: where it is within the rounding of the two (route_near), the whole warp
 // takes the row again in 64 bits.
 //
-// A row lies in the registers of 1 to 32 lanes (8 experts a lane, 16 and 32 beyond 256 experts); a choice is a maximum over a lane's
-// keys and a few shuffles.  Bound by issue slots: the row's bytes are few.
+// A row lies in the registers of 1 to 32 lanes (8 experts a lane, 16 and 32 beyond 256 experts), or of one thread where experts and
+// places are few.  Bound by issue slots: the row's bytes are few.
 #include <float.h>
 #include <math.h>
 #include <type_traits>
@@ -132,7 +132,15 @@ __device__ __forceinline__ bool route_near(float a, float b, float pa, float pb)
 }
 __device__ __forceinline__ float route_slack(float score, float below_top) { return score * fmaf(fabsf(below_top), 0.125f, 1.f); }
 
-// L lanes per row, C experts per lane.
+// A float as an unsigned number of the same order (neither operand is NaN; -0 counts as 0).
+__device__ __forceinline__ unsigned route_order(float k) {
+  const unsigned u = __float_as_uint(k + 0.f);
+  return u ^ ((unsigned)((int)u >> 31) | 0x80000000u);
+}
+__device__ __forceinline__ float route_unorder(unsigned o) { return __uint_as_float(o ^ ((o >> 31) ? 0x80000000u : 0xffffffffu)); }
+
+// L lanes per row, C experts per lane; a round of the choice is a maximum over a lane's keys and over the lanes.  The scores of the chosen
+// are taken afterwards, a lane each.
 template <typename T, int L, int C>
 __global__ void __launch_bounds__(ROUTE_THREADS) route_kernel(const RouteParams p) {
   it_allow_next();
@@ -142,75 +150,69 @@ __global__ void __launch_bounds__(ROUTE_THREADS) route_kernel(const RouteParams 
   constexpr unsigned full = 0xffffffffu;
   extern __shared__ double route_smem[];
   const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31, gl = lane % L, r = lane / L;
-  // per warp: ids and weights of its rows [R][k] each, the fp32 keys and worths of its rows (groups), or the 64-bit ones of one row
-  const int E = p.experts, per_warp = E + p.n_groups;
+  // per warp: expert, key and score of its rows' choices [R][rounds] each, the fp32 keys and worths of its rows (groups); the 64-bit ones of one row
+  const int E = p.experts, per_warp = E + p.n_groups, rounds = p.k + (p.bias && p.k < E ? 1 : 0);
   double *mine64 = route_smem + (size_t)warp * per_warp;
   const int row_words = E + E / 32 + 1 + p.n_groups;   // a pad word after every 32 keys
   float *after = reinterpret_cast<float *>(route_smem + (size_t)ROUTE_WARPS * per_warp);
-  const int warp_words = R * 2 * p.k + (p.n_groups > 1 ? R * row_words : 0);
-  int32_t *out_ids = reinterpret_cast<int32_t *>(after + (size_t)warp * warp_words);
-  float *out_w = reinterpret_cast<float *>(out_ids + R * p.k);
-  float *keys = out_w + R * p.k + (size_t)r * row_words, *worth = keys + E + E / 32 + 1;
+  const int warp_words = R * 3 * rounds + (p.n_groups > 1 ? R * row_words : 0);
+  int32_t *at_s = reinterpret_cast<int32_t *>(after + (size_t)warp * warp_words);
+  float *key_s = reinterpret_cast<float *>(at_s + R * rounds), *score_s = key_s + R * rounds;
+  float *keys = score_s + R * rounds + (size_t)r * row_words, *worth = keys + E + E / 32 + 1;
   auto expert = [&](int c) { return ((c / N) * L + gl) * N + c % N; };
   const bool vec = (E * (int)sizeof(T)) % 16 == 0 && N == kVec<T> && ((uintptr_t)p.logits & 15) == 0;
+  float bias[C];
+#pragma unroll
+  for (int c = 0; c < C; ++c) bias[c] = p.bias && expert(c) < E ? p.bias[expert(c)] : 0.f;
+  // groups: lanes that scan one group together
+  int per_group = 1;
+  while (per_group * 2 * p.n_groups <= L && p.group_size % (per_group * 2) == 0) per_group *= 2;
 
   for (int64_t row0 = ((int64_t)blockIdx.x * ROUTE_WARPS + warp) * R; row0 < p.n; row0 += (int64_t)gridDim.x * ROUTE_WARPS * R) {
     const int64_t row = row0 + r < p.n ? row0 + r : p.n - 1;   // lanes past the last row repeat it, and store nothing
     const T *from = reinterpret_cast<const T *>(p.logits) + row * E;
-    float logit[C], key[C];
+    float key[C];   // logits first
 #pragma unroll
     for (int c0 = 0; c0 < C; c0 += N) {
       const int e0 = expert(c0);
       if constexpr (N == kVec<T>) {
         if (vec) {
           float v[N];
-          if (e0 < E) vec_to_f32(*reinterpret_cast<const uint4 *>(from + e0), v);
+          if (e0 < E) vec_to_f32(__ldg(reinterpret_cast<const uint4 *>(from + e0)), v);
 #pragma unroll
-          for (int i = 0; i < N; ++i) logit[c0 + i] = e0 < E ? open_logit(v[i]) : kClosed;
+          for (int i = 0; i < N; ++i) key[c0 + i] = e0 < E ? open_logit(v[i]) : kClosed;
           continue;
         }
       }
 #pragma unroll
-      for (int i = 0; i < N; ++i) logit[c0 + i] = e0 + i < E ? open_logit(to_f32(from[e0 + i])) : kClosed;
+      for (int i = 0; i < N; ++i) key[c0 + i] = e0 + i < E ? open_logit(to_f32(from[e0 + i])) : kClosed;
     }
     float top = 0.f, inv = 1.f;
     if (!p.sigmoid) {
-      top = logit[0];
+      top = key[0];
 #pragma unroll
-      for (int c = 1; c < C; ++c) top = fmaxf(top, logit[c]);
+      for (int c = 1; c < C; ++c) top = fmaxf(top, key[c]);
 #pragma unroll
       for (int o = L / 2; o > 0; o >>= 1) top = fmaxf(top, __shfl_xor_sync(full, top, o));
       if (!(top > kClosed)) top = 0.f;   // nothing is open
     }
-    auto raw = [&](float l) { return p.sigmoid ? 1.f / (1.f + expf(-l)) : expf(l - top); };   // (a closed logit: 0)
+    auto raw = [&](float l, float top_of) { return p.sigmoid ? 1.f / (1.f + expf(-l)) : expf(l - top_of); };   // (a closed logit: 0)
     bool near = false;
-    if (p.bias) {
-      float sum = 0.f;
+    if (p.bias || p.need_sum) {
+      float sum = 0.f, s[C];
 #pragma unroll
       for (int c = 0; c < C; ++c) {
-        key[c] = raw(logit[c]);
-        sum += key[c];
+        s[c] = raw(key[c], top);
+        sum += s[c];
       }
       if (!p.sigmoid) {
 #pragma unroll
         for (int o = L / 2; o > 0; o >>= 1) sum += __shfl_xor_sync(full, sum, o);
         inv = sum > 0.f ? 1.f / sum : 0.f;
       }
+      if (p.bias) {
 #pragma unroll
-      for (int c = 0; c < C; ++c) {
-        const int e = expert(c);
-        key[c] = logit[c] > kClosed ? open_key(fmaf(key[c], inv, __ldg(p.bias + e))) : kClosed;
-      }
-    } else {
-#pragma unroll
-      for (int c = 0; c < C; ++c) key[c] = logit[c];
-      if (p.need_sum) {
-        float sum = 0.f;
-#pragma unroll
-        for (int c = 0; c < C; ++c) sum += raw(logit[c]);
-#pragma unroll
-        for (int o = L / 2; o > 0; o >>= 1) sum += __shfl_xor_sync(full, sum, o);
-        inv = sum > 0.f ? 1.f / sum : 0.f;
+        for (int c = 0; c < C; ++c) key[c] = key[c] > kClosed ? open_key(fmaf(s[c], inv, bias[c])) : kClosed;
       }
     }
     if (p.n_groups > 1) {
@@ -221,21 +223,33 @@ __global__ void __launch_bounds__(ROUTE_THREADS) route_kernel(const RouteParams 
         if (e < E) keys[e + (e >> 5)] = key[c];
       }
       __syncwarp();
-      for (int g = gl; g < p.n_groups; g += L) {
+      const int share = p.group_size / per_group, at_once = L / per_group;
+      for (int g0 = 0; g0 < p.n_groups; g0 += at_once) {   // (whole warps: the lanes of a group compare notes)
+        const int g = g0 + gl / per_group;
         float a = kClosed, b = kClosed;
-        for (int i = 0, e = g * p.group_size; i < p.group_size; ++i, ++e) {
-          const float k = keys[e + (e >> 5)];
-          b = fmaxf(b, fminf(a, k));
-          a = fmaxf(a, k);
+        if (g < p.n_groups) {
+          int e = g * p.group_size + (gl % per_group) * share;
+          for (int i = 0; i < share; ++i, ++e) {
+            const float k = keys[e + (e >> 5)];
+            b = fmaxf(b, fminf(a, k));
+            a = fmaxf(a, k);
+          }
         }
-        if (p.group_best == 2 && a > kClosed) {
-          const float second = b > kClosed ? (p.bias ? b : raw(b)) : 0.f;
-          a = (p.bias ? a : raw(a)) + second;
+        for (int o = 1; o < per_group; o <<= 1) {
+          const float a2 = __shfl_xor_sync(full, a, o), b2 = __shfl_xor_sync(full, b, o);
+          b = fmaxf(fmaxf(b, b2), fminf(a, a2));
+          a = fmaxf(a, a2);
         }
-        worth[g] = a;
+        if (g < p.n_groups && gl % per_group == 0) {
+          if (p.group_best == 2 && a > kClosed) {
+            const float second = b > kClosed ? (p.bias ? b : raw(b, top)) : 0.f;
+            a = (p.bias ? a : raw(a, top)) + second;
+          }
+          worth[g] = a;
+        }
       }
       __syncwarp();
-      // every lane ranks all groups whose experts it holds by way of one flag per group, kept in place of the keys
+      // one flag per group, in place of the keys
       const bool exact = !p.bias && p.group_best == 1;
       for (int g = gl; g < p.n_groups; g += L) {
         const float w = worth[g];
@@ -255,72 +269,235 @@ __global__ void __launch_bounds__(ROUTE_THREADS) route_kernel(const RouteParams 
         if (e < E && keys[(e * p.group_magic) >> 22] == 0.f) key[c] = kClosed;
       }
     }
+    __syncwarp();   // the last row's choices have been read
     // the choice, one more than asked for where its border has to be looked at
-    float before = INFINITY, p_before = 0.f, sum = 0.f;
-    const int rounds = p.k + (p.bias && p.k < E ? 1 : 0);
-    for (int j = 0; j < rounds; ++j) {
-      float best = kClosed, l = kClosed;
-      int at = ROUTE_MAX_EXPERTS;
+    if constexpr (L == 32) {
+      // keys as numbers, so that a warp's maximum is one instruction; a lane looks again at its keys only when one of them went
+      unsigned k[C], best = 0;
+      int at = 0;
 #pragma unroll
-      for (int c = 0; c < C; ++c)
-        if (key[c] > best) { best = key[c]; at = expert(c); l = logit[c]; }
-#pragma unroll
-      for (int o = L / 2; o > 0; o >>= 1) {
-        const float b = __shfl_xor_sync(full, best, o), bl = __shfl_xor_sync(full, l, o);
-        const int a = __shfl_xor_sync(full, at, o);
-        if (b > best || (b == best && a < at)) { best = b; at = a; l = bl; }
+      for (int c = 0; c < C; ++c) {
+        k[c] = key[c] > kClosed ? route_order(key[c]) : 0u;
+        if (k[c] > best) { best = k[c]; at = expert(c); }
       }
+      for (int j = 0; j < rounds; ++j) {
+        const unsigned m = __reduce_max_sync(full, best);
+        const int e = (int)__reduce_min_sync(full, best == m ? (unsigned)at : (unsigned)ROUTE_MAX_EXPERTS);
+        if (lane == 0) { at_s[j] = m ? e : -1; key_s[j] = m ? route_unorder(m) : kClosed; }
+        if (best == m && at == e) {
+          best = 0;
 #pragma unroll
-      for (int c = 0; c < C; ++c)
-        if (expert(c) == at) key[c] = kClosed;
-      const bool some = best > kClosed;
-      const float w = some ? raw(l) * (p.bias || p.need_sum ? inv : 1.f) : 0.f;
-      const float slack = p.sigmoid ? w : route_slack(w, some ? l - top : 0.f);
-      if (p.bias && some && j > 0) near |= route_near(before, best, p_before, slack);
-      before = best;
-      p_before = slack;
-      if (j < p.k) {
-        sum += w;
-        if (gl == 0) { out_ids[r * p.k + j] = some ? at : -1; out_w[r * p.k + j] = w; }
+          for (int c = 0; c < C; ++c) {
+            if (expert(c) == e) k[c] = 0u;
+          }
+#pragma unroll
+          for (int c = 0; c < C; ++c)
+            if (k[c] > best) { best = k[c]; at = expert(c); }
+        }
+        __syncwarp();
+      }
+    } else {
+      for (int j = 0; j < rounds; ++j) {
+        float best = kClosed;
+        int at = ROUTE_MAX_EXPERTS;
+#pragma unroll
+        for (int c = 0; c < C; ++c)
+          if (key[c] > best) { best = key[c]; at = expert(c); }
+#pragma unroll
+        for (int o = L / 2; o > 0; o >>= 1) {
+          const float b = __shfl_xor_sync(full, best, o);
+          const int a = __shfl_xor_sync(full, at, o);
+          if (b > best || (b == best && a < at)) { best = b; at = a; }
+        }
+#pragma unroll
+        for (int c = 0; c < C; ++c)
+          if (expert(c) == at) key[c] = kClosed;
+        if (gl == 0) { at_s[r * rounds + j] = best > kClosed ? at : -1; key_s[r * rounds + j] = best; }
+      }
+      __syncwarp();
+    }
+    // scores of the chosen, a lane each: unbiased, and divided by the row's sum where the keys are
+    for (int i0 = 0; i0 < R * rounds; i0 += 32) {
+      const int i = i0 + lane, rr = R == 1 ? 0 : (i < R * rounds ? i / rounds : 0);
+      const float t = __shfl_sync(full, top, rr * L), f = __shfl_sync(full, inv, rr * L);
+      if (i < R * rounds) {
+        const int e = at_s[i];
+        float w = 0.f;
+        if (e >= 0) {
+          const int64_t row_i = row0 + rr < p.n ? row0 + rr : p.n - 1;
+          w = raw(p.bias ? open_logit(to_f32(reinterpret_cast<const T *>(p.logits)[row_i * E + e])) : key_s[i], t) * f;
+        }
+        score_s[i] = w;
       }
     }
-    const float f = p.renorm ? (sum > 0.f ? p.scale / sum : 0.f) : p.scale;
     __syncwarp();
-    if (gl == 0)
-      for (int j = 0; j < p.k; ++j) out_w[r * p.k + j] *= f;
-    __syncwarp();
-    const int real = p.n - row0 < R ? (int)(p.n - row0) : R;
-    for (int i = lane; i < real * p.k; i += 32) {
-      p.ids[row0 * p.k + i] = out_ids[i];
-      p.weights[row0 * p.k + i] = out_w[i];
+    unsigned again = 0;   // rows that are taken again, a bit each
+    for (int i0 = 0; i0 < R * rounds; i0 += 32) {
+      const int i = i0 + lane, rr = R == 1 ? 0 : (i < R * rounds ? i / rounds : 0), j = i - rr * rounds;
+      bool close = false;
+      if (i < R * rounds) {
+        float sum = 0.f;
+        for (int q = 0; q < p.k; ++q) sum += score_s[rr * rounds + q];
+        const float w = score_s[i], key_i = key_s[i];
+        if (p.bias && j > 0 && at_s[i] >= 0) {
+          // (-ln of a score is at least the distance of its logit from the top: the sum is 1 or more)
+          const float before = score_s[i - 1];
+          close = route_near(key_s[i - 1], key_i, p.sigmoid ? before : route_slack(before, __logf(fmaxf(before, 1e-38f))),
+                             p.sigmoid ? w : route_slack(w, __logf(fmaxf(w, 1e-38f))));
+        }
+        if (j < p.k && row0 + rr < p.n) {
+          const int64_t to = (row0 + rr) * p.k + j;
+          p.ids[to] = at_s[i];
+          p.weights[to] = w * (p.renorm ? (sum > 0.f ? p.scale / sum : 0.f) : p.scale);
+        }
+      }
+      if (p.bias) again |= __reduce_or_sync(full, close ? 1u << rr : 0u);
     }
-    __syncwarp();
-    unsigned again = __ballot_sync(full, near);
+    if (p.n_groups > 1) again |= __reduce_or_sync(full, near ? 1u << r : 0u);
     while (again) {
-      const int which = (__ffs(again) - 1) / L;
-      route_row_exact(p, p.logits, sizeof(T) == 2, row0 + which < p.n ? row0 + which : p.n - 1, mine64, lane);
-      again &= ~((full >> (32 - L)) << (which * L));
+      const int which = __ffs(again) - 1;
+      again &= again - 1;
+      if (row0 + which < p.n) route_row_exact(p, p.logits, sizeof(T) == 2, row0 + which, mine64, lane);
       __syncwarp();
     }
   }
+}
+
+// Few experts, few places, no groups: a thread per row, its best keys kept in order as the experts go by.  KL: keys kept (with a bias
+// one more than top_k, whose border is looked at).
+template <typename T, int C, int KL>
+__global__ void __launch_bounds__(ROUTE_THREADS) route_thread_kernel(const RouteParams p) {
+  it_allow_next();
+  it_wait_prior();
+  constexpr int N = kVec<T>;
+  constexpr unsigned full = 0xffffffffu;
+  extern __shared__ double route_smem[];
+  const int E = p.experts, lane = threadIdx.x & 31;
+  double *mine64 = route_smem + (size_t)(threadIdx.x >> 5) * (E + p.n_groups);
+  const bool vec = (E * (int)sizeof(T)) % 16 == 0 && ((uintptr_t)p.logits & 15) == 0;
+  for (int64_t row0 = (int64_t)blockIdx.x * ROUTE_THREADS; row0 < p.n; row0 += (int64_t)gridDim.x * ROUTE_THREADS) {
+    const bool real = row0 + threadIdx.x < p.n;
+    const int64_t row = real ? row0 + threadIdx.x : p.n - 1;
+    const T *from = reinterpret_cast<const T *>(p.logits) + row * E;
+    float key[C];
+    if (vec) {
+#pragma unroll
+      for (int c0 = 0; c0 < C; c0 += N) {
+        float v[N];
+        if (c0 < E) vec_to_f32(__ldg(reinterpret_cast<const uint4 *>(from + c0)), v);
+#pragma unroll
+        for (int i = 0; i < N; ++i) key[c0 + i] = c0 < E ? open_logit(v[i]) : kClosed;
+      }
+    } else {
+#pragma unroll
+      for (int c = 0; c < C; ++c) key[c] = c < E ? open_logit(to_f32(from[c])) : kClosed;
+    }
+    float top = key[0], inv = 1.f;
+#pragma unroll
+    for (int c = 1; c < C; ++c) top = fmaxf(top, key[c]);
+    if (!(top > kClosed)) top = 0.f;
+    auto raw = [&](float l) { return p.sigmoid ? 1.f / (1.f + expf(-l)) : expf(l - top); };
+    if (p.bias || p.need_sum) {
+      float sum = 0.f;
+#pragma unroll
+      for (int c = 0; c < C; ++c) {
+        const float s = raw(key[c]);
+        sum += s;
+      }
+      if (!p.sigmoid) inv = sum > 0.f ? 1.f / sum : 0.f;
+      if (p.bias) {
+#pragma unroll
+        for (int c = 0; c < C; ++c)
+          if (c < E) key[c] = key[c] > kClosed ? open_key(fmaf(raw(key[c]), inv, __ldg(p.bias + c))) : kClosed;
+      }
+    }
+    float best[KL];
+    int at[KL];
+#pragma unroll
+    for (int j = 0; j < KL; ++j) { best[j] = kClosed; at[j] = -1; }
+#pragma unroll
+    for (int c = 0; c < C; ++c) {   // (an equal key that comes later stays behind)
+#pragma unroll
+      for (int j = KL - 1; j > 0; --j) {
+        const bool past = key[c] > best[j - 1], here = key[c] > best[j];
+        at[j] = past ? at[j - 1] : (here ? c : at[j]);
+        best[j] = past ? best[j - 1] : (here ? key[c] : best[j]);
+      }
+      if (key[c] > best[0]) { best[0] = key[c]; at[0] = c; }
+    }
+    float w[KL], sum = 0.f;
+    bool near = false;
+#pragma unroll
+    for (int j = 0; j < KL; ++j) {
+      w[j] = 0.f;
+      float slack = 0.f;
+      if (at[j] >= 0) {
+        const float l = p.bias ? open_logit(to_f32(from[at[j]])) : best[j];
+        w[j] = raw(l) * inv;
+        slack = p.sigmoid ? w[j] : route_slack(w[j], l - top);
+      }
+      if (j < p.k) sum += w[j];
+      if (p.bias && j > 0 && j <= p.k && at[j] >= 0) {
+        const float l = open_logit(to_f32(from[at[j - 1]]));
+        near |= route_near(best[j - 1], best[j], p.sigmoid ? w[j - 1] : route_slack(w[j - 1], l - top), slack);
+      }
+    }
+    const float f = p.renorm ? (sum > 0.f ? p.scale / sum : 0.f) : p.scale;
+    if (real) {
+      int32_t *ids = p.ids + row * p.k;
+      float *ws = p.weights + row * p.k;
+      if (p.k == 2 && (((uintptr_t)p.ids | (uintptr_t)p.weights) & 7) == 0) {
+        *reinterpret_cast<int2 *>(ids) = make_int2(at[0], at[1]);
+        *reinterpret_cast<float2 *>(ws) = make_float2(w[0] * f, w[1] * f);
+      } else {
+#pragma unroll
+        for (int j = 0; j < KL; ++j)
+          if (j < p.k) { ids[j] = at[j]; ws[j] = w[j] * f; }
+      }
+    }
+    unsigned again = p.bias ? __ballot_sync(full, near && real) : 0u;
+    while (again) {
+      const int which = __ffs(again) - 1;
+      again &= again - 1;
+      route_row_exact(p, p.logits, sizeof(T) == 2, row0 + (threadIdx.x & ~31) + which, mine64, lane);
+      __syncwarp();
+    }
+  }
+}
+
+it_status launch_route(void (*kernel)(const RouteParams), const RouteParams &p, int rows_per_block, size_t smem, double bytes, double flops, cudaStream_t st) {
+  if (smem > 48 * 1024) IT_CUDA_TRY(cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)smem));
+  const int64_t blocks = (p.n + rows_per_block - 1) / rows_per_block, most = (int64_t)it_current_sms() * 16;
+  IT_LAUNCH(IT_K_ROUTE, bytes, flops, st,
+            IT_CUDA_TRY(it_launch_pdl(kernel, dim3((unsigned)(blocks < most ? blocks : most)), dim3(ROUTE_THREADS), smem, st, p)));
+  return IT_OK;
 }
 
 template <typename T, int L, int C>
 it_status launch(const RouteParams &p, double bytes, double flops, cudaStream_t st) {
   constexpr int R = 32 / L;
   const size_t warp64 = (size_t)(p.experts + p.n_groups) * 8;
-  const size_t warp32 = ((size_t)R * 2 * p.k + (p.n_groups > 1 ? (size_t)R * (p.experts + p.experts / 32 + 1 + p.n_groups) : 0)) * 4;
-  const size_t smem = ROUTE_WARPS * (warp64 + warp32);
-  if (smem > 48 * 1024) IT_CUDA_TRY(cudaFuncSetAttribute(route_kernel<T, L, C>, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)smem));
-  const int64_t blocks = (p.n + ROUTE_WARPS * R - 1) / (ROUTE_WARPS * R), most = (int64_t)it_current_sms() * 16;
-  IT_LAUNCH(IT_K_ROUTE, bytes, flops, st,
-            IT_CUDA_TRY(it_launch_pdl(route_kernel<T, L, C>, dim3((unsigned)(blocks < most ? blocks : most)), dim3(ROUTE_THREADS), smem, st, p)));
-  return IT_OK;
+  const size_t warp32 = ((size_t)R * 3 * (p.k + 1) + (p.n_groups > 1 ? (size_t)R * (p.experts + p.experts / 32 + 1 + p.n_groups) : 0)) * 4;
+  return launch_route(route_kernel<T, L, C>, p, ROUTE_WARPS * R, ROUTE_WARPS * (warp64 + warp32), bytes, flops, st);
+}
+
+template <typename T, int C>
+it_status launch_thread(const RouteParams &p, double bytes, double flops, cudaStream_t st) {
+  const int kl = p.k + (p.bias ? 1 : 0);
+  const size_t smem = (size_t)ROUTE_WARPS * (p.experts + p.n_groups) * 8;
+  if (kl <= 2) return launch_route(route_thread_kernel<T, C, 2>, p, ROUTE_THREADS, smem, bytes, flops, st);
+  if (kl <= 3) return launch_route(route_thread_kernel<T, C, 3>, p, ROUTE_THREADS, smem, bytes, flops, st);
+  return launch_route(route_thread_kernel<T, C, 5>, p, ROUTE_THREADS, smem, bytes, flops, st);
 }
 
 template <typename T>
 it_status dispatch(const RouteParams &p, double bytes, double flops, cudaStream_t st) {
   const int e = p.experts;
+  if (e <= 32 && p.k <= 4 && p.n_groups == 1) {
+    if (e <= 8) return launch_thread<T, 8>(p, bytes, flops, st);
+    if (e <= 16) return launch_thread<T, 16>(p, bytes, flops, st);
+    return launch_thread<T, 32>(p, bytes, flops, st);
+  }
   if (e <= 8) return launch<T, 1, 8>(p, bytes, flops, st);
   if (e <= 16) return launch<T, 2, 8>(p, bytes, flops, st);
   if (e <= 32) return launch<T, 4, 8>(p, bytes, flops, st);
