@@ -63,8 +63,13 @@ it_status it_launch_expert_gemm(const it_experts_args &a, const it_experts_plan 
 // ----------------------------------------------------------------------------- experts.cu
 // Activations of the experts, in fp32.
 #ifdef __CUDACC__
+__device__ __forceinline__ float it_max_nan(float a, float b) {   // NaN if either is
+  float r;
+  asm("max.NaN.f32 %0, %1, %2;" : "=f"(r) : "f"(a), "f"(b));
+  return r;
+}
 __device__ __forceinline__ float it_expert_act(float v, int act) {
-  if (act == IT_ACT_RELU) return fmaxf(v, 0.f);
+  if (act == IT_ACT_RELU) return it_max_nan(v, 0.f);
   if (act == IT_ACT_ELU) return it_elu(v);
   if (act == IT_ACT_SILU) return __fdividef(v, 1.f + it_exp(-v));   // (off by a few ulp; 0 where the divisor passes 2^126)
   return v;

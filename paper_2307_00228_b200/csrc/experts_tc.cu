@@ -22,7 +22,10 @@ constexpr int EX_EPI_WARPS = 8;    // two per TMEM lane quarter, each takes ever
 constexpr int EX_EPI_SUBS = EX_EPI_WARPS / 4;
 constexpr int EX_THREADS = 32 * (EX_EPI_WARP0 + EX_EPI_WARPS);
 constexpr int EX_STAGE_A = TC_BM * TC_KBLOCK_BYTES;
-constexpr int EX_STAGING = 2048;   // per epilogue warp: 32 rows of 64 bytes (of 128 bytes they would cost a stage of operands)
+// Per epilogue warp: 32 rows of 64 bytes; rows of the output that lie apart are written 128 bytes at a time (at the cost of a stage of operands):
+// 1.5M rows of 512 bytes in halves of a line 339 us, by two warps in turn 634.
+__host__ __device__ constexpr bool ex_direct(it_expert_store s) { return s == IT_EXPERT_OUT_BF16 || s == IT_EXPERT_OUT_F32; }
+__host__ __device__ constexpr int ex_staging(it_expert_store s) { return ex_direct(s) ? 4096 : 2048; }
 // What the epilogue of a tile needs besides the product: places of the rows, their weights and scales, bias and scale of the columns.
 struct ExMeta { int32_t place[TC_BM]; float weight[TC_BM]; float bias[256]; };
 struct ExMetaEight : ExMeta { float xs[TC_BM]; float scale[256]; };
@@ -61,14 +64,64 @@ __device__ __forceinline__ void ex_mma(uint32_t d_tmem, uint64_t a_desc, uint64_
   }
 }
 
-template <int N> __device__ __forceinline__ void expert_act(float (&v)[N], int act) {
-  if (act == IT_ACT_RELU) {
+// Lane i of the warp reads 32 consecutive columns of TMEM lane (lane base of taddr) + i.
+__device__ __forceinline__ void tmem_ld32(uint32_t taddr, uint32_t (&r)[32]) {
+  asm volatile(
+      "tcgen05.ld.sync.aligned.32x32b.x32.b32 {%0, %1, %2, %3, %4, %5, %6, %7, %8, %9, %10, %11, %12, %13, %14, %15, "
+      "%16, %17, %18, %19, %20, %21, %22, %23, %24, %25, %26, %27, %28, %29, %30, %31}, [%32];"
+      : "=r"(r[0]), "=r"(r[1]), "=r"(r[2]), "=r"(r[3]), "=r"(r[4]), "=r"(r[5]), "=r"(r[6]), "=r"(r[7]), "=r"(r[8]), "=r"(r[9]), "=r"(r[10]),
+        "=r"(r[11]), "=r"(r[12]), "=r"(r[13]), "=r"(r[14]), "=r"(r[15]), "=r"(r[16]), "=r"(r[17]), "=r"(r[18]), "=r"(r[19]), "=r"(r[20]),
+        "=r"(r[21]), "=r"(r[22]), "=r"(r[23]), "=r"(r[24]), "=r"(r[25]), "=r"(r[26]), "=r"(r[27]), "=r"(r[28]), "=r"(r[29]), "=r"(r[30]), "=r"(r[31])
+      : "r"(taddr));
+}
+// Two fp32 values at a time: an epilogue is bound by its instructions.
+__device__ __forceinline__ uint64_t pack2(uint32_t lo, uint32_t hi) {
+  uint64_t d;
+  asm("mov.b64 %0, {%1, %2};" : "=l"(d) : "r"(lo), "r"(hi));
+  return d;
+}
+__device__ __forceinline__ float2 unpack2(uint64_t a) {
+  float2 d;
+  asm("mov.b64 {%0, %1}, %2;" : "=f"(d.x), "=f"(d.y) : "l"(a));
+  return d;
+}
+__device__ __forceinline__ uint64_t add2(uint64_t a, uint64_t b) {
+  uint64_t d;
+  asm("add.rn.f32x2 %0, %1, %2;" : "=l"(d) : "l"(a), "l"(b));
+  return d;
+}
+__device__ __forceinline__ uint64_t mul2(uint64_t a, uint64_t b) {
+  uint64_t d;
+  asm("mul.rn.f32x2 %0, %1, %2;" : "=l"(d) : "l"(a), "l"(b));
+  return d;
+}
+__device__ __forceinline__ uint64_t fma2(uint64_t a, uint64_t b, uint64_t c) {
+  uint64_t d;
+  asm("fma.rn.f32x2 %0, %1, %2, %3;" : "=l"(d) : "l"(a), "l"(b), "l"(c));
+  return d;
+}
+__device__ __forceinline__ uint32_t bf16x2_of(float lo, float hi) {
+  const __nv_bfloat162 h = __floats2bfloat162_rn(lo, hi);
+  return *reinterpret_cast<const uint32_t *>(&h);
+}
+__device__ __forceinline__ uint32_t max_bf16x2(uint32_t a, uint32_t b) {   // NaN stays
+  uint32_t d;
+  asm("max.NaN.bf16x2 %0, %1, %2;" : "=r"(d) : "r"(a), "r"(b));
+  return d;
+}
+
+// The activation of 32 columns (one decision for all of them).
+template <int ACT> __device__ __forceinline__ void expert_act_as(uint64_t (&v)[16]) {
 #pragma unroll
-    for (int i = 0; i < N; ++i) v[i] = fmaxf(v[i], 0.f);
-  } else if (act != IT_ACT_NONE) {
-#pragma unroll
-    for (int i = 0; i < N; ++i) v[i] = it_expert_act(v[i], act);
+  for (int i = 0; i < 16; ++i) {
+    const float2 f = unpack2(v[i]);
+    v[i] = pack2(__float_as_uint(it_expert_act(f.x, ACT)), __float_as_uint(it_expert_act(f.y, ACT)));
   }
+}
+__device__ __forceinline__ void expert_act(uint64_t (&v)[16], int act) {
+  if (act == IT_ACT_RELU) expert_act_as<IT_ACT_RELU>(v);
+  else if (act == IT_ACT_ELU) expert_act_as<IT_ACT_ELU>(v);
+  else if (act == IT_ACT_SILU) expert_act_as<IT_ACT_SILU>(v);
 }
 
 struct ExParams {
@@ -108,7 +161,7 @@ expert_gemm_kernel(const __grid_constant__ CUtensorMap map_a, const __grid_const
 
   unsigned char *staging = base + (size_t)p.stages * stage_bytes;
   using Meta = std::conditional_t<EIGHT, ExMetaEight, ExMeta>;
-  Meta *meta = reinterpret_cast<Meta *>(staging + EX_EPI_WARPS * EX_STAGING);   // [2], one per accumulator
+  Meta *meta = reinterpret_cast<Meta *>(staging + EX_EPI_WARPS * ex_staging(STORE));   // [2], one per accumulator
   uint64_t *full = reinterpret_cast<uint64_t *>(meta + 2);   // [stages]
   uint64_t *empty = full + EX_MAX_STAGES;      // [stages]
   uint64_t *acc_full = empty + EX_MAX_STAGES;  // [2]
@@ -313,9 +366,15 @@ expert_gemm_kernel(const __grid_constant__ CUtensorMap map_a, const __grid_const
     // ------------------------------------------------------------------ epilogue: a thread per row of the tile, a warp per 32 rows and step of columns
     const int quarter = warp & 3, sub = (warp - EX_EPI_WARP0) >> 2;   // a warp may only touch TMEM lanes [32 * (warp % 4), +32)
     constexpr bool F32_OUT = STORE == IT_EXPERT_SUMS || STORE == IT_EXPERT_OUT_F32, DIRECT = STORE == IT_EXPERT_OUT_BF16 || STORE == IT_EXPERT_OUT_F32;
-    constexpr int STEP = F32_OUT ? 16 : 32;   // columns that a warp takes at a time: 64 bytes of a row, written
+    constexpr int ESIZE = F32_OUT ? 4 : 2, COLS = 64 / ESIZE;   // 64 bytes of a row are staged at a time
     constexpr int PLANES = STORE == IT_EXPERT_PARTS ? 3 : 1;
-    const uint32_t stage_s = smem_u32(staging) + (uint32_t)(warp - EX_EPI_WARP0) * EX_STAGING, swz = ((uint32_t)lane >> 1) & 3u;
+    constexpr int ROW = DIRECT ? 128 : 64, PIECES = ROW / 16, AT_ONCE = 32 / PIECES;   // staging tile: bytes of a row, its lanes, rows that a warp stores at once
+    const uint32_t stage_s = smem_u32(staging) + (uint32_t)(warp - EX_EPI_WARP0) * ex_staging(STORE);
+    // 16-byte pieces are swizzled: this lane's row as it writes it (piece i: put ^ 16 i), and its piece of every row that it stores
+    const int row0 = lane / PIECES, piece = lane % PIECES;
+    const uint32_t put = stage_s + (uint32_t)lane * ROW + (uint32_t)((DIRECT ? lane & 7 : (lane >> 1) & 3) << 4);
+    const uint32_t row8 = 8u * (uint32_t)p.cols * ESIZE;
+    const uint32_t floor2 = p.act == IT_ACT_RELU ? 0u : 0xff80ff80u;   // bf16 pair: 0, or minus infinity where nothing is cut off
     uint32_t acc = 0, acc_phase = 0;
     for (uint32_t tile = blockIdx.x; tile < n_tiles; tile += gridDim.x) {
       const int m = (int)(tile / splits), c_tile = (int)(tile % splits) * p.cols_per_tile;
@@ -325,100 +384,136 @@ expert_gemm_kernel(const __grid_constant__ CUtensorMap map_a, const __grid_const
       if (!__all_sync(0xffffffffu, ok)) break;
       tc_fence_after();
       const Meta &k = meta[acc];
-      float xs = 1.f, weight = 1.f;
-      if constexpr (EIGHT) xs = k.xs[quarter * 32 + lane];
-      if constexpr (DIRECT) weight = k.weight[quarter * 32 + lane];
+      uint64_t xs2 = 0, weight2 = 0;
+      if constexpr (EIGHT) { const uint32_t x = __float_as_uint(k.xs[quarter * 32 + lane]); xs2 = pack2(x, x); }
+      if constexpr (DIRECT) { const uint32_t x = __float_as_uint(k.weight[quarter * 32 + lane]); weight2 = pack2(x, x); }
+      unsigned char *to = reinterpret_cast<unsigned char *>(p.dst) + ((DIRECT ? 0 : pos0 + row0) * p.cols + c_tile) * ESIZE + piece * 16;
+      uint32_t real = 0;   // rows of this lane that are stored
+      if constexpr (!DIRECT) {
+#pragma unroll
+        for (int i = 0; i < 4; ++i) real |= (k.place[quarter * 32 + 8 * i + row0] >= 0 ? 1u : 0u) << i;
+      }
       const uint32_t taddr = tmem_base + ((uint32_t)(quarter * 32) << 16) + acc * (uint32_t)p.bn;
       const int width = p.cols - c_tile < p.cols_per_tile ? p.cols - c_tile : p.cols_per_tile;
-      const int steps = width > sub * STEP ? (width - sub * STEP + EX_EPI_SUBS * STEP - 1) / (EX_EPI_SUBS * STEP) : 0;   // of this warp
-      uint32_t r[16], r2[16];   // 16 columns of the accumulator; gated: and of what they gate
-      auto fetch = [&](int col) {
-        tmem_ld16(taddr + (uint32_t)col, r);
-        if constexpr (GATED) tmem_ld16(taddr + (uint32_t)(p.cols_per_tile + col), r2);
+      // 64 bytes of this lane's row into the staging tile ...
+      auto stage = [&](const uint32_t *w, int half) {
+#pragma unroll
+        for (int i = 0; i < 4; ++i) st_shared_v4(put ^ (16u * (4 * half + i)), w[4 * i], w[4 * i + 1], w[4 * i + 2], w[4 * i + 3]);
       };
-      if (steps > 0) fetch(sub * STEP);
-      for (int s = 0; s < steps; ++s) {
-        const int ch = (s * EX_EPI_SUBS + sub) * STEP;   // first column of the step in the tile
-        uint32_t w[PLANES][16];
+      // ... and out again as pieces of rows; c: their first column in the tile
+      auto flush = [&](int c, int64_t plane, bool both) {
+        __syncwarp();
+        const bool in = c + piece * (16 / ESIZE) < width && (!DIRECT || both || piece < 4);
 #pragma unroll
-        for (int q = 0; q < STEP; q += 16) {
-          float v[16];
-          tmem_ld_wait();
-          auto finish = [&](const uint32_t (&acc_r)[16], int at_c) {   // accumulator -> scaled, with the bias
-#pragma unroll
-            for (int i = 0; i < 4; ++i) {
-              const float4 b = *reinterpret_cast<const float4 *>(k.bias + at_c + 4 * i);
-              if constexpr (EIGHT) {
-                const float4 f = *reinterpret_cast<const float4 *>(k.scale + at_c + 4 * i);
-                v[4 * i] = fmaf(__uint_as_float(acc_r[4 * i]) * xs, f.x, b.x); v[4 * i + 1] = fmaf(__uint_as_float(acc_r[4 * i + 1]) * xs, f.y, b.y);
-                v[4 * i + 2] = fmaf(__uint_as_float(acc_r[4 * i + 2]) * xs, f.z, b.z); v[4 * i + 3] = fmaf(__uint_as_float(acc_r[4 * i + 3]) * xs, f.w, b.w);
-              } else {
-                v[4 * i] = __uint_as_float(acc_r[4 * i]) + b.x; v[4 * i + 1] = __uint_as_float(acc_r[4 * i + 1]) + b.y;
-                v[4 * i + 2] = __uint_as_float(acc_r[4 * i + 2]) + b.z; v[4 * i + 3] = __uint_as_float(acc_r[4 * i + 3]) + b.w;
-              }
-            }
-          };
-          float gate[GATED ? 16 : 1];
-          finish(r, ch + q);
-          if constexpr (GATED) {
-#pragma unroll
-            for (int i = 0; i < 16; ++i) gate[i] = v[i];
-            finish(r2, p.cols_per_tile + ch + q);
-          }
-          // the next 16 columns are fetched while these are finished
-          if (q + 16 < STEP) fetch(ch + q + 16);
-          else if (s + 1 < steps) fetch(ch + EX_EPI_SUBS * STEP);
-          if constexpr (GATED) {
-            expert_act(gate, p.act);
-#pragma unroll
-            for (int i = 0; i < 16; ++i) v[i] *= gate[i];
+        for (int i = 0; i < 32 / AT_ONCE; ++i) {
+          const int row = AT_ONCE * i + row0;
+          const uint32_t from = stage_s + (uint32_t)row * ROW + (uint32_t)((piece ^ (DIRECT ? row & 7 : (row >> 1) & 3)) << 4);
+          uint4 d;
+          asm volatile("ld.shared.v4.b32 {%0, %1, %2, %3}, [%4];" : "=r"(d.x), "=r"(d.y), "=r"(d.z), "=r"(d.w) : "r"(from) : "memory");
+          if constexpr (DIRECT) {
+            const int at = k.place[quarter * 32 + row];
+            if (in && at >= 0) *reinterpret_cast<uint4 *>(to + ((int64_t)at * p.cols + c) * ESIZE) = d;
           } else {
-            expert_act(v, p.act);
+            if (in && ((real >> i) & 1u)) *reinterpret_cast<uint4 *>(to + (uint64_t)i * row8 + (plane + c) * ESIZE) = d;
+          }
+        }
+        __syncwarp();
+      };
+      // this warp's columns: one half of the tile's, so that what it writes of a row lies together
+      const int half_cols = (width + 32 * EX_EPI_SUBS - 1) / (32 * EX_EPI_SUBS) * 32, lo = sub * half_cols, hi = lo + half_cols < width ? lo + half_cols : width;
+      // 32 columns of the accumulator (gated: and of what they gate), from c on
+      auto finish = [&](const uint32_t (&r)[32], const uint32_t (&r2)[GATED ? 32 : 1], int c) {
+        uint64_t v[16];
+        auto scaled = [&](const uint32_t *acc_r, int at, uint64_t *o) {
+          const ulonglong2 *b = reinterpret_cast<const ulonglong2 *>(k.bias + at);
+#pragma unroll
+          for (int i = 0; i < 8; ++i) {
+            const ulonglong2 bb = b[i];
+            uint64_t lo = pack2(acc_r[4 * i], acc_r[4 * i + 1]), hi = pack2(acc_r[4 * i + 2], acc_r[4 * i + 3]);
+            if constexpr (EIGHT) {
+              const ulonglong2 f = reinterpret_cast<const ulonglong2 *>(k.scale + at)[i];
+              lo = fma2(mul2(lo, xs2), f.x, bb.x);
+              hi = fma2(mul2(hi, xs2), f.y, bb.y);
+            } else {
+              lo = add2(lo, bb.x);
+              hi = add2(hi, bb.y);
+            }
+            o[2 * i] = lo;
+            o[2 * i + 1] = hi;
+          }
+        };
+        scaled(r, c, v);
+        constexpr bool CUT_LATER = !F32_OUT && !GATED && !DIRECT && STORE != IT_EXPERT_PARTS;   // ReLU on the rounded pairs
+        if (!CUT_LATER || p.act != IT_ACT_RELU) expert_act(v, p.act);
+        if constexpr (GATED) {
+          uint64_t u[16];
+          scaled(r2, p.cols_per_tile + c, u);
+#pragma unroll
+          for (int i = 0; i < 16; ++i) v[i] = mul2(v[i], u[i]);
+        }
+        if constexpr (DIRECT) {
+#pragma unroll
+          for (int i = 0; i < 16; ++i) v[i] = mul2(v[i], weight2);
+        }
+        if constexpr (F32_OUT) {
+          uint32_t w[32];
+#pragma unroll
+          for (int i = 0; i < 16; ++i) {
+            const float2 f = unpack2(v[i]);
+            w[2 * i] = __float_as_uint(f.x); w[2 * i + 1] = __float_as_uint(f.y);
           }
           if constexpr (DIRECT) {
-#pragma unroll
-            for (int i = 0; i < 16; ++i) v[i] *= weight;
-          }
-          if constexpr (F32_OUT) {
-#pragma unroll
-            for (int i = 0; i < 16; ++i) w[0][i] = __float_as_uint(v[i]);
-          } else if constexpr (STORE == IT_EXPERT_PARTS) {
-#pragma unroll
-            for (int i = 0; i < 16; i += 2) {
-              const float2 x1 = make_float2(v[i] - __uint_as_float(__float_as_uint(v[i]) & 0xffff0000u), v[i + 1] - __uint_as_float(__float_as_uint(v[i + 1]) & 0xffff0000u));
-              const float2 x2 = make_float2(x1.x - __uint_as_float(__float_as_uint(x1.x) & 0xffff0000u), x1.y - __uint_as_float(__float_as_uint(x1.y) & 0xffff0000u));
-              w[0][(q + i) / 2] = __byte_perm(__float_as_uint(v[i]), __float_as_uint(v[i + 1]), 0x7632);
-              w[1][(q + i) / 2] = __byte_perm(__float_as_uint(x1.x), __float_as_uint(x1.y), 0x7632);
-              w[2][(q + i) / 2] = __byte_perm(__float_as_uint(x2.x), __float_as_uint(x2.y), 0x7632);
-            }
+            stage(w, 0);
+            stage(w + 16, 1);
+            flush(c, 0, true);
           } else {
-#pragma unroll
-            for (int i = 0; i < 16; i += 2) {
-              const __nv_bfloat162 h = __floats2bfloat162_rn(v[i], v[i + 1]);
-              w[0][(q + i) / 2] = *reinterpret_cast<const uint32_t *>(&h);
+            stage(w, 0);
+            flush(c, 0, false);
+            if (c + COLS < width) {
+              stage(w + 16, 0);
+              flush(c + COLS, 0, false);
             }
           }
-        }
-        // rows of 64 bytes through the staging tile, four lanes a row
-        constexpr int ESIZE = F32_OUT ? 4 : 2;
-        const int piece = lane & 3, c64 = c_tile + ch + piece * (16 / ESIZE);
+        } else if constexpr (STORE == IT_EXPERT_PARTS) {
+          constexpr uint64_t MINUS = 0xbf800000bf800000ull;   // (-1, -1)
 #pragma unroll
-        for (int pl = 0; pl < PLANES; ++pl) {
+          for (int pl = 0; pl < PLANES; ++pl) {   // the upper halves, then what they leave
+            uint32_t w[16];
 #pragma unroll
-          for (int i = 0; i < 4; ++i)
-            st_shared_v4(stage_s + (uint32_t)lane * 64u + (((uint32_t)i ^ swz) << 4), w[pl][4 * i], w[pl][4 * i + 1], w[pl][4 * i + 2], w[pl][4 * i + 3]);
-          __syncwarp();
-#pragma unroll
-          for (int r0 = 0; r0 < 32; r0 += 8) {
-            const int row = r0 + (lane >> 2), at = k.place[quarter * 32 + row];
-            uint4 d;
-            asm volatile("ld.shared.v4.b32 {%0, %1, %2, %3}, [%4];" : "=r"(d.x), "=r"(d.y), "=r"(d.z), "=r"(d.w)
-                         : "r"(stage_s + (uint32_t)row * 64u + ((uint32_t)(piece ^ ((row >> 1) & 3)) << 4)) : "memory");
-            if (at >= 0 && c64 < p.cols)
-              *reinterpret_cast<uint4 *>(reinterpret_cast<unsigned char *>(p.dst) + (pl * p.part_stride + (DIRECT ? (int64_t)at : pos0 + row) * p.cols + c64) * ESIZE) = d;
+            for (int i = 0; i < 16; ++i) {
+              const float2 f = unpack2(v[i]);
+              const uint32_t lo = __float_as_uint(f.x), hi = __float_as_uint(f.y);
+              w[i] = __byte_perm(lo, hi, 0x7632);
+              if (pl < 2) v[i] = fma2(pack2(lo & 0xffff0000u, hi & 0xffff0000u), MINUS, v[i]);
+            }
+            stage(w, 0);
+            flush(c, pl * p.part_stride, false);
           }
-          __syncwarp();
+        } else {
+          uint32_t w[16];
+#pragma unroll
+          for (int i = 0; i < 16; ++i) {
+            const float2 f = unpack2(v[i]);
+            w[i] = bf16x2_of(f.x, f.y);
+            if constexpr (CUT_LATER) w[i] = max_bf16x2(w[i], floor2);
+          }
+          if constexpr (DIRECT) {
+            const int half = ((c - lo) >> 5) & 1;
+            stage(w, half);
+            if (half == 1 || c + 32 >= hi) flush(c - 32 * half, 0, half == 1);
+          } else {
+            stage(w, 0);
+            flush(c, 0, false);
+          }
         }
+      };
+      // (the next 32 columns read ahead would take registers that are not there: with them spilled the epilogue took twice as long)
+      uint32_t r[32], r2[GATED ? 32 : 1];
+      for (int c = lo; c < hi; c += 32) {
+        tmem_ld32(taddr + (uint32_t)c, r);
+        if constexpr (GATED) tmem_ld32(taddr + (uint32_t)(p.cols_per_tile + c), r2);
+        tmem_ld_wait();
+        finish(r, r2, c);
       }
       tc_fence_before();
       __syncwarp();
@@ -484,7 +579,7 @@ it_status it_launch_expert_gemm(const it_experts_args &a, const it_experts_plan 
   IT_TRY(encode(&ma, g.eight, g.A, 2, da, sa, ba));
   IT_TRY(encode(&mw, g.eight, g.W, 3, dw, sw, bw));
 
-  const int stage = EX_STAGE_A + p.bn * TC_KBLOCK_BYTES, fixed = EX_EPI_WARPS * EX_STAGING + 2 * (int)(g.eight ? sizeof(ExMetaEight) : sizeof(ExMeta)) + (2 * EX_MAX_STAGES + 9) * 8;
+  const int stage = EX_STAGE_A + p.bn * TC_KBLOCK_BYTES, fixed = EX_EPI_WARPS * ex_staging(g.store) + 2 * (int)(g.eight ? sizeof(ExMetaEight) : sizeof(ExMeta)) + (2 * EX_MAX_STAGES + 9) * 8;
   p.stages = (227 * 1024 - fixed) / stage;
   if (p.stages > EX_MAX_STAGES) p.stages = EX_MAX_STAGES;
   const int smem = fixed + p.stages * stage;
