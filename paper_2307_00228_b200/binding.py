@@ -409,17 +409,28 @@ def _dtype_code(t: torch.dtype) -> int:
     return _DTYPES[t]
 
 
-def _addr(name, t, dtype, shape, optional=False):
-    """Address of a dense tensor on the current device, its type and shape checked (the library sees addresses only)."""
+_raw_stream = getattr(torch._C, "_cuda_getCurrentRawStream", None)   # the current stream without an object around it
+
+
+def _device() -> int:
+    return torch._C._cuda_getDevice() if torch.cuda.is_initialized() else -2   # (-1 is what a CPU tensor says)
+
+
+def _addr(name, t, dtype, shape, device):
+    """Address of a dense tensor on the current device, its type and shape checked (the library sees addresses only); None stays None."""
     if t is None:
-        if not optional:
-            raise ValueError(f"{name} is None")
         return None
-    if t.dtype != dtype or tuple(t.shape) != tuple(shape):
-        raise ValueError(f"{name} is {t.dtype} {tuple(t.shape)}, expected {dtype} {tuple(shape)}")
-    if not t.is_cuda or not t.is_contiguous() or t.device.index != torch.cuda.current_device():
+    if t.dtype is not dtype or t.shape != shape:
+        raise ValueError(f"{name} is {t.dtype} {tuple(t.shape)}, expected {dtype} {shape}")
+    if t.get_device() != device or not t.is_contiguous():
         raise ValueError(f"{name} must be a contiguous tensor on the current CUDA device")
     return t.data_ptr()
+
+
+def _stream_on(device, stream):
+    if stream is not None:
+        return stream.cuda_stream
+    return _raw_stream(device) if _raw_stream is not None else torch.cuda.current_stream().cuda_stream
 
 
 @dataclass(frozen=True)
@@ -435,15 +446,18 @@ class NormDesc:
         out = self.feat_dtype if self.out_dtype is None else self.out_dtype
         object.__setattr__(self, "out_dtype", out)
         object.__setattr__(self, "_c", it_norm_desc(self.dim, _dtype_code(self.feat_dtype), _dtype_code(out), self.eps,
-                                                    _addr("weight", self.weight, torch.float32, (self.dim,), optional=True)))
+                                                    _addr("weight", self.weight, torch.float32, (self.dim,), _device())))
+        object.__setattr__(self, "_ref", C.byref(self._c))
 
 
 def it_residual_norm(d: NormDesc, x, out, residual=None, sum_out=None, scales=None, stream=None):
     """s = x + residual; out = s / sqrt(mean(s^2) + eps) * weight, in feat_dtype or in e4m3 with scales [n]; sum_out = s.  Returns out."""
-    shape = (x.shape[0], d.dim)
-    _check(lib().it_residual_norm(C.byref(d._c), shape[0], _addr("x", x, d.feat_dtype, shape), _addr("residual", residual, d.feat_dtype, shape, True),
-                                  _addr("sum_out", sum_out, d.feat_dtype, shape, True), _addr("out", out, d.out_dtype, shape),
-                                  _addr("scales", scales, torch.float32, shape[:1], True), _stream(stream)))
+    n, f, dev = x.shape[0], d.feat_dtype, _device()
+    shape = (n, d.dim)
+    status = lib().it_residual_norm(d._ref, n, _addr("x", x, f, shape, dev), _addr("residual", residual, f, shape, dev), _addr("sum_out", sum_out, f, shape, dev),
+                                    _addr("out", out, d.out_dtype, shape, dev), _addr("scales", scales, torch.float32, (n,), dev), _stream_on(dev, stream))
+    if status:
+        _check(status)
     return out
 
 
@@ -462,16 +476,20 @@ class RouteDesc:
     weight_scale: float = 1.0
 
     def __post_init__(self):
-        bias = _addr("balance_bias", self.balance_bias, torch.float32, (self.n_experts,), optional=True)
+        bias = _addr("balance_bias", self.balance_bias, torch.float32, (self.n_experts,), _device())
         object.__setattr__(self, "_c", it_route_desc(self.n_experts, self.top_k, _dtype_code(self.logit_dtype), SCORES[self.score], bias, self.n_groups,
                                                      self.group_k, self.group_best, int(self.renormalise), self.weight_scale))
+        object.__setattr__(self, "_ref", C.byref(self._c))
 
 
 def it_route(d: RouteDesc, logits, ids, weights, stream=None):
     """logits [n, n_experts] -> ids int32 [n, top_k] (-1: none left), weights fp32 [n, top_k].  Returns (ids, weights)."""
-    n = logits.shape[0]
-    _check(lib().it_route(C.byref(d._c), n, _addr("logits", logits, d.logit_dtype, (n, d.n_experts)), _addr("ids", ids, torch.int32, (n, d.top_k)),
-                          _addr("weights", weights, torch.float32, (n, d.top_k)), _stream(stream)))
+    n, dev = logits.shape[0], _device()
+    chosen = (n, d.top_k)
+    status = lib().it_route(d._ref, n, _addr("logits", logits, d.logit_dtype, (n, d.n_experts), dev), _addr("ids", ids, torch.int32, chosen, dev),
+                            _addr("weights", weights, torch.float32, chosen, dev), _stream_on(dev, stream))
+    if status:
+        _check(status)
     return ids, weights
 
 
@@ -497,17 +515,18 @@ class ExpertsDesc:
         n1 = h * (2 if self.gated else 1) if h > 0 else o
         eight = self.W1.dtype == torch.float8_e4m3fn
         object.__setattr__(self, "in_dtype", torch.float8_e4m3fn if eight else self.feat_dtype)
-        f32 = torch.float32
+        f32, dev = torch.float32, _device()
         c = it_experts_desc(e, self.top_k, self.in_dim, h, o, _dtype_code(self.feat_dtype), _dtype_code(self.in_dtype), EXPERT_ACTS[self.act], int(self.gated),
-                            _addr("W1", self.W1, self.in_dtype, (e, self.in_dim, n1)), _addr("b1", self.b1, f32, (e, n1), True),
-                            _addr("W2", self.W2, self.feat_dtype, (e, h, o), True), _addr("b2", self.b2, f32, (e, o), True),
-                            _addr("w1_scale", self.w1_scale, f32, (e, n1), True))
+                            _addr("W1", self.W1, self.in_dtype, (e, self.in_dim, n1), dev), _addr("b1", self.b1, f32, (e, n1), dev),
+                            _addr("W2", self.W2, self.feat_dtype, (e, h, o), dev), _addr("b2", self.b2, f32, (e, o), dev),
+                            _addr("w1_scale", self.w1_scale, f32, (e, n1), dev))
         object.__setattr__(self, "_c", c)
+        object.__setattr__(self, "_ref", C.byref(c))
 
 
 def it_experts_workspace_bytes(d: ExpertsDesc, n: int) -> int:
     out = C.c_size_t()
-    _check(lib().it_experts_workspace_bytes(C.byref(d._c), n, C.byref(out)))
+    _check(lib().it_experts_workspace_bytes(d._ref, n, C.byref(out)))
     return out.value
 
 
@@ -522,11 +541,15 @@ def it_debug_expire_wait_experts(d: ExpertsDesc, x, ids, weights, out, workspace
 
 
 def _experts(call, d, x, ids, weights, out, workspace, x_scale, stream):
-    n = x.shape[0]
-    f32 = torch.float32
-    _check(call(C.byref(d._c), n, _addr("x", x, d.in_dtype, (n, d.in_dim)), _addr("x_scale", x_scale, f32, (n,), True),
-                                    _addr("ids", ids, torch.int32, (n, d.top_k)), _addr("weights", weights, f32, (n, d.top_k)),
-                                    _addr("out", out, d.feat_dtype, (n, d.out_dim)), _ptr(workspace), _nbytes(workspace), _stream(stream)))
+    n, f32, dev = x.shape[0], torch.float32, _device()
+    chosen = (n, d.top_k)
+    if not workspace.is_contiguous() or workspace.get_device() != dev:
+        raise ValueError("workspace must be a contiguous tensor on the current CUDA device")
+    status = call(d._ref, n, _addr("x", x, d.in_dtype, (n, d.in_dim), dev), _addr("x_scale", x_scale, f32, (n,), dev), _addr("ids", ids, torch.int32, chosen, dev),
+                  _addr("weights", weights, f32, chosen, dev), _addr("out", out, d.feat_dtype, (n, d.out_dim), dev), workspace.data_ptr(), _nbytes(workspace),
+                  _stream_on(dev, stream))
+    if status:
+        _check(status)
     return out
 
 

@@ -123,14 +123,14 @@ __device__ void route_row_exact(const RouteParams &p, const void *logits, bool b
 }
 
 // ----------------------------------------------------------------------------- the fast kernel
-// Whether fp32 leaves open which of two keys (or sums of keys) a >= b is larger.  pa, pb: the scores in them, each off by at most 5 ulp
-// (expf 2, the sum of a row 1, the division 1, their product 1); adding a bias rounds once more, by half an ulp of the key.
-// In a softmax the difference from the row's largest logit is rounded too, by |difference| * 2^-24: pa and pb come with that share
-// (route_slack), which below 1e-30 would no longer be represented.
+// Whether fp32 leaves open which of two keys (or sums of keys) a >= b is larger.  pa, pb: the scores in them, each off by at most 2e-6 of itself
+// (the hardware exponential 2^-22, a reciprocal 2^-23, the sum of a row up to 21 additions, two products); adding a bias rounds once more, by
+// half an ulp of the key.  The exponent is rounded too, twice, by |exponent| * 2^-24: pa and pb come with that share (route_slack), which
+// below 1e-30 would no longer be represented.
 __device__ __forceinline__ bool route_near(float a, float b, float pa, float pb) {
-  return a - b <= 1e-6f * (pa + pb) + 2.5e-7f * (fabsf(a) + fabsf(b)) + 1e-30f;
+  return a - b <= 2e-6f * (pa + pb) + 2.5e-7f * (fabsf(a) + fabsf(b)) + 1e-30f;
 }
-__device__ __forceinline__ float route_slack(float score, float below_top) { return score * fmaf(fabsf(below_top), 0.125f, 1.f); }
+__device__ __forceinline__ float route_slack(float score, float below_top) { return score * fmaf(fabsf(below_top), 0.0625f, 1.f); }
 
 // A float as an unsigned number of the same order (neither operand is NaN; -0 counts as 0).
 __device__ __forceinline__ unsigned route_order(float k) {
@@ -155,16 +155,19 @@ __global__ void __launch_bounds__(ROUTE_THREADS) route_kernel(const RouteParams 
   double *mine64 = route_smem + (size_t)warp * per_warp;
   const int row_words = E + E / 32 + 1 + p.n_groups;   // a pad word after every 32 keys
   float *after = reinterpret_cast<float *>(route_smem + (size_t)ROUTE_WARPS * per_warp);
-  const int warp_words = R * 3 * rounds + (p.n_groups > 1 ? R * row_words : 0);
+  const int warp_words = R * 3 * rounds + (L == 32 ? 64 : 0) + (p.n_groups > 1 ? R * row_words : 0);
   int32_t *at_s = reinterpret_cast<int32_t *>(after + (size_t)warp * warp_words);
-  float *key_s = reinterpret_cast<float *>(at_s + R * rounds), *score_s = key_s + R * rounds;
+  unsigned *order_s = reinterpret_cast<unsigned *>(at_s + R * rounds + 32);   // (one row a warp: 32 candidates, their experts behind the choices)
+  float *key_s = reinterpret_cast<float *>(at_s + R * rounds + (L == 32 ? 64 : 0)), *score_s = key_s + R * rounds;
   float *keys = score_s + R * rounds + (size_t)r * row_words, *worth = keys + E + E / 32 + 1;
   auto expert = [&](int c) { return ((c / N) * L + gl) * N + c % N; };
   const bool vec = (E * (int)sizeof(T)) % 16 == 0 && N == kVec<T> && ((uintptr_t)p.logits & 15) == 0;
   float bias[C];
 #pragma unroll
   for (int c = 0; c < C; ++c) bias[c] = p.bias && expert(c) < E ? p.bias[expert(c)] : 0.f;
-  // groups: lanes that scan one group together
+  // groups: whether they are runs of lanes, and of how many; else lanes that scan one group together
+  const int segment = p.group_size / N;
+  const bool segments = p.n_groups > 1 && p.n_groups <= 64 && p.group_size % N == 0 && segment <= L && (segment & (segment - 1)) == 0;
   int per_group = 1;
   while (per_group * 2 * p.n_groups <= L && p.group_size % (per_group * 2) == 0) per_group *= 2;
 
@@ -197,12 +200,13 @@ __global__ void __launch_bounds__(ROUTE_THREADS) route_kernel(const RouteParams 
       if (!(top > kClosed)) top = 0.f;   // nothing is open
     }
     auto raw = [&](float l, float top_of) { return p.sigmoid ? 1.f / (1.f + expf(-l)) : expf(l - top_of); };   // (a closed logit: 0)
+    auto rough = [&](float l) { return p.sigmoid ? __fdividef(1.f, 1.f + it_exp(-l)) : it_exp(l - top); };         // what keys are made of
     bool near = false;
     if (p.bias || p.need_sum) {
       float sum = 0.f, s[C];
 #pragma unroll
       for (int c = 0; c < C; ++c) {
-        s[c] = raw(key[c], top);
+        s[c] = p.bias ? rough(key[c]) : raw(key[c], top);
         sum += s[c];
       }
       if (!p.sigmoid) {
@@ -215,7 +219,62 @@ __global__ void __launch_bounds__(ROUTE_THREADS) route_kernel(const RouteParams 
         for (int c = 0; c < C; ++c) key[c] = key[c] > kClosed ? open_key(fmaf(s[c], inv, bias[c])) : kClosed;
       }
     }
-    if (p.n_groups > 1) {
+    const bool exact_worth = !p.bias && p.group_best == 1;
+    // a worth with a bias: two scores of at most inv each, whose slack (x e^-x / 16) is below 3 %; without: sums of e^-x with x < 104
+    auto worth_near = [&](float v, float w) { return route_near(v, w, p.bias ? 2.2f * inv : 8.f * v, p.bias ? 2.2f * inv : 8.f * w); };
+    auto worth_of = [&](float a, float b) {   // a group's two largest keys
+      if (p.group_best == 1 || !(a > kClosed)) return a;
+      const float second = b > kClosed ? (p.bias ? b : raw(b, top)) : 0.f;
+      return (p.bias ? a : raw(a, top)) + second;
+    };
+    if (p.n_groups > 1 && segments) {
+      // groups are runs of lanes in every chunk of N consecutive experts a lane: nothing leaves the registers
+      constexpr int CH = C / N;
+      float w[CH], keep = INFINITY, drop = kClosed;   // worth of this lane's group in every chunk; the least that is kept, the most that is not
+      int rank[CH];
+#pragma unroll
+      for (int j = 0; j < CH; ++j) {
+        float a = kClosed, b = kClosed;
+#pragma unroll
+        for (int i = 0; i < N; ++i) {
+          b = fmaxf(b, fminf(a, key[j * N + i]));
+          a = fmaxf(a, key[j * N + i]);
+        }
+        for (int o = 1; o < segment; o <<= 1) {
+          const float a2 = __shfl_xor_sync(full, a, o), b2 = __shfl_xor_sync(full, b, o);
+          b = fmaxf(fmaxf(b, b2), fminf(a, a2));
+          a = fmaxf(a, a2);
+        }
+        w[j] = worth_of(a, b);
+        rank[j] = 0;
+      }
+      const int per_chunk = L / segment, mine = gl / segment;
+#pragma unroll
+      for (int jo = 0; jo < CH; ++jo)
+        for (int o = 0; o < per_chunk; ++o) {
+          if (jo * per_chunk + o >= p.n_groups) break;
+          const float v = __shfl_sync(full, w[jo], r * L + o * segment);
+#pragma unroll
+          for (int j = 0; j < CH; ++j) rank[j] += v > w[j] || (v == w[j] && jo * per_chunk + o < j * per_chunk + mine);
+        }
+#pragma unroll
+      for (int j = 0; j < CH; ++j) {
+        if (!(w[j] > kClosed)) continue;   // (no open expert, or no group at all)
+        if (rank[j] < p.group_k) keep = fminf(keep, w[j]);
+        else drop = fmaxf(drop, w[j]);
+      }
+#pragma unroll
+      for (int o = L / 2; o > 0; o >>= 1) {
+        keep = fminf(keep, __shfl_xor_sync(full, keep, o));
+        drop = fmaxf(drop, __shfl_xor_sync(full, drop, o));
+      }
+      if (!exact_worth && drop > kClosed) near |= worth_near(keep, drop);
+#pragma unroll
+      for (int j = 0; j < CH; ++j)
+#pragma unroll
+        for (int i = 0; i < N; ++i)
+          if (rank[j] >= p.group_k) key[j * N + i] = kClosed;
+    } else if (p.n_groups > 1) {
       __syncwarp();
 #pragma unroll
       for (int c = 0; c < C; ++c) {
@@ -240,25 +299,17 @@ __global__ void __launch_bounds__(ROUTE_THREADS) route_kernel(const RouteParams 
           b = fmaxf(fmaxf(b, b2), fminf(a, a2));
           a = fmaxf(a, a2);
         }
-        if (g < p.n_groups && gl % per_group == 0) {
-          if (p.group_best == 2 && a > kClosed) {
-            const float second = b > kClosed ? (p.bias ? b : raw(b, top)) : 0.f;
-            a = (p.bias ? a : raw(a, top)) + second;
-          }
-          worth[g] = a;
-        }
+        if (g < p.n_groups && gl % per_group == 0) worth[g] = worth_of(a, b);
       }
       __syncwarp();
       // one flag per group, in place of the keys
-      const bool exact = !p.bias && p.group_best == 1;
       for (int g = gl; g < p.n_groups; g += L) {
         const float w = worth[g];
         int rank = 0;
         for (int o = 0; o < p.n_groups; ++o) {
           const float v = worth[o];
           rank += v > w || (v == w && o < g);
-          // a worth with a bias: two scores of at most inv each, whose slack (x e^-x / 8) is below 5 %; without: sums of e^-x with x < 104
-          if (!exact && o != g && v > kClosed && w > kClosed) near |= v >= w && route_near(v, w, p.bias ? 2.2f * inv : 14.f * v, p.bias ? 2.2f * inv : 14.f * w);
+          if (!exact_worth && o != g && v > kClosed && w > kClosed) near |= v >= w && worth_near(v, w);
         }
         keys[g] = rank < p.group_k ? 1.f : 0.f;
       }
@@ -272,29 +323,60 @@ __global__ void __launch_bounds__(ROUTE_THREADS) route_kernel(const RouteParams 
     __syncwarp();   // the last row's choices have been read
     // the choice, one more than asked for where its border has to be looked at
     if constexpr (L == 32) {
-      // keys as numbers, so that a warp's maximum is one instruction; a lane looks again at its keys only when one of them went
+      // Keys as numbers, so that a warp's maximum is one instruction.  The `rounds` largest of the lanes' own largest keys bound the choice from
+      // below; the keys from there on, few more than asked for, are ranked against one another, a lane each.
       unsigned k[C], best = 0;
-      int at = 0;
 #pragma unroll
       for (int c = 0; c < C; ++c) {
         k[c] = key[c] > kClosed ? route_order(key[c]) : 0u;
-        if (k[c] > best) { best = k[c]; at = expert(c); }
+        best = best > k[c] ? best : k[c];
       }
-      for (int j = 0; j < rounds; ++j) {
-        const unsigned m = __reduce_max_sync(full, best);
-        const int e = (int)__reduce_min_sync(full, best == m ? (unsigned)at : (unsigned)ROUTE_MAX_EXPERTS);
-        if (lane == 0) { at_s[j] = m ? e : -1; key_s[j] = m ? route_unorder(m) : kClosed; }
-        if (best == m && at == e) {
-          best = 0;
+      unsigned least = 0, m = best;
+      for (int j = 0; j < rounds;) {
+        const unsigned top_m = __reduce_max_sync(full, m);
+        if (top_m == 0) break;
+        least = top_m;
+        j += __popc(__ballot_sync(full, m == top_m));
+        if (m == top_m) m = 0;
+        if (j < rounds) least = 1;   // (fewer lanes with an open key than rounds: every open key)
+      }
+      int total = 0;
 #pragma unroll
-          for (int c = 0; c < C; ++c) {
-            if (expert(c) == e) k[c] = 0u;
-          }
+      for (int c = 0; c < C; ++c) {
+        const bool in = k[c] >= least && k[c] != 0;
+        const unsigned who = __ballot_sync(full, in);
+        const int pos = total + __popc(who & ((1u << lane) - 1u));
+        if (in && pos < 32) { at_s[rounds + pos] = expert(c); order_s[pos] = k[c]; }
+        total += __popc(who);
+      }
+      __syncwarp();
+      if (total <= 32) {
+        const unsigned mine = lane < total ? order_s[lane] : 0u;
+        const int e = lane < total ? at_s[rounds + lane] : 0;
+        int rank = 0;
+        for (int q = 0; q < total; ++q) {
+          const unsigned o = order_s[q];
+          rank += o > mine || (o == mine && at_s[rounds + q] < e);
+        }
+        if (lane < total && rank < rounds) { at_s[rank] = e; key_s[rank] = route_unorder(mine); }
+        if (lane >= total && lane < rounds) { at_s[lane] = -1; key_s[lane] = kClosed; }
+        if (lane + 32 < rounds) { at_s[lane + 32] = -1; key_s[lane + 32] = kClosed; }
+        __syncwarp();
+      } else {   // many equal keys: one after the other
+        for (int j = 0; j < rounds; ++j) {
+          unsigned most = 0;
+          int at = ROUTE_MAX_EXPERTS;
 #pragma unroll
           for (int c = 0; c < C; ++c)
-            if (k[c] > best) { best = k[c]; at = expert(c); }
+            if (k[c] > most) { most = k[c]; at = expert(c); }
+          const unsigned of_all = __reduce_max_sync(full, most);
+          const int e = (int)__reduce_min_sync(full, most == of_all ? (unsigned)at : (unsigned)ROUTE_MAX_EXPERTS);
+          if (lane == 0) { at_s[j] = of_all ? e : -1; key_s[j] = of_all ? route_unorder(of_all) : kClosed; }
+#pragma unroll
+          for (int c = 0; c < C; ++c)
+            if (expert(c) == e) k[c] = 0u;
+          __syncwarp();
         }
-        __syncwarp();
       }
     } else {
       for (int j = 0; j < rounds; ++j) {
@@ -337,13 +419,13 @@ __global__ void __launch_bounds__(ROUTE_THREADS) route_kernel(const RouteParams 
       bool close = false;
       if (i < R * rounds) {
         float sum = 0.f;
-        for (int q = 0; q < p.k; ++q) sum += score_s[rr * rounds + q];
+        if (p.renorm)
+          for (int q = 0; q < p.k; ++q) sum += score_s[rr * rounds + q];
         const float w = score_s[i], key_i = key_s[i];
         if (p.bias && j > 0 && at_s[i] >= 0) {
-          // (-ln of a score is at least the distance of its logit from the top: the sum is 1 or more)
+          // (-ln of a score is at least its exponent: a softmax divides by 1 or more, a sigmoid by 1 + e^-x)
           const float before = score_s[i - 1];
-          close = route_near(key_s[i - 1], key_i, p.sigmoid ? before : route_slack(before, __logf(fmaxf(before, 1e-38f))),
-                             p.sigmoid ? w : route_slack(w, __logf(fmaxf(w, 1e-38f))));
+          close = route_near(key_s[i - 1], key_i, route_slack(before, __logf(fmaxf(before, 1e-38f))), route_slack(w, __logf(fmaxf(w, 1e-38f))));
         }
         if (j < p.k && row0 + rr < p.n) {
           const int64_t to = (row0 + rr) * p.k + j;
@@ -397,18 +479,18 @@ __global__ void __launch_bounds__(ROUTE_THREADS) route_thread_kernel(const Route
     for (int c = 1; c < C; ++c) top = fmaxf(top, key[c]);
     if (!(top > kClosed)) top = 0.f;
     auto raw = [&](float l) { return p.sigmoid ? 1.f / (1.f + expf(-l)) : expf(l - top); };
+    auto rough = [&](float l) { return p.sigmoid ? __fdividef(1.f, 1.f + it_exp(-l)) : it_exp(l - top); };   // what keys are made of
     if (p.bias || p.need_sum) {
       float sum = 0.f;
 #pragma unroll
       for (int c = 0; c < C; ++c) {
-        const float s = raw(key[c]);
-        sum += s;
+        sum += p.bias ? rough(key[c]) : raw(key[c]);
       }
       if (!p.sigmoid) inv = sum > 0.f ? 1.f / sum : 0.f;
       if (p.bias) {
 #pragma unroll
         for (int c = 0; c < C; ++c)
-          if (c < E) key[c] = key[c] > kClosed ? open_key(fmaf(raw(key[c]), inv, __ldg(p.bias + c))) : kClosed;
+          if (c < E) key[c] = key[c] > kClosed ? open_key(fmaf(rough(key[c]), inv, __ldg(p.bias + c))) : kClosed;
       }
     }
     float best[KL];
@@ -434,12 +516,12 @@ __global__ void __launch_bounds__(ROUTE_THREADS) route_thread_kernel(const Route
       if (at[j] >= 0) {
         const float l = p.bias ? open_logit(to_f32(from[at[j]])) : best[j];
         w[j] = raw(l) * inv;
-        slack = p.sigmoid ? w[j] : route_slack(w[j], l - top);
+        slack = route_slack(w[j], p.sigmoid ? fminf(l, 0.f) : l - top);
       }
       if (j < p.k) sum += w[j];
       if (p.bias && j > 0 && j <= p.k && at[j] >= 0) {
         const float l = open_logit(to_f32(from[at[j - 1]]));
-        near |= route_near(best[j - 1], best[j], p.sigmoid ? w[j - 1] : route_slack(w[j - 1], l - top), slack);
+        near |= route_near(best[j - 1], best[j], route_slack(w[j - 1], p.sigmoid ? fminf(l, 0.f) : l - top), slack);
       }
     }
     const float f = p.renorm ? (sum > 0.f ? p.scale / sum : 0.f) : p.scale;
@@ -477,7 +559,7 @@ template <typename T, int L, int C>
 it_status launch(const RouteParams &p, double bytes, double flops, cudaStream_t st) {
   constexpr int R = 32 / L;
   const size_t warp64 = (size_t)(p.experts + p.n_groups) * 8;
-  const size_t warp32 = ((size_t)R * 3 * (p.k + 1) + (p.n_groups > 1 ? (size_t)R * (p.experts + p.experts / 32 + 1 + p.n_groups) : 0)) * 4;
+  const size_t warp32 = ((size_t)R * 3 * (p.k + 1) + (L == 32 ? 64 : 0) + (p.n_groups > 1 ? (size_t)R * (p.experts + p.experts / 32 + 1 + p.n_groups) : 0)) * 4;
   return launch_route(route_kernel<T, L, C>, p, ROUTE_WARPS * R, ROUTE_WARPS * (warp64 + warp32), bytes, flops, st);
 }
 

@@ -107,3 +107,26 @@ def test_structures_match_the_header():
             nums = [int(t) for t in subprocess.check_output([exe]).split()]
         assert nums == [C.sizeof(s)] + [getattr(s, f).offset for f in fields]
     assert re.search(r"IT_E4M3 = 2", open(os.path.join(root, "include", "inferturbo.h")).read())
+
+
+def test_binding_refuses_tensors_that_the_library_could_not_tell():
+    """Wrong types, shapes and places of tensors, which are addresses only to the library."""
+    import torch
+    with pytest.raises(ValueError, match="current CUDA device"):
+        B.NormDesc(dim=8, feat_dtype=torch.float32, weight=torch.ones(8))
+    with pytest.raises(ValueError, match="expected"):
+        B.NormDesc(dim=8, feat_dtype=torch.float32, weight=torch.ones(9))
+    with pytest.raises(TypeError):
+        B.NormDesc(dim=8, feat_dtype=torch.float16)
+    d = B.NormDesc(dim=8, feat_dtype=torch.float32)
+    with pytest.raises(ValueError, match="current CUDA device"):
+        B.it_residual_norm(d, torch.ones(2, 8), torch.ones(2, 8))
+    with pytest.raises(ValueError, match="expected"):
+        B.it_residual_norm(d, torch.ones(2, 8, dtype=torch.bfloat16), torch.ones(2, 8))
+    r = B.RouteDesc(n_experts=4, top_k=2, logit_dtype=torch.float32)
+    with pytest.raises(ValueError, match="current CUDA device"):
+        B.it_route(r, torch.ones(2, 4), torch.zeros(2, 2, dtype=torch.int32), torch.ones(2, 2))
+    with pytest.raises(KeyError):
+        B.RouteDesc(n_experts=4, top_k=2, logit_dtype=torch.float32, score="tanh")
+    with pytest.raises(ValueError, match="current CUDA device"):
+        B.ExpertsDesc(n_experts=2, top_k=1, in_dim=8, out_dim=8, feat_dtype=torch.float32, W1=torch.ones(2, 8, 8))
