@@ -309,7 +309,7 @@ it_status plan(const it_experts_desc *d, int64_t n, ExpertsWs *w) {
     w->off_position = take((size_t)places * 4);
     w->off_tiles = take(((size_t)w->tiles_max + 1) * 4);
     w->off_counts = take(it_experts_count_words(places, d->n_experts) * 4);
-    w->off_hidden = take(d->hidden_dim > 0 ? rows * cols * (f32 ? 6 : 2) : 0);
+    w->off_hidden = take(d->hidden_dim > 0 && !it_experts_fused(*d) ? rows * cols * (f32 ? 6 : 2) : 0);
     w->off_sums = take(d->top_k > 1 ? rows * (size_t)d->out_dim * 4 : 0);
     w->off_x = take(f32 ? (size_t)n * d->in_dim * 6 : 0);
     w->off_w1 = take(f32 ? E * d->in_dim * n1 * 6 : 0);
@@ -341,6 +341,10 @@ it_status many_places(const it_experts_args &a, const ExpertsWs &w, char *ws, ui
   }
   const it_expert_store last = d.top_k > 1 ? IT_EXPERT_SUMS : (f32 ? IT_EXPERT_OUT_F32 : IT_EXPERT_OUT_BF16);
   void *result = d.top_k > 1 ? (void *)(ws + w.off_sums) : a.out;
+  if (it_experts_fused(d)) {
+    IT_TRY(it_launch_experts_fused(a, q, result, spin_limit, no_loads, st));
+    return d.top_k > 1 ? launch_combine(a, (const float *)result, q.position, st) : IT_OK;
+  }
   it_expert_gemm g{};
   g.parts = f32 ? 3 : 1; g.spin_limit = spin_limit; g.no_loads = no_loads;
   g.A = x; g.gather = 1; g.a_rows = a.n; g.W = W1; g.K = d.in_dim; g.w_cols = a.n1; g.cols = two ? d.hidden_dim : d.out_dim;

@@ -60,6 +60,11 @@ struct it_expert_gemm {
 };
 it_status it_launch_expert_gemm(const it_experts_args &a, const it_experts_plan &q, const it_expert_gemm &g, cudaStream_t st);
 
+// ----------------------------------------------------------------------------- experts_fused.cu
+// Both products in one kernel, the hidden row never in memory; dst: fp32 rows by position (top_k > 1), or the output.
+bool it_experts_fused(const it_experts_desc &d);
+it_status it_launch_experts_fused(const it_experts_args &a, const it_experts_plan &q, void *dst, uint32_t spin_limit, int no_loads, cudaStream_t st);
+
 // ----------------------------------------------------------------------------- experts.cu
 // Activations of the experts, in fp32.
 #ifdef __CUDACC__

@@ -1,0 +1,533 @@
+// Both products of an expert in one kernel, for rows that fit an SM: a tile of 128 places keeps its input in shared memory and its result
+// in TMEM while the hidden columns go by, 128 at a time, so that the hidden row is neither written to nor read from device memory:
+//   S = X W1[:, chunk]  (TMEM)  ->  P = bf16( act( S + b1 ) )  (TMEM, where S lay)  ->  O += P W2[chunk, :]  (TMEM)
+// Gated: a chunk is 64 columns of the gate and the 64 that it gates.  With the hidden row in memory the two products of 1M vertices, 2 of 16,
+// 128-512-128, moved 6 GB, 4 of them hidden rows, and took 1160 us at 5.2 TB/s.
+//
+// Warps: 0 and 1 fetch rows of X by place (16-byte asynchronous copies, a tile ahead), 2 the weights (TMA, in the order of their use), 3 issues the
+// MMAs (S of chunk g + 1 before O of chunk g, so that the tensor core works while P is made), 4-11 make P, 12-15 store O: sixteen, which
+// leave 128 registers a thread.
+// S and P are buffered twice, O twice where it has at most 128 columns.
+// Waits are bounded as in the other products.
+#include <type_traits>
+
+#include "experts_tc.cuh"
+
+namespace {
+
+constexpr int FU_FETCH_WARPS = 2, FU_W_WARP = 2, FU_MMA_WARP = 3, FU_P_WARP0 = 4, FU_P_WARPS = 8, FU_O_WARP0 = 12, FU_O_WARPS = 4;
+constexpr int FU_THREADS = 32 * (FU_O_WARP0 + FU_O_WARPS);
+constexpr int FU_STAGE = 16384;      // of the weights: a k-block of 128 columns
+constexpr int FU_XBLOCK = TC_BM * TC_KBLOCK_BYTES;
+constexpr int FU_MAX_STAGES = 8;
+constexpr int FU_BACKOFF = 32;       // ns between polls
+constexpr int FU_S_COLS = 128;       // accumulator columns of a chunk
+
+struct FuParams {
+  const int32_t *order, *tile_expert, *n_tiles;
+  const void *x;
+  const float *x_scale, *w_scale, *b1, *b2, *weights;
+  int tiles_max, top_k, n_experts;
+  int in_bytes, kbx;                 // bytes of a row of X, its k-blocks
+  int hidden, n1, chunks, chunk_hidden;   // columns of W1; chunks of 128 (gated: 64) hidden columns
+  int out, bn, halves;               // columns of the result, padded to panels; parts of up to 128 of them
+  int x_slots, stages, o_bufs;
+  int act;
+  void *dst;
+  int *status;
+  uint32_t spin_limit;
+  int no_loads;
+};
+
+// The same product with the A operand in tensor memory (lane = row of the tile, two bf16 a column).
+__device__ __forceinline__ void fu_mma_tmem_a(uint32_t d_tmem, uint32_t a_tmem, uint64_t b_desc, uint32_t idesc, uint32_t accumulate) {
+  asm volatile(
+      "{\n\t.reg .pred p;\n\tsetp.ne.b32 p, %4, 0;\n\t"
+      "tcgen05.mma.cta_group::1.kind::f16 [%0], [%1], %2, %3, {%5, %5, %5, %5}, p;\n\t}"
+      ::"r"(d_tmem), "r"(a_tmem), "l"(b_desc), "r"(idesc), "r"(accumulate), "r"(0u)
+      : "memory");
+}
+
+template <bool EIGHT, bool GATED, bool DIRECT>
+__global__ void __launch_bounds__(FU_THREADS, 1)
+expert_fused_kernel(const __grid_constant__ CUtensorMap map_w1, const __grid_constant__ CUtensorMap map_w2, const FuParams p) {
+  extern __shared__ __align__(1024) unsigned char base[];
+  const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
+  constexpr int BK1 = EIGHT ? 128 : 64;              // elements of a k-block of X, and columns of a panel of W1
+  constexpr int STAGING = DIRECT ? 4096 : 2048;      // per storing warp: 32 rows of 128 or 64 bytes
+  unsigned char *x_s = base;
+  unsigned char *w_s = x_s + (size_t)p.x_slots * p.kbx * FU_XBLOCK;
+  unsigned char *staging = w_s + (size_t)p.stages * FU_STAGE;
+  float *p_consts = reinterpret_cast<float *>(staging + FU_O_WARPS * STAGING);   // [8 warps][2][64 bias | 64 scale]
+  float *o_consts = p_consts + FU_P_WARPS * 2 * (EIGHT ? 128 : 64);               // [4 warps][256] b2
+  int32_t *o_place = reinterpret_cast<int32_t *>(o_consts + FU_O_WARPS * 256);    // [128]
+  uint64_t *w_full = reinterpret_cast<uint64_t *>(o_place + TC_BM);
+  uint64_t *w_empty = w_full + FU_MAX_STAGES;
+  uint64_t *x_full = w_empty + FU_MAX_STAGES;   // [2]
+  uint64_t *x_empty = x_full + 2;               // [2]
+  uint64_t *s_full = x_empty + 2;               // [2]
+  uint64_t *p_full = s_full + 2;                // [2]
+  uint64_t *o_full = p_full + 2;                // [2]
+  uint64_t *o_empty = o_full + 2;               // [2]
+  uint64_t *mma_done = o_empty + 2;             // [1]
+  uint32_t *tmem_slot = reinterpret_cast<uint32_t *>(mma_done + 1);
+  volatile int *abort_flag = reinterpret_cast<volatile int *>(tmem_slot + 1);
+
+  if (threadIdx.x == 0) {
+    for (int s = 0; s < p.stages; ++s) {
+      mbar_init(&w_full[s], 1);
+      mbar_init(&w_empty[s], 1);
+    }
+    for (int a = 0; a < 2; ++a) {
+      mbar_init(&x_full[a], 32 * FU_FETCH_WARPS);
+      mbar_init(&x_empty[a], 1);
+      mbar_init(&s_full[a], 1);
+      mbar_init(&p_full[a], FU_P_WARPS);
+      mbar_init(&o_full[a], 1);
+      mbar_init(&o_empty[a], FU_O_WARPS);
+    }
+    mbar_init(mma_done, 1);
+    *abort_flag = 0;
+    asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");
+  }
+  if (warp == FU_MMA_WARP) {
+    tmem_alloc(tmem_slot, 512);
+    tmem_relinquish();
+  }
+  it_allow_next();
+  it_wait_prior();
+  tc_fence_before();
+  __syncthreads();
+  tc_fence_after();
+  const uint32_t tmem_base = *tmem_slot, s_col = (uint32_t)(p.o_bufs * p.bn);   // O first, then the two S
+  int m_tiles = *p.n_tiles;
+  m_tiles = m_tiles < p.tiles_max ? m_tiles : p.tiles_max;
+
+  if (warp < FU_FETCH_WARPS) {
+    // ------------------------------------------------------------------ rows of X, by place
+    constexpr int GROUPS = TC_BM / 32 / FU_FETCH_WARPS;   // of 32 rows a warp
+    const int chunk = lane & 7;
+    uint32_t slot = 0, phase = 0;
+    int place_next[GROUPS];
+    auto look = [&](int m) {
+#pragma unroll
+      for (int q = 0; q < GROUPS; ++q)
+        if (m < m_tiles) place_next[q] = p.order[(int64_t)m * TC_BM + (warp * GROUPS + q) * 32 + lane];
+    };
+    look(blockIdx.x);
+    for (int m = blockIdx.x; m < m_tiles && !p.no_loads; m += gridDim.x) {
+      int row[GROUPS];
+#pragma unroll
+      for (int q = 0; q < GROUPS; ++q) row[q] = place_next[q] < 0 ? -1 : place_next[q] / p.top_k;
+      look(m + gridDim.x);
+      const int ok = lane == 0 ? mbar_wait(&x_empty[slot], phase ^ 1u, abort_flag, p.spin_limit, FU_BACKOFF) : 1;
+      if (!__shfl_sync(0xffffffffu, ok, 0)) break;
+      const uint32_t to = smem_u32(x_s) + slot * (uint32_t)(p.kbx * FU_XBLOCK);
+#pragma unroll
+      for (int q = 0; q < GROUPS; ++q)
+#pragma unroll
+        for (int i = 0; i < 8; ++i) {
+          const int local = i * 4 + (lane >> 3), r = __shfl_sync(0xffffffffu, row[q], local), in_tile = (warp * GROUPS + q) * 32 + local;
+          const unsigned char *from = reinterpret_cast<const unsigned char *>(p.x) + (int64_t)(r < 0 ? 0 : r) * p.in_bytes;
+          const uint32_t dst = to + (uint32_t)in_tile * TC_KBLOCK_BYTES + (uint32_t)((chunk ^ (in_tile & 7)) << 4);
+          for (int kb = 0; kb < p.kbx; ++kb) {
+            const int at = kb * TC_KBLOCK_BYTES + chunk * 16;
+            const bool in = r >= 0 && at < p.in_bytes;
+            cp_async16(dst + (uint32_t)kb * FU_XBLOCK, in ? from + at : p.x, in ? 16u : 0u);
+          }
+        }
+      cp_async_arrive(&x_full[slot]);
+      if (++slot == (uint32_t)p.x_slots) { slot = 0; phase ^= 1u; }
+    }
+    __syncwarp();
+    cp_async_wait_all();
+  } else if (warp == FU_W_WARP) {
+    // ------------------------------------------------------------------ weights: W1 of a chunk, then W2 of the one before it
+    uint32_t stage = 0, phase = 0;
+    bool ok = !p.no_loads, came_round = false;
+    auto next_stage = [&](uint32_t bytes) {   // a free stage, armed
+      if (lane == 0) {
+        ok = mbar_wait(&w_empty[stage], phase ^ 1u, abort_flag, p.spin_limit, FU_BACKOFF);
+        if (ok) mbar_arrive_expect_tx(&w_full[stage], bytes);
+      }
+      ok = __shfl_sync(0xffffffffu, (int)ok, 0);
+      return ok;
+    };
+    auto advance = [&]() {
+      __syncwarp();
+      if (++stage == (uint32_t)p.stages) { stage = 0; phase ^= 1u; came_round = true; }
+    };
+    auto first = [&](int e, int c) {
+      for (int kb = 0; kb < p.kbx; ++kb) {
+        if (!next_stage(FU_STAGE)) return;
+        unsigned char *to = w_s + (size_t)stage * FU_STAGE;
+        if (lane < 128 / BK1) {
+          const int col = GATED ? lane * p.hidden + c * 64 : c * 128 + lane * BK1;
+          tma_load_3d(to + lane * BK1 * TC_KBLOCK_BYTES, &map_w1, col, kb * BK1, e, &w_full[stage]);
+        }
+        advance();
+      }
+    };
+    auto second = [&](int e, int c) {
+      for (int kb = 0; kb < p.chunk_hidden / 64; ++kb)
+        for (int h = 0; h < p.halves; ++h) {
+          const int cols = p.bn - 128 * h < 128 ? p.bn - 128 * h : 128;
+          if (!next_stage((uint32_t)cols * TC_KBLOCK_BYTES)) return;
+          unsigned char *to = w_s + (size_t)stage * FU_STAGE;
+          if (lane < cols / 64) tma_load_3d(to + lane * 64 * TC_KBLOCK_BYTES, &map_w2, 128 * h + lane * 64, c * p.chunk_hidden + kb * 64, e, &w_full[stage]);
+          advance();
+        }
+    };
+    int e_before = -1;
+    int e_next = (int)blockIdx.x < m_tiles ? p.tile_expert[blockIdx.x] : 0;
+    for (int m = blockIdx.x; m < m_tiles && ok; m += gridDim.x) {
+      const int e = e_next;
+      if (m + (int)gridDim.x < m_tiles) e_next = p.tile_expert[m + gridDim.x];
+      for (int c = 0; c < p.chunks && ok; ++c) {
+        first(e, c);
+        if (ok && (c > 0 || e_before >= 0)) second(c > 0 ? e : e_before, c > 0 ? c - 1 : p.chunks - 1);
+      }
+      e_before = e;
+    }
+    if (ok && e_before >= 0) second(e_before, p.chunks - 1);
+    __syncwarp();
+    if (lane == 0) ring_drain(w_full, (uint32_t)p.stages, stage, phase, came_round);
+  } else if (warp == FU_MMA_WARP) {
+    // ------------------------------------------------------------------ MMA issuer
+    if (lane == 0) {
+      const uint32_t fmt = EIGHT ? 0u : 1u;
+      const uint32_t idesc1 = (1u << 4) | (fmt << 7) | (fmt << 10) | (1u << 16) | ((uint32_t)(FU_S_COLS >> 3) << 17) | ((uint32_t)(TC_BM >> 4) << 24);
+      uint32_t stage = 0, phase = 0, slot = 0, x_phase = 0;
+      bool ok = true;
+      auto weights = [&]() {
+        ok = mbar_wait(&w_full[stage], phase, abort_flag, p.spin_limit);
+        tc_fence_after();
+        return ok;
+      };
+      auto advance = [&]() {
+        tc_commit(&w_empty[stage]);
+        if (++stage == (uint32_t)p.stages) { stage = 0; phase ^= 1u; }
+      };
+      // chunk number g of this CTA: its S and P buffer g % 2; tile number t: its O buffer t % o_bufs
+      auto issue_s = [&](uint32_t g, bool first_chunk, bool last_chunk) {
+        if (first_chunk) {
+          ok = mbar_wait(&x_full[slot], x_phase, abort_flag, p.spin_limit);
+          if (!ok) return;
+          asm volatile("fence.proxy.async.shared::cta;" ::: "memory");   // the rows were written by other threads' copies
+        }
+        // (P of chunk g - 2 lay where this S goes: its product was issued before)
+        const uint32_t d = tmem_base + s_col + (g & 1u) * FU_S_COLS, x0 = smem_u32(x_s) + slot * (uint32_t)(p.kbx * FU_XBLOCK);
+        for (int kb = 0; kb < p.kbx; ++kb) {
+          if (!weights()) return;
+          const uint32_t a_s = x0 + (uint32_t)kb * FU_XBLOCK, b_s = smem_u32(w_s) + stage * FU_STAGE;
+#pragma unroll
+          for (int k = 0; k < 4; ++k)
+            ex_mma<EIGHT>(d, make_desc(a_s + k * 32), make_desc_mn(b_s + k * (BK1 * TC_KBLOCK_BYTES / 4), BK1 * TC_KBLOCK_BYTES), idesc1, (kb | k) != 0);
+          advance();
+        }
+        tc_commit(&s_full[g & 1u]);
+        if (last_chunk) {
+          tc_commit(&x_empty[slot]);
+          if (++slot == (uint32_t)p.x_slots) { slot = 0; x_phase ^= 1u; }
+        }
+      };
+      auto issue_o = [&](uint32_t g, uint32_t t, bool first_chunk, bool last_chunk) {
+        ok = mbar_wait(&p_full[g & 1u], (g >> 1) & 1u, abort_flag, p.spin_limit);
+        if (!ok) return;
+        const uint32_t ob = p.o_bufs == 2 ? t & 1u : 0u, ot = p.o_bufs == 2 ? t >> 1 : t;
+        if (first_chunk) {
+          ok = mbar_wait(&o_empty[ob], (ot & 1u) ^ 1u, abort_flag, p.spin_limit);
+          if (!ok) return;
+        }
+        tc_fence_after();
+        const uint32_t pt = tmem_base + s_col + (g & 1u) * FU_S_COLS;
+        for (int kb = 0; kb < p.chunk_hidden / 64; ++kb)
+          for (int h = 0; h < p.halves; ++h) {
+            const int cols = p.bn - 128 * h < 128 ? p.bn - 128 * h : 128;
+            const uint32_t idesc2 = (1u << 4) | (1u << 7) | (1u << 10) | (1u << 16) | ((uint32_t)(cols >> 3) << 17) | ((uint32_t)(TC_BM >> 4) << 24);
+            if (!weights()) return;
+            const uint32_t b_s = smem_u32(w_s) + stage * FU_STAGE, d = tmem_base + ob * (uint32_t)p.bn + 128u * (uint32_t)h;
+#pragma unroll
+            for (int k = 0; k < 4; ++k) {
+              // where the warps that make P leave it: 32 columns of theirs hold 64 hidden columns, gated 16 hold 32
+              const uint32_t a = GATED ? pt + (k >> 1) * 32 + (k & 1) * 8 : pt + kb * 64 + k * 8;
+              fu_mma_tmem_a(d, a, make_desc_mn(b_s + k * 2048, 8192), idesc2, !first_chunk || (kb | k) != 0);
+            }
+            advance();
+          }
+        if (last_chunk) tc_commit(&o_full[ob]);
+      };
+      uint32_t g = 0, t = 0;
+      for (int m = blockIdx.x; m < m_tiles && ok; m += gridDim.x, ++t)
+        for (int c = 0; c < p.chunks && ok; ++c, ++g) {
+          issue_s(g, c == 0, c + 1 == p.chunks);
+          if (ok && g > 0) issue_o(g - 1, c > 0 ? t : t - 1, c > 0 ? c == 1 : p.chunks == 1, c == 0);
+        }
+      if (ok && g > 0) issue_o(g - 1, t - 1, p.chunks == 1, true);
+      tc_commit(mma_done);
+      mbar_drain(mma_done, 0);
+    }
+  } else if (warp < FU_P_WARP0 + FU_P_WARPS) {
+    // ------------------------------------------------------------------ P: a thread per row, 64 accumulator columns a warp (gated: 32 of the gate, 32 gated)
+    const int quarter = warp & 3, sub = (warp - FU_P_WARP0) >> 2;   // a warp may only touch TMEM lanes [32 * (warp % 4), +32)
+    float *consts = p_consts + (warp - FU_P_WARP0) * 2 * (EIGHT ? 128 : 64);
+    // two constants a lane, those of the columns 2 lane and 2 lane + 1 (gated: of column lane of either half), fetched a chunk ahead
+    struct Two { float2 b, s; };
+    auto fetch = [&](int e, int c) {
+      Two q{make_float2(0.f, 0.f), make_float2(1.f, 1.f)};
+      const int64_t row = (int64_t)e * p.n1;
+      if constexpr (GATED) {
+        const int h = c * 64 + sub * 32 + lane;
+        if (h < p.hidden && p.b1) q.b = make_float2(p.b1[row + h], p.b1[row + p.hidden + h]);
+      } else {
+        const int h = c * 128 + sub * 64 + lane * 2;
+        if (h < p.hidden) {   // (hidden is a multiple of 8)
+          if (p.b1) q.b = *reinterpret_cast<const float2 *>(p.b1 + row + h);
+          if constexpr (EIGHT) q.s = *reinterpret_cast<const float2 *>(p.w_scale + row + h);
+        }
+      }
+      return q;
+    };
+    const uint32_t floor2 = p.act == IT_ACT_RELU ? 0u : 0xff80ff80u;
+    uint32_t g = 0;
+    bool ok = true;
+    int e_next = (int)blockIdx.x < m_tiles ? p.tile_expert[blockIdx.x] : 0;
+    int place_next = EIGHT && (int)blockIdx.x < m_tiles ? p.order[(int64_t)blockIdx.x * TC_BM + quarter * 32 + lane] : -1;
+    float xs_next = EIGHT && place_next >= 0 ? p.x_scale[place_next / p.top_k] : 1.f;
+    Two next{};
+    if ((int)blockIdx.x < m_tiles) next = fetch(e_next, 0);
+    for (int m = blockIdx.x; m < m_tiles && ok; m += gridDim.x) {
+      const int e = e_next, after = m + gridDim.x;
+      const uint32_t xw = __float_as_uint(xs_next);
+      const uint64_t xs2 = pack2(xw, xw);
+      if (after < m_tiles) {
+        e_next = p.tile_expert[after];
+        if constexpr (EIGHT) place_next = p.order[(int64_t)after * TC_BM + quarter * 32 + lane];
+      }
+      for (int c = 0; c < p.chunks; ++c, ++g) {
+        float *k = consts + (g & 1u) * (EIGHT ? 128 : 64);
+        __syncwarp();
+        if constexpr (GATED) { k[lane] = next.b.x; k[32 + lane] = next.b.y; }
+        else {
+          *reinterpret_cast<float2 *>(k + 2 * lane) = next.b;
+          if constexpr (EIGHT) *reinterpret_cast<float2 *>(k + 64 + 2 * lane) = next.s;
+        }
+        __syncwarp();
+        if (c + 1 < p.chunks) next = fetch(e, c + 1);
+        else if (after < m_tiles) {
+          next = fetch(e_next, 0);
+          if constexpr (EIGHT) xs_next = place_next >= 0 ? p.x_scale[place_next / p.top_k] : 1.f;
+        }
+        ok = mbar_wait(&s_full[g & 1u], (g >> 1) & 1u, abort_flag, p.spin_limit);
+        ok = __all_sync(0xffffffffu, ok);
+        if (!ok) break;
+        tc_fence_after();
+        const uint32_t st = tmem_base + ((uint32_t)(quarter * 32) << 16) + s_col + (g & 1u) * FU_S_COLS;
+        // 32 columns of S, scaled, with their bias
+        auto scaled = [&](const uint32_t (&r)[32], int at, uint64_t (&v)[16]) {
+          const ulonglong2 *b = reinterpret_cast<const ulonglong2 *>(k + at);
+#pragma unroll
+          for (int i = 0; i < 8; ++i) {
+            const ulonglong2 bb = b[i];
+            uint64_t lo = pack2(r[4 * i], r[4 * i + 1]), hi = pack2(r[4 * i + 2], r[4 * i + 3]);
+            if constexpr (EIGHT) {
+              const ulonglong2 f = reinterpret_cast<const ulonglong2 *>(k + 64 + at)[i];
+              lo = fma2(mul2(lo, xs2), f.x, bb.x);
+              hi = fma2(mul2(hi, xs2), f.y, bb.y);
+            } else {
+              lo = add2(lo, bb.x);
+              hi = add2(hi, bb.y);
+            }
+            v[2 * i] = lo;
+            v[2 * i + 1] = hi;
+          }
+        };
+        auto pack = [&](const uint64_t (&v)[16], uint32_t (&w)[16], bool cut) {
+#pragma unroll
+          for (int i = 0; i < 16; ++i) {
+            const float2 f = unpack2(v[i]);
+            w[i] = bf16x2_of(f.x, f.y);
+            if (cut) w[i] = max_bf16x2(w[i], floor2);
+          }
+        };
+        if constexpr (GATED) {
+          uint32_t r[32], u[32], w[16];
+          tmem_ld32(st + (uint32_t)(sub * 32), r);
+          tmem_ld32(st + 64u + (uint32_t)(sub * 32), u);
+          tmem_ld_wait();
+          uint64_t v[16], q[16];
+          scaled(r, 0, v);
+          expert_act(v, p.act);
+          scaled(u, 32, q);
+#pragma unroll
+          for (int i = 0; i < 16; ++i) v[i] = mul2(v[i], q[i]);
+          pack(v, w, false);
+          tmem_st16(st + (uint32_t)(sub * 32), w);
+        } else {
+          uint32_t r[32], w[16];
+          uint64_t v[16];
+          tmem_ld32(st + (uint32_t)(sub * 64), r);
+          tmem_ld_wait();
+          scaled(r, 0, v);
+          tmem_ld32(st + (uint32_t)(sub * 64 + 32), r);   // (all 64 are read before P takes the place of the first 32)
+          if (p.act != IT_ACT_RELU) expert_act(v, p.act);
+          pack(v, w, true);
+          tmem_ld_wait();
+          tmem_st16(st + (uint32_t)(sub * 64), w);
+          scaled(r, 32, v);
+          if (p.act != IT_ACT_RELU) expert_act(v, p.act);
+          pack(v, w, true);
+          tmem_st16(st + (uint32_t)(sub * 64 + 16), w);
+        }
+        tmem_st_wait();
+        tc_fence_before();
+        __syncwarp();
+        if (lane == 0) mbar_arrive(&p_full[g & 1u]);
+      }
+    }
+  } else {
+    // ------------------------------------------------------------------ O: rows of the result, through a staging tile
+    const int quarter = warp & 3;
+    constexpr int ESIZE = DIRECT ? 2 : 4, ROW = DIRECT ? 128 : 64, PIECES = ROW / 16, AT_ONCE = 32 / PIECES;
+    const uint32_t stage_s = smem_u32(staging) + (uint32_t)(warp - FU_O_WARP0) * STAGING;
+    const int row0 = lane / PIECES, piece = lane % PIECES;
+    const uint32_t put = stage_s + (uint32_t)lane * ROW + (uint32_t)((DIRECT ? lane & 7 : (lane >> 1) & 3) << 4);
+    float *bias = o_consts + (warp - FU_O_WARP0) * 256;
+    int32_t *places = o_place + quarter * 32;
+    uint32_t t = 0;
+    for (int m = blockIdx.x; m < m_tiles; m += gridDim.x, ++t) {
+      const int64_t pos0 = (int64_t)m * TC_BM + quarter * 32;
+      const int place = p.order[pos0 + lane], e = p.tile_expert[m];
+      const float weight = DIRECT && place >= 0 ? p.weights[place] : 1.f;
+      const uint64_t weight2 = pack2(__float_as_uint(weight), __float_as_uint(weight));
+      __syncwarp();
+      places[lane] = place;
+#pragma unroll
+      for (int i = 0; i < 2; ++i) {
+        const int c = i * 128 + lane * 4;
+        *reinterpret_cast<float4 *>(bias + c) = p.b2 && c < p.out ? *reinterpret_cast<const float4 *>(p.b2 + (int64_t)e * p.out + c) : make_float4(0.f, 0.f, 0.f, 0.f);
+      }
+      __syncwarp();
+      const uint32_t ob = p.o_bufs == 2 ? t & 1u : 0u, ot = p.o_bufs == 2 ? t >> 1 : t;
+      const bool ok = mbar_wait(&o_full[ob], ot & 1u, abort_flag, p.spin_limit, 4 * FU_BACKOFF);
+      if (!__all_sync(0xffffffffu, ok)) break;
+      tc_fence_after();
+      const uint32_t taddr = tmem_base + ((uint32_t)(quarter * 32) << 16) + ob * (uint32_t)p.bn;
+      auto flush = [&](int c, bool both) {   // the staged pieces of rows, from column c on
+        __syncwarp();
+        const bool in = c + piece * (16 / ESIZE) < p.out && (!DIRECT || both || piece < 4);
+#pragma unroll
+        for (int i = 0; i < 32 / AT_ONCE; ++i) {
+          const int row = AT_ONCE * i + row0, at = places[row];
+          uint4 d;
+          asm volatile("ld.shared.v4.b32 {%0, %1, %2, %3}, [%4];" : "=r"(d.x), "=r"(d.y), "=r"(d.z), "=r"(d.w)
+                       : "r"(stage_s + (uint32_t)row * ROW + (uint32_t)((piece ^ (DIRECT ? row & 7 : (row >> 1) & 3)) << 4)) : "memory");
+          if (in && at >= 0)
+            *reinterpret_cast<uint4 *>(reinterpret_cast<unsigned char *>(p.dst) + ((DIRECT ? (int64_t)at : pos0 + row) * p.out + c) * ESIZE + piece * 16) = d;
+        }
+        __syncwarp();
+      };
+      for (int c = 0; c < p.out; c += 32) {
+        uint32_t r[32];
+        tmem_ld32(taddr + (uint32_t)c, r);
+        tmem_ld_wait();
+        const ulonglong2 *b = reinterpret_cast<const ulonglong2 *>(bias + c);
+        uint64_t v[16];
+#pragma unroll
+        for (int i = 0; i < 8; ++i) {
+          const ulonglong2 bb = b[i];
+          v[2 * i] = add2(pack2(r[4 * i], r[4 * i + 1]), bb.x);
+          v[2 * i + 1] = add2(pack2(r[4 * i + 2], r[4 * i + 3]), bb.y);
+        }
+        if constexpr (DIRECT) {
+          uint32_t w[16];
+#pragma unroll
+          for (int i = 0; i < 16; ++i) {
+            const float2 f = unpack2(mul2(v[i], weight2));
+            w[i] = bf16x2_of(f.x, f.y);
+          }
+          const int half = (c >> 5) & 1;
+#pragma unroll
+          for (int i = 0; i < 4; ++i) st_shared_v4(put ^ (16u * (4 * half + i)), w[4 * i], w[4 * i + 1], w[4 * i + 2], w[4 * i + 3]);
+          if (half == 1 || c + 32 >= p.out) flush(c - 32 * half, half == 1);
+        } else {
+#pragma unroll
+          for (int h = 0; h < 2; ++h) {
+            if (c + 16 * h >= p.out) break;
+#pragma unroll
+            for (int i = 0; i < 4; ++i) {
+              const float2 f0 = unpack2(v[8 * h + 2 * i]), f1 = unpack2(v[8 * h + 2 * i + 1]);
+              st_shared_v4(put ^ (16u * i), __float_as_uint(f0.x), __float_as_uint(f0.y), __float_as_uint(f1.x), __float_as_uint(f1.y));
+            }
+            flush(c + 16 * h, false);
+          }
+        }
+      }
+      tc_fence_before();
+      __syncwarp();
+      if (lane == 0) mbar_arrive(&o_empty[ob]);
+    }
+  }
+
+  // ------------------------------------------------------------------ teardown
+  __syncwarp();
+  tc_fence_before();
+  __syncthreads();
+  if (threadIdx.x == 0 && *abort_flag) atomicExch(p.status, 1);
+  if (warp == FU_MMA_WARP) {
+    tc_fence_after();
+    tmem_dealloc(tmem_base, 512);
+  }
+}
+
+template <bool EIGHT, bool GATED, bool DIRECT>
+it_status launch(const CUtensorMap &m1, const CUtensorMap &m2, const FuParams &p, int grid, int smem, double bytes, double flops, cudaStream_t st) {
+  IT_CUDA_TRY(cudaFuncSetAttribute(expert_fused_kernel<EIGHT, GATED, DIRECT>, cudaFuncAttributeMaxDynamicSharedMemorySize, smem));
+  IT_LAUNCH(IT_K_EXPERT_GEMM, bytes, flops, st,
+            IT_CUDA_TRY((it_launch_pdl(expert_fused_kernel<EIGHT, GATED, DIRECT>, dim3((unsigned)grid), dim3(FU_THREADS), smem, st, m1, m2, p))));
+  return IT_OK;
+}
+
+}  // namespace
+
+// Rows of X of up to 512 bytes (a tile of them fits shared memory twice beside the weights' stages), results of up to 256 columns (that
+// fit TMEM beside the two chunks); not gated in 8 bits, whose panels of 128 columns do not divide into gate and gated.
+bool it_experts_fused(const it_experts_desc &d) {
+  const int in_bytes = d.in_dim * (d.in_dtype == IT_E4M3 ? 1 : 2);
+  return d.hidden_dim > 0 && d.feat_dtype == IT_BF16 && in_bytes <= 512 && d.out_dim <= 256 && !(d.gated && d.in_dtype == IT_E4M3);
+}
+
+it_status it_launch_experts_fused(const it_experts_args &a, const it_experts_plan &q, void *dst, uint32_t spin_limit, int no_loads, cudaStream_t st) {
+  const it_experts_desc &d = a.d;
+  const bool eight = d.in_dtype == IT_E4M3, gated = d.gated != 0, direct = d.top_k == 1;
+  const int elem = eight ? 1 : 2, BK = TC_KBLOCK_BYTES / elem;
+  FuParams p{};
+  p.order = q.order; p.tile_expert = q.tile_expert; p.n_tiles = q.n_tiles; p.tiles_max = (int)q.tiles_max;
+  p.x = a.x; p.x_scale = a.x_scale; p.w_scale = d.w1_scale; p.b1 = d.b1; p.b2 = d.b2; p.weights = a.weights;
+  p.top_k = d.top_k; p.n_experts = d.n_experts; p.in_bytes = d.in_dim * elem; p.kbx = (d.in_dim + BK - 1) / BK;
+  p.hidden = d.hidden_dim; p.n1 = a.n1; p.chunk_hidden = gated ? 64 : 128; p.chunks = (d.hidden_dim + p.chunk_hidden - 1) / p.chunk_hidden;
+  p.out = d.out_dim; p.bn = (d.out_dim + 63) / 64 * 64; p.halves = p.bn > 128 ? 2 : 1; p.o_bufs = p.bn <= 128 ? 2 : 1;
+  p.act = d.act; p.dst = dst; p.status = a.status; p.spin_limit = spin_limit ? spin_limit : TC_SPIN_LIMIT; p.no_loads = no_loads;
+
+  const cuuint64_t d1[3] = {(cuuint64_t)a.n1, (cuuint64_t)d.in_dim, (cuuint64_t)d.n_experts}, s1[2] = {(cuuint64_t)a.n1 * elem, (cuuint64_t)a.n1 * elem * (cuuint64_t)d.in_dim};
+  const cuuint64_t d2[3] = {(cuuint64_t)d.out_dim, (cuuint64_t)d.hidden_dim, (cuuint64_t)d.n_experts}, s2[2] = {(cuuint64_t)d.out_dim * 2, (cuuint64_t)d.out_dim * 2 * (cuuint64_t)d.hidden_dim};
+  const cuuint32_t b1[3] = {(cuuint32_t)BK, (cuuint32_t)BK, 1}, b2[3] = {64, 64, 1};
+  CUtensorMap m1, m2;
+  IT_TRY(encode(&m1, eight, d.W1, 3, d1, s1, b1));
+  IT_TRY(encode(&m2, false, d.W2, 3, d2, s2, b2));
+
+  const int fixed = FU_O_WARPS * (direct ? 4096 : 2048) + FU_P_WARPS * 2 * (eight ? 128 : 64) * 4 + FU_O_WARPS * 256 * 4 + TC_BM * 4 + (2 * FU_MAX_STAGES + 14) * 8;
+  p.x_slots = 2;
+  p.stages = (227 * 1024 - fixed - p.x_slots * p.kbx * FU_XBLOCK) / FU_STAGE;
+  if (p.stages > FU_MAX_STAGES) p.stages = FU_MAX_STAGES;
+  const int smem = fixed + p.x_slots * p.kbx * FU_XBLOCK + p.stages * FU_STAGE;
+  const int grid = (int)(q.tiles_max < a.sms ? q.tiles_max : a.sms);
+  const double places = (double)a.n * d.top_k;
+  const double flops = 2.0 * places * ((double)d.in_dim * a.n1 + (double)d.hidden_dim * d.out_dim), bytes = places * (p.in_bytes + (double)d.out_dim * (direct ? 2 : 4));
+#define IT_FU_LAUNCH(EIGHT, GATED, DIRECT) return launch<EIGHT, GATED, DIRECT>(m1, m2, p, grid, smem, bytes, flops, st)
+  if (eight) { if (direct) IT_FU_LAUNCH(true, false, true); else IT_FU_LAUNCH(true, false, false); }
+  if (gated) { if (direct) IT_FU_LAUNCH(false, true, true); else IT_FU_LAUNCH(false, true, false); }
+  if (direct) IT_FU_LAUNCH(false, false, true);
+  IT_FU_LAUNCH(false, false, false);
+#undef IT_FU_LAUNCH
+}

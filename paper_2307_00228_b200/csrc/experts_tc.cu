@@ -11,8 +11,7 @@
 // flight, frees its TMEM and returns, and a status word in global memory is set.
 #include <type_traits>
 
-#include "experts.cuh"
-#include "tc.cuh"
+#include "experts_tc.cuh"
 
 namespace {
 
@@ -31,98 +30,6 @@ struct ExMeta { int32_t place[TC_BM]; float weight[TC_BM]; float bias[256]; };
 struct ExMetaEight : ExMeta { float xs[TC_BM]; float scale[256]; };
 constexpr int EX_MAX_STAGES = 8;
 constexpr int EX_EPI_BACKOFF = 64, EX_TMA_BACKOFF = 32;   // ns between polls
-
-// 16 bytes of a row into shared memory, asynchronously; `bytes` 0: zeros.
-__device__ __forceinline__ void cp_async16(uint32_t dst, const void *src, uint32_t bytes) {
-  asm volatile("cp.async.cg.shared.global [%0], [%1], 16, %2;" ::"r"(dst), "l"(src), "r"(bytes) : "memory");
-}
-// One arrival (of those that the barrier was set up for) once all of this thread's copies so far are in.
-__device__ __forceinline__ void cp_async_arrive(uint64_t *bar) {
-  asm volatile("cp.async.mbarrier.arrive.noinc.shared::cta.b64 [%0];" ::"r"(smem_u32(bar)) : "memory");
-}
-__device__ __forceinline__ void cp_async_wait_all() { asm volatile("cp.async.wait_all;" ::: "memory"); }
-__device__ __forceinline__ void tma_load_3d(void *dst, const CUtensorMap *map, int c0, int c1, int c2, uint64_t *bar) {
-  asm volatile(
-      "cp.async.bulk.tensor.3d.shared::cluster.global.tile.mbarrier::complete_tx::bytes [%0], [%1, {%3, %4, %5}], [%2];"
-      ::"r"(smem_u32(dst)), "l"(map), "r"(smem_u32(bar)), "r"(c0), "r"(c1), "r"(c2)
-      : "memory");
-}
-// Descriptor of an MN-major tile: panels of 128 bytes of columns x the k-block's rows (128 bytes apart, swizzled), `panel` bytes each.
-__device__ __forceinline__ uint64_t make_desc_mn(uint32_t smem_addr, uint32_t panel) {
-  return (uint64_t)((smem_addr & 0x3FFFFu) >> 4) | ((uint64_t)(panel >> 4) << 16) | ((uint64_t)(1024 >> 4) << 32) | ((uint64_t)1 << 46) | ((uint64_t)2 << 61);
-}
-template <bool EIGHT>
-__device__ __forceinline__ void ex_mma(uint32_t d_tmem, uint64_t a_desc, uint64_t b_desc, uint32_t idesc, uint32_t accumulate) {
-  if constexpr (EIGHT) {
-    asm volatile(
-        "{\n\t.reg .pred p;\n\tsetp.ne.b32 p, %4, 0;\n\t"
-        "tcgen05.mma.cta_group::1.kind::f8f6f4 [%0], %1, %2, %3, {%5, %5, %5, %5}, p;\n\t}"
-        ::"r"(d_tmem), "l"(a_desc), "l"(b_desc), "r"(idesc), "r"(accumulate), "r"(0u)
-        : "memory");
-  } else {
-    tc_mma<false>(d_tmem, a_desc, b_desc, idesc, accumulate);
-  }
-}
-
-// Lane i of the warp reads 32 consecutive columns of TMEM lane (lane base of taddr) + i.
-__device__ __forceinline__ void tmem_ld32(uint32_t taddr, uint32_t (&r)[32]) {
-  asm volatile(
-      "tcgen05.ld.sync.aligned.32x32b.x32.b32 {%0, %1, %2, %3, %4, %5, %6, %7, %8, %9, %10, %11, %12, %13, %14, %15, "
-      "%16, %17, %18, %19, %20, %21, %22, %23, %24, %25, %26, %27, %28, %29, %30, %31}, [%32];"
-      : "=r"(r[0]), "=r"(r[1]), "=r"(r[2]), "=r"(r[3]), "=r"(r[4]), "=r"(r[5]), "=r"(r[6]), "=r"(r[7]), "=r"(r[8]), "=r"(r[9]), "=r"(r[10]),
-        "=r"(r[11]), "=r"(r[12]), "=r"(r[13]), "=r"(r[14]), "=r"(r[15]), "=r"(r[16]), "=r"(r[17]), "=r"(r[18]), "=r"(r[19]), "=r"(r[20]),
-        "=r"(r[21]), "=r"(r[22]), "=r"(r[23]), "=r"(r[24]), "=r"(r[25]), "=r"(r[26]), "=r"(r[27]), "=r"(r[28]), "=r"(r[29]), "=r"(r[30]), "=r"(r[31])
-      : "r"(taddr));
-}
-// Two fp32 values at a time: an epilogue is bound by its instructions.
-__device__ __forceinline__ uint64_t pack2(uint32_t lo, uint32_t hi) {
-  uint64_t d;
-  asm("mov.b64 %0, {%1, %2};" : "=l"(d) : "r"(lo), "r"(hi));
-  return d;
-}
-__device__ __forceinline__ float2 unpack2(uint64_t a) {
-  float2 d;
-  asm("mov.b64 {%0, %1}, %2;" : "=f"(d.x), "=f"(d.y) : "l"(a));
-  return d;
-}
-__device__ __forceinline__ uint64_t add2(uint64_t a, uint64_t b) {
-  uint64_t d;
-  asm("add.rn.f32x2 %0, %1, %2;" : "=l"(d) : "l"(a), "l"(b));
-  return d;
-}
-__device__ __forceinline__ uint64_t mul2(uint64_t a, uint64_t b) {
-  uint64_t d;
-  asm("mul.rn.f32x2 %0, %1, %2;" : "=l"(d) : "l"(a), "l"(b));
-  return d;
-}
-__device__ __forceinline__ uint64_t fma2(uint64_t a, uint64_t b, uint64_t c) {
-  uint64_t d;
-  asm("fma.rn.f32x2 %0, %1, %2, %3;" : "=l"(d) : "l"(a), "l"(b), "l"(c));
-  return d;
-}
-__device__ __forceinline__ uint32_t bf16x2_of(float lo, float hi) {
-  const __nv_bfloat162 h = __floats2bfloat162_rn(lo, hi);
-  return *reinterpret_cast<const uint32_t *>(&h);
-}
-__device__ __forceinline__ uint32_t max_bf16x2(uint32_t a, uint32_t b) {   // NaN stays
-  uint32_t d;
-  asm("max.NaN.bf16x2 %0, %1, %2;" : "=r"(d) : "r"(a), "r"(b));
-  return d;
-}
-
-// The activation of 32 columns (one decision for all of them).
-template <int ACT> __device__ __forceinline__ void expert_act_as(uint64_t (&v)[16]) {
-#pragma unroll
-  for (int i = 0; i < 16; ++i) {
-    const float2 f = unpack2(v[i]);
-    v[i] = pack2(__float_as_uint(it_expert_act(f.x, ACT)), __float_as_uint(it_expert_act(f.y, ACT)));
-  }
-}
-__device__ __forceinline__ void expert_act(uint64_t (&v)[16], int act) {
-  if (act == IT_ACT_RELU) expert_act_as<IT_ACT_RELU>(v);
-  else if (act == IT_ACT_ELU) expert_act_as<IT_ACT_ELU>(v);
-  else if (act == IT_ACT_SILU) expert_act_as<IT_ACT_SILU>(v);
-}
 
 struct ExParams {
   const int32_t *order, *tile_expert, *n_tiles;
@@ -534,16 +441,6 @@ expert_gemm_kernel(const __grid_constant__ CUtensorMap map_a, const __grid_const
 }
 
 // ----------------------------------------------------------------------------- host side
-it_status encode(CUtensorMap *map, bool eight, const void *ptr, int rank, const cuuint64_t *dims, const cuuint64_t *strides, const cuuint32_t *box) {
-  EncodeTiledFn enc = get_encode();
-  IT_REQUIRE(enc != nullptr, IT_ERR_CUDA, "cuTensorMapEncodeTiled is not available from the driver");
-  const cuuint32_t estr[3] = {1, 1, 1};
-  CUresult r = enc(map, eight ? CU_TENSOR_MAP_DATA_TYPE_UINT8 : CU_TENSOR_MAP_DATA_TYPE_BFLOAT16, (cuuint32_t)rank, const_cast<void *>(ptr), dims, strides, box, estr,
-                   CU_TENSOR_MAP_INTERLEAVE_NONE, CU_TENSOR_MAP_SWIZZLE_128B, CU_TENSOR_MAP_L2_PROMOTION_L2_256B, CU_TENSOR_MAP_FLOAT_OOB_FILL_NONE);
-  IT_REQUIRE(r == CUDA_SUCCESS, IT_ERR_CUDA, "cuTensorMapEncodeTiled failed with code %d", (int)r);
-  return IT_OK;
-}
-
 template <bool EIGHT, it_expert_store STORE, bool GATED>
 it_status launch(const CUtensorMap &ma, const CUtensorMap &mw, const ExParams &p, int grid, int smem, double bytes, double flops, cudaStream_t st) {
   IT_CUDA_TRY(cudaFuncSetAttribute(expert_gemm_kernel<EIGHT, STORE, GATED>, cudaFuncAttributeMaxDynamicSharedMemorySize, smem));
