@@ -39,15 +39,6 @@ struct FuParams {
   int no_loads;
 };
 
-// The same product with the A operand in tensor memory (lane = row of the tile, two bf16 a column).
-__device__ __forceinline__ void fu_mma_tmem_a(uint32_t d_tmem, uint32_t a_tmem, uint64_t b_desc, uint32_t idesc, uint32_t accumulate) {
-  asm volatile(
-      "{\n\t.reg .pred p;\n\tsetp.ne.b32 p, %4, 0;\n\t"
-      "tcgen05.mma.cta_group::1.kind::f16 [%0], [%1], %2, %3, {%5, %5, %5, %5}, p;\n\t}"
-      ::"r"(d_tmem), "r"(a_tmem), "l"(b_desc), "r"(idesc), "r"(accumulate), "r"(0u)
-      : "memory");
-}
-
 template <bool EIGHT, bool GATED, bool DIRECT>
 __global__ void __launch_bounds__(FU_THREADS, 1)
 expert_fused_kernel(const __grid_constant__ CUtensorMap map_w1, const __grid_constant__ CUtensorMap map_w2, const FuParams p) {
@@ -194,79 +185,74 @@ expert_fused_kernel(const __grid_constant__ CUtensorMap map_w1, const __grid_con
     if (lane == 0) ring_drain(w_full, (uint32_t)p.stages, stage, phase, came_round);
   } else if (warp == FU_MMA_WARP) {
     // ------------------------------------------------------------------ MMA issuer
-    if (lane == 0) {
-      const uint32_t fmt = EIGHT ? 0u : 1u;
-      const uint32_t idesc1 = (1u << 4) | (fmt << 7) | (fmt << 10) | (1u << 16) | ((uint32_t)(FU_S_COLS >> 3) << 17) | ((uint32_t)(TC_BM >> 4) << 24);
-      uint32_t stage = 0, phase = 0, slot = 0, x_phase = 0;
-      bool ok = true;
-      auto weights = [&]() {
-        ok = mbar_wait(&w_full[stage], phase, abort_flag, p.spin_limit);
-        tc_fence_after();
-        return ok;
-      };
-      auto advance = [&]() {
-        tc_commit(&w_empty[stage]);
-        if (++stage == (uint32_t)p.stages) { stage = 0; phase ^= 1u; }
-      };
-      // chunk number g of this CTA: its S and P buffer g % 2; tile number t: its O buffer t % o_bufs
-      auto issue_s = [&](uint32_t g, bool first_chunk, bool last_chunk) {
-        if (first_chunk) {
-          ok = mbar_wait(&x_full[slot], x_phase, abort_flag, p.spin_limit);
-          if (!ok) return;
-          asm volatile("fence.proxy.async.shared::cta;" ::: "memory");   // the rows were written by other threads' copies
-        }
-        // (P of chunk g - 2 lay where this S goes: its product was issued before)
-        const uint32_t d = tmem_base + s_col + (g & 1u) * FU_S_COLS, x0 = smem_u32(x_s) + slot * (uint32_t)(p.kbx * FU_XBLOCK);
-        for (int kb = 0; kb < p.kbx; ++kb) {
-          if (!weights()) return;
-          const uint32_t a_s = x0 + (uint32_t)kb * FU_XBLOCK, b_s = smem_u32(w_s) + stage * FU_STAGE;
+    const uint32_t fmt = EIGHT ? 0u : 1u, lead = lane == 0;
+    const uint32_t idesc1 = (1u << 4) | (fmt << 7) | (fmt << 10) | (1u << 16) | ((uint32_t)(FU_S_COLS >> 3) << 17) | ((uint32_t)(TC_BM >> 4) << 24);
+    uint32_t stage = 0, phase = 0, slot = 0, x_phase = 0;
+    bool ok = true;
+    auto weights = [&]() {
+      ok = ex_wait_warp(&w_full[stage], phase, abort_flag, p.spin_limit);
+      tc_fence_after();
+      return ok;
+    };
+    auto advance = [&]() {
+      ex_commit(lead, &w_empty[stage]);
+      if (++stage == (uint32_t)p.stages) { stage = 0; phase ^= 1u; }
+    };
+    // chunk number g of this CTA: its S and P buffer g % 2; tile number t: its O buffer t % o_bufs
+    auto issue_s = [&](uint32_t g, bool first_chunk, bool last_chunk) {
+      if (first_chunk) {
+        ok = ex_wait_warp(&x_full[slot], x_phase, abort_flag, p.spin_limit);
+        if (!ok) return;
+        asm volatile("fence.proxy.async.shared::cta;" ::: "memory");   // the rows were written by other threads' copies
+      }
+      // (P of chunk g - 2 lay where this S goes: its product was issued before)
+      const uint32_t d = tmem_base + s_col + (g & 1u) * FU_S_COLS, x0 = smem_u32(x_s) + slot * (uint32_t)(p.kbx * FU_XBLOCK);
+      for (int kb = 0; kb < p.kbx; ++kb) {
+        if (!weights()) return;
+        const uint64_t a_d = make_desc(x0 + (uint32_t)kb * FU_XBLOCK), b_d = make_desc_mn(smem_u32(w_s) + stage * FU_STAGE, BK1 * TC_KBLOCK_BYTES);
 #pragma unroll
-          for (int k = 0; k < 4; ++k)
-            ex_mma<EIGHT>(d, make_desc(a_s + k * 32), make_desc_mn(b_s + k * (BK1 * TC_KBLOCK_BYTES / 4), BK1 * TC_KBLOCK_BYTES), idesc1, (kb | k) != 0);
+        for (int k = 0; k < 4; ++k) ex_mma<EIGHT>(lead, d, a_d + k * 2, b_d + k * (BK1 * TC_KBLOCK_BYTES / 64), idesc1, (kb | k) != 0);
+        advance();
+      }
+      ex_commit(lead, &s_full[g & 1u]);
+      if (last_chunk) {
+        ex_commit(lead, &x_empty[slot]);
+        if (++slot == (uint32_t)p.x_slots) { slot = 0; x_phase ^= 1u; }
+      }
+    };
+    auto issue_o = [&](uint32_t g, uint32_t t, bool first_chunk, bool last_chunk) {
+      ok = ex_wait_warp(&p_full[g & 1u], (g >> 1) & 1u, abort_flag, p.spin_limit);
+      if (!ok) return;
+      const uint32_t ob = p.o_bufs == 2 ? t & 1u : 0u, ot = p.o_bufs == 2 ? t >> 1 : t;
+      if (first_chunk) {
+        ok = ex_wait_warp(&o_empty[ob], (ot & 1u) ^ 1u, abort_flag, p.spin_limit);
+        if (!ok) return;
+      }
+      tc_fence_after();
+      const uint32_t pt = tmem_base + s_col + (g & 1u) * FU_S_COLS;
+      for (int kb = 0; kb < p.chunk_hidden / 64; ++kb)
+        for (int h = 0; h < p.halves; ++h) {
+          const int cols = p.bn - 128 * h < 128 ? p.bn - 128 * h : 128;
+          const uint32_t idesc2 = (1u << 4) | (1u << 7) | (1u << 10) | (1u << 16) | ((uint32_t)(cols >> 3) << 17) | ((uint32_t)(TC_BM >> 4) << 24);
+          if (!weights()) return;
+          const uint64_t b_d = make_desc_mn(smem_u32(w_s) + stage * FU_STAGE, 8192);
+          const uint32_t d = tmem_base + ob * (uint32_t)p.bn + 128u * (uint32_t)h;
+#pragma unroll
+          for (int k = 0; k < 4; ++k)   // where the warps that make P leave it: 32 columns of theirs hold 64 hidden columns, gated 16 hold 32
+            ex_mma_tmem_a(lead, d, GATED ? pt + (k >> 1) * 32 + (k & 1) * 8 : pt + kb * 64 + k * 8, b_d + k * 128, idesc2, !first_chunk || (kb | k) != 0);
           advance();
         }
-        tc_commit(&s_full[g & 1u]);
-        if (last_chunk) {
-          tc_commit(&x_empty[slot]);
-          if (++slot == (uint32_t)p.x_slots) { slot = 0; x_phase ^= 1u; }
-        }
-      };
-      auto issue_o = [&](uint32_t g, uint32_t t, bool first_chunk, bool last_chunk) {
-        ok = mbar_wait(&p_full[g & 1u], (g >> 1) & 1u, abort_flag, p.spin_limit);
-        if (!ok) return;
-        const uint32_t ob = p.o_bufs == 2 ? t & 1u : 0u, ot = p.o_bufs == 2 ? t >> 1 : t;
-        if (first_chunk) {
-          ok = mbar_wait(&o_empty[ob], (ot & 1u) ^ 1u, abort_flag, p.spin_limit);
-          if (!ok) return;
-        }
-        tc_fence_after();
-        const uint32_t pt = tmem_base + s_col + (g & 1u) * FU_S_COLS;
-        for (int kb = 0; kb < p.chunk_hidden / 64; ++kb)
-          for (int h = 0; h < p.halves; ++h) {
-            const int cols = p.bn - 128 * h < 128 ? p.bn - 128 * h : 128;
-            const uint32_t idesc2 = (1u << 4) | (1u << 7) | (1u << 10) | (1u << 16) | ((uint32_t)(cols >> 3) << 17) | ((uint32_t)(TC_BM >> 4) << 24);
-            if (!weights()) return;
-            const uint32_t b_s = smem_u32(w_s) + stage * FU_STAGE, d = tmem_base + ob * (uint32_t)p.bn + 128u * (uint32_t)h;
-#pragma unroll
-            for (int k = 0; k < 4; ++k) {
-              // where the warps that make P leave it: 32 columns of theirs hold 64 hidden columns, gated 16 hold 32
-              const uint32_t a = GATED ? pt + (k >> 1) * 32 + (k & 1) * 8 : pt + kb * 64 + k * 8;
-              fu_mma_tmem_a(d, a, make_desc_mn(b_s + k * 2048, 8192), idesc2, !first_chunk || (kb | k) != 0);
-            }
-            advance();
-          }
-        if (last_chunk) tc_commit(&o_full[ob]);
-      };
-      uint32_t g = 0, t = 0;
-      for (int m = blockIdx.x; m < m_tiles && ok; m += gridDim.x, ++t)
-        for (int c = 0; c < p.chunks && ok; ++c, ++g) {
-          issue_s(g, c == 0, c + 1 == p.chunks);
-          if (ok && g > 0) issue_o(g - 1, c > 0 ? t : t - 1, c > 0 ? c == 1 : p.chunks == 1, c == 0);
-        }
-      if (ok && g > 0) issue_o(g - 1, t - 1, p.chunks == 1, true);
-      tc_commit(mma_done);
-      mbar_drain(mma_done, 0);
-    }
+      if (last_chunk) ex_commit(lead, &o_full[ob]);
+    };
+    uint32_t g = 0, t = 0;
+    for (int m = blockIdx.x; m < m_tiles && ok; m += gridDim.x, ++t)
+      for (int c = 0; c < p.chunks && ok; ++c, ++g) {
+        issue_s(g, c == 0, c + 1 == p.chunks);
+        if (ok && g > 0) issue_o(g - 1, c > 0 ? t : t - 1, c > 0 ? c == 1 : p.chunks == 1, c == 0);
+      }
+    if (ok && g > 0) issue_o(g - 1, t - 1, p.chunks == 1, true);
+    ex_commit(lead, mma_done);
+    mbar_drain(mma_done, 0);
   } else if (warp < FU_P_WARP0 + FU_P_WARPS) {
     // ------------------------------------------------------------------ P: a thread per row, 64 accumulator columns a warp (gated: 32 of the gate, 32 gated)
     const int quarter = warp & 3, sub = (warp - FU_P_WARP0) >> 2;   // a warp may only touch TMEM lanes [32 * (warp % 4), +32)

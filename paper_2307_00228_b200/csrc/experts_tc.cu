@@ -185,37 +185,36 @@ expert_gemm_kernel(const __grid_constant__ CUtensorMap map_a, const __grid_const
     if (lane == 0 && warp == 0) ring_drain(full, (uint32_t)p.stages, stage, phase, came_round);
   } else if (warp == EX_MMA_WARP) {
     // ------------------------------------------------------------------ MMA issuer
-    if (lane == 0) {
-      // D = fp32, A K-major, B MN-major (bit 16), N = bn, M = 128; operands bf16 (1) or e4m3 (0)
-      const uint32_t fmt = EIGHT ? 0u : 1u;
-      const uint32_t idesc = (1u << 4) | (fmt << 7) | (fmt << 10) | (1u << 16) | ((uint32_t)(p.bn >> 3) << 17) | ((uint32_t)(TC_BM >> 4) << 24);
-      uint32_t stage = 0, phase = 0, acc = 0, acc_phase = 0;
-      bool ok = true;
-      for (uint32_t tile = blockIdx.x; tile < n_tiles && ok; tile += gridDim.x) {
-        ok = mbar_wait(&acc_empty[acc], acc_phase ^ 1u, abort_flag, p.spin_limit);
+    // D = fp32, A K-major, B MN-major (bit 16), N = bn, M = 128; operands bf16 (1) or e4m3 (0)
+    const uint32_t fmt = EIGHT ? 0u : 1u, lead = lane == 0;
+    const uint32_t idesc = (1u << 4) | (fmt << 7) | (fmt << 10) | (1u << 16) | ((uint32_t)(p.bn >> 3) << 17) | ((uint32_t)(TC_BM >> 4) << 24);
+    uint32_t stage = 0, phase = 0, acc = 0, acc_phase = 0;
+    bool ok = true;
+    for (uint32_t tile = blockIdx.x; tile < n_tiles && ok; tile += gridDim.x) {
+      ok = ex_wait_warp(&acc_empty[acc], acc_phase ^ 1u, abort_flag, p.spin_limit);
+      if (!ok) break;
+      tc_fence_after();
+      const uint32_t d_tmem = tmem_base + acc * (uint32_t)p.bn;
+      for (int kb = 0; kb < KB; ++kb) {
+        ok = ex_wait_warp(&full[stage], phase, abort_flag, p.spin_limit);
         if (!ok) break;
+        // gathered rows were written by the threads of the other warps: what follows reads them through the tensor core's path
+        if (p.gather_div) asm volatile("fence.proxy.async.shared::cta;" ::: "memory");
         tc_fence_after();
-        const uint32_t d_tmem = tmem_base + acc * (uint32_t)p.bn;
-        for (int kb = 0; kb < KB; ++kb) {
-          ok = mbar_wait(&full[stage], phase, abort_flag, p.spin_limit);
-          if (!ok) break;
-          // gathered rows were written by the threads of the other warps: what follows reads them through the tensor core's path
-          if (p.gather_div) asm volatile("fence.proxy.async.shared::cta;" ::: "memory");
-          tc_fence_after();
-          const uint32_t a_s = smem_u32(base + (size_t)stage * stage_bytes), b_s = a_s + EX_STAGE_A;
+        const uint32_t a_s = smem_u32(base) + stage * (uint32_t)stage_bytes;
+        const uint64_t a_d = make_desc(a_s), b_d = make_desc_mn(a_s + EX_STAGE_A, PANEL);
 #pragma unroll
-          for (int k = 0; k < 4; ++k)   // four steps of 32 bytes of K: a quarter of the k-block's rows of W
-            ex_mma<EIGHT>(d_tmem, make_desc(a_s + k * 32), make_desc_mn(b_s + k * (PANEL / 4), PANEL), idesc, (kb | k) != 0);
-          tc_commit(&empty[stage]);
-          if (++stage == (uint32_t)p.stages) { stage = 0; phase ^= 1u; }
-        }
-        if (!ok) break;
-        tc_commit(&acc_full[acc]);
-        if (++acc == 2) { acc = 0; acc_phase ^= 1u; }
+        for (int k = 0; k < 4; ++k)   // four steps of 32 bytes of K: a quarter of the k-block's rows of W
+          ex_mma<EIGHT>(lead, d_tmem, a_d + k * 2, b_d + k * (PANEL / 64), idesc, (kb | k) != 0);
+        ex_commit(lead, &empty[stage]);
+        if (++stage == (uint32_t)p.stages) { stage = 0; phase ^= 1u; }
       }
-      tc_commit(mma_done);
-      mbar_drain(mma_done, 0);
+      if (!ok) break;
+      ex_commit(lead, &acc_full[acc]);
+      if (++acc == 2) { acc = 0; acc_phase ^= 1u; }
     }
+    ex_commit(lead, mma_done);
+    mbar_drain(mma_done, 0);
   } else if (warp == EX_META_WARP) {
     // ------------------------------------------------------------------ what the epilogue needs, ahead of it: two loads, one behind the other, for
     // every tile, and four rows and columns a lane.  (Made by the epilogue where it needs them, these waits took most of its time.)

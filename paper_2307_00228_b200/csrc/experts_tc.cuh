@@ -25,19 +25,45 @@ __device__ __forceinline__ void tma_load_3d(void *dst, const CUtensorMap *map, i
 __device__ __forceinline__ uint64_t make_desc_mn(uint32_t smem_addr, uint32_t panel) {
   return (uint64_t)((smem_addr & 0x3FFFFu) >> 4) | ((uint64_t)(panel >> 4) << 16) | ((uint64_t)(1024 >> 4) << 32) | ((uint64_t)1 << 46) | ((uint64_t)2 << 61);
 }
+// MMAs are issued by a whole warp of which one lane, `lead`, is let through: descriptors and loops are then the same for the warp and stay
+// in its uniform registers.  (Issued by one thread in a branch of its own, an MMA took some 140 cycles, more than twice what one of 128 x 128 x 16
+// keeps the tensor core busy.)
 template <bool EIGHT>
-__device__ __forceinline__ void ex_mma(uint32_t d_tmem, uint64_t a_desc, uint64_t b_desc, uint32_t idesc, uint32_t accumulate) {
+__device__ __forceinline__ void ex_mma(uint32_t lead, uint32_t d_tmem, uint64_t a_desc, uint64_t b_desc, uint32_t idesc, uint32_t accumulate) {
   if constexpr (EIGHT) {
     asm volatile(
-        "{\n\t.reg .pred p;\n\tsetp.ne.b32 p, %4, 0;\n\t"
-        "tcgen05.mma.cta_group::1.kind::f8f6f4 [%0], %1, %2, %3, {%5, %5, %5, %5}, p;\n\t}"
-        ::"r"(d_tmem), "l"(a_desc), "l"(b_desc), "r"(idesc), "r"(accumulate), "r"(0u)
+        "{\n\t.reg .pred p, q;\n\tsetp.ne.b32 p, %4, 0;\n\tsetp.ne.b32 q, %6, 0;\n\t"
+        "@q tcgen05.mma.cta_group::1.kind::f8f6f4 [%0], %1, %2, %3, {%5, %5, %5, %5}, p;\n\t}"
+        ::"r"(d_tmem), "l"(a_desc), "l"(b_desc), "r"(idesc), "r"(accumulate), "r"(0u), "r"(lead)
         : "memory");
   } else {
-    tc_mma<false>(d_tmem, a_desc, b_desc, idesc, accumulate);
+    asm volatile(
+        "{\n\t.reg .pred p, q;\n\tsetp.ne.b32 p, %4, 0;\n\tsetp.ne.b32 q, %6, 0;\n\t"
+        "@q tcgen05.mma.cta_group::1.kind::f16 [%0], %1, %2, %3, {%5, %5, %5, %5}, p;\n\t}"
+        ::"r"(d_tmem), "l"(a_desc), "l"(b_desc), "r"(idesc), "r"(accumulate), "r"(0u), "r"(lead)
+        : "memory");
   }
 }
-
+// The same product with the A operand in tensor memory (lane = row of the tile, two bf16 a column).
+__device__ __forceinline__ void ex_mma_tmem_a(uint32_t lead, uint32_t d_tmem, uint32_t a_tmem, uint64_t b_desc, uint32_t idesc, uint32_t accumulate) {
+  asm volatile(
+      "{\n\t.reg .pred p, q;\n\tsetp.ne.b32 p, %4, 0;\n\tsetp.ne.b32 q, %6, 0;\n\t"
+      "@q tcgen05.mma.cta_group::1.kind::f16 [%0], [%1], %2, %3, {%5, %5, %5, %5}, p;\n\t}"
+      ::"r"(d_tmem), "r"(a_tmem), "l"(b_desc), "r"(idesc), "r"(accumulate), "r"(0u), "r"(lead)
+      : "memory");
+}
+__device__ __forceinline__ void ex_commit(uint32_t lead, uint64_t *bar) {
+  asm volatile(
+      "{\n\t.reg .pred q;\n\tsetp.ne.b32 q, %1, 0;\n\t"
+      "@q tcgen05.commit.cta_group::1.mbarrier::arrive::one.shared::cluster.b64 [%0];\n\t}"
+      ::"r"(smem_u32(bar)), "r"(lead)
+      : "memory");
+}
+// A wait of a whole warp: the same answer for all its lanes.
+__device__ __forceinline__ bool ex_wait_warp(uint64_t *bar, uint32_t parity, volatile int *abort_flag, uint32_t limit) {
+  const bool ok = mbar_wait(bar, parity, abort_flag, limit);
+  return __all_sync(0xffffffffu, ok);
+}
 // Lane i of the warp reads 32 consecutive columns of TMEM lane (lane base of taddr) + i.
 __device__ __forceinline__ void tmem_ld32(uint32_t taddr, uint32_t (&r)[32]) {
   asm volatile(
