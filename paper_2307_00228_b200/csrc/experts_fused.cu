@@ -4,9 +4,10 @@
 // Gated: a chunk is 64 columns of the gate and the 64 that it gates.  With the hidden row in memory the two products of 1M vertices, 2 of 16,
 // 128-512-128, moved 6 GB, 4 of them hidden rows, and took 1160 us at 5.2 TB/s.
 //
-// Warps: 0 and 1 fetch rows of X by place (16-byte asynchronous copies, a tile ahead), 2 the weights (TMA, in the order of their use), 3 issues the
-// MMAs (S of chunk g + 1 before O of chunk g, so that the tensor core works while P is made), 4-11 make P, 12-15 store O: sixteen, which
-// leave 128 registers a thread.
+// Warps: 0 fetches rows of X by place (16-byte asynchronous copies, a tile ahead), 1 the weights (TMA, W1 of chunk g + 1 before W2 of chunk g), 2 and 3
+// issue the MMAs of S and of O, 4-11 make P, 12-15 store O: sixteen, which leave 128 registers a thread.  S and O have a warp each because a
+// wait costs an issuing warp some 160 cycles and a commit 95, as much together as the products of a chunk (128 columns in and out) take: issued by one
+// warp, with a stage of weights per k-block, a chunk took 3300 cycles.
 // S and P are buffered twice, O twice where it has at most 128 columns.
 // Waits are bounded as in the other products.
 #include <type_traits>
@@ -15,11 +16,10 @@
 
 namespace {
 
-constexpr int FU_FETCH_WARPS = 2, FU_W_WARP = 2, FU_MMA_WARP = 3, FU_P_WARP0 = 4, FU_P_WARPS = 8, FU_O_WARP0 = 12, FU_O_WARPS = 4;
+constexpr int FU_FETCH_WARP = 0, FU_W_WARP = 1, FU_S_WARP = 2, FU_MMA_WARP = 3 /* of O */, FU_P_WARP0 = 4, FU_P_WARPS = 8, FU_O_WARP0 = 12, FU_O_WARPS = 4;
 constexpr int FU_THREADS = 32 * (FU_O_WARP0 + FU_O_WARPS);
-constexpr int FU_STAGE = 16384;      // of the weights: a k-block of 128 columns
 constexpr int FU_XBLOCK = TC_BM * TC_KBLOCK_BYTES;
-constexpr int FU_MAX_STAGES = 8;
+constexpr int FU_MAX_STAGES = 4;     // of either ring of weights
 constexpr int FU_BACKOFF = 32;       // ns between polls
 constexpr int FU_S_COLS = 128;       // accumulator columns of a chunk
 
@@ -30,8 +30,10 @@ struct FuParams {
   int tiles_max, top_k, n_experts;
   int in_bytes, kbx;                 // bytes of a row of X, its k-blocks
   int hidden, n1, chunks, chunk_hidden;   // columns of W1; chunks of 128 (gated: 64) hidden columns
-  int out, bn, halves;               // columns of the result, padded to panels; parts of up to 128 of them
-  int x_slots, stages, o_bufs;
+  int out, bn;                       // columns of the result, and padded to panels
+  int kb1, stages1, stage1;          // W1: k-blocks of a stage, stages, bytes of one
+  int kb2, stages2, stage2;          // W2: of 64 hidden columns each
+  int x_slots, o_bufs;
   int act;
   void *dst;
   int *status;
@@ -47,37 +49,44 @@ expert_fused_kernel(const __grid_constant__ CUtensorMap map_w1, const __grid_con
   constexpr int BK1 = EIGHT ? 128 : 64;              // elements of a k-block of X, and columns of a panel of W1
   constexpr int STAGING = DIRECT ? 4096 : 2048;      // per storing warp: 32 rows of 128 or 64 bytes
   unsigned char *x_s = base;
-  unsigned char *w_s = x_s + (size_t)p.x_slots * p.kbx * FU_XBLOCK;
-  unsigned char *staging = w_s + (size_t)p.stages * FU_STAGE;
+  unsigned char *w1_s = x_s + (size_t)p.x_slots * p.kbx * FU_XBLOCK;
+  unsigned char *w2_s = w1_s + (size_t)p.stages1 * p.stage1;
+  unsigned char *staging = w2_s + (size_t)p.stages2 * p.stage2;
   float *p_consts = reinterpret_cast<float *>(staging + FU_O_WARPS * STAGING);   // [8 warps][2][64 bias | 64 scale]
   float *o_consts = p_consts + FU_P_WARPS * 2 * (EIGHT ? 128 : 64);               // [4 warps][256] b2
   int32_t *o_place = reinterpret_cast<int32_t *>(o_consts + FU_O_WARPS * 256);    // [128]
-  uint64_t *w_full = reinterpret_cast<uint64_t *>(o_place + TC_BM);
-  uint64_t *w_empty = w_full + FU_MAX_STAGES;
-  uint64_t *x_full = w_empty + FU_MAX_STAGES;   // [2]
+  uint64_t *w1_full = reinterpret_cast<uint64_t *>(o_place + TC_BM);
+  uint64_t *w1_empty = w1_full + FU_MAX_STAGES;
+  uint64_t *w2_full = w1_empty + FU_MAX_STAGES;
+  uint64_t *w2_empty = w2_full + FU_MAX_STAGES;
+  uint64_t *x_full = w2_empty + FU_MAX_STAGES;   // [2]
   uint64_t *x_empty = x_full + 2;               // [2]
   uint64_t *s_full = x_empty + 2;               // [2]
-  uint64_t *p_full = s_full + 2;                // [2]
+  uint64_t *s_free = s_full + 2;                // [2]  the product that read P from this buffer is over
+  uint64_t *p_full = s_free + 2;                // [2]
   uint64_t *o_full = p_full + 2;                // [2]
   uint64_t *o_empty = o_full + 2;               // [2]
-  uint64_t *mma_done = o_empty + 2;             // [1]
-  uint32_t *tmem_slot = reinterpret_cast<uint32_t *>(mma_done + 1);
+  uint64_t *mma_done = o_empty + 2;             // [2]  every MMA of S, of O is over
+  uint32_t *tmem_slot = reinterpret_cast<uint32_t *>(mma_done + 2);
   volatile int *abort_flag = reinterpret_cast<volatile int *>(tmem_slot + 1);
 
   if (threadIdx.x == 0) {
-    for (int s = 0; s < p.stages; ++s) {
-      mbar_init(&w_full[s], 1);
-      mbar_init(&w_empty[s], 1);
+    for (int s = 0; s < FU_MAX_STAGES; ++s) {
+      mbar_init(&w1_full[s], 1);
+      mbar_init(&w1_empty[s], 1);
+      mbar_init(&w2_full[s], 1);
+      mbar_init(&w2_empty[s], 1);
     }
     for (int a = 0; a < 2; ++a) {
-      mbar_init(&x_full[a], 32 * FU_FETCH_WARPS);
+      mbar_init(&x_full[a], 32);
+      mbar_init(&s_free[a], 1);
+      mbar_init(&mma_done[a], 1);
       mbar_init(&x_empty[a], 1);
       mbar_init(&s_full[a], 1);
       mbar_init(&p_full[a], FU_P_WARPS);
       mbar_init(&o_full[a], 1);
       mbar_init(&o_empty[a], FU_O_WARPS);
     }
-    mbar_init(mma_done, 1);
     *abort_flag = 0;
     asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");
   }
@@ -94,16 +103,16 @@ expert_fused_kernel(const __grid_constant__ CUtensorMap map_w1, const __grid_con
   int m_tiles = *p.n_tiles;
   m_tiles = m_tiles < p.tiles_max ? m_tiles : p.tiles_max;
 
-  if (warp < FU_FETCH_WARPS) {
+  if (warp == FU_FETCH_WARP) {
     // ------------------------------------------------------------------ rows of X, by place
-    constexpr int GROUPS = TC_BM / 32 / FU_FETCH_WARPS;   // of 32 rows a warp
+    constexpr int GROUPS = TC_BM / 32;   // of 32 rows
     const int chunk = lane & 7;
     uint32_t slot = 0, phase = 0;
     int place_next[GROUPS];
     auto look = [&](int m) {
 #pragma unroll
       for (int q = 0; q < GROUPS; ++q)
-        if (m < m_tiles) place_next[q] = p.order[(int64_t)m * TC_BM + (warp * GROUPS + q) * 32 + lane];
+        if (m < m_tiles) place_next[q] = p.order[(int64_t)m * TC_BM + q * 32 + lane];
     };
     look(blockIdx.x);
     for (int m = blockIdx.x; m < m_tiles && !p.no_loads; m += gridDim.x) {
@@ -114,60 +123,72 @@ expert_fused_kernel(const __grid_constant__ CUtensorMap map_w1, const __grid_con
       const int ok = lane == 0 ? mbar_wait(&x_empty[slot], phase ^ 1u, abort_flag, p.spin_limit, FU_BACKOFF) : 1;
       if (!__shfl_sync(0xffffffffu, ok, 0)) break;
       const uint32_t to = smem_u32(x_s) + slot * (uint32_t)(p.kbx * FU_XBLOCK);
+      // (addresses of eight rows first, then their copies one behind the other: a warp that makes them row by row waits for itself)
 #pragma unroll
-      for (int q = 0; q < GROUPS; ++q)
+      for (int q = 0; q < GROUPS; ++q) {
+        const unsigned char *src[8];
+        uint32_t bytes[8];
 #pragma unroll
         for (int i = 0; i < 8; ++i) {
-          const int local = i * 4 + (lane >> 3), r = __shfl_sync(0xffffffffu, row[q], local), in_tile = (warp * GROUPS + q) * 32 + local;
-          const unsigned char *from = reinterpret_cast<const unsigned char *>(p.x) + (int64_t)(r < 0 ? 0 : r) * p.in_bytes;
-          const uint32_t dst = to + (uint32_t)in_tile * TC_KBLOCK_BYTES + (uint32_t)((chunk ^ (in_tile & 7)) << 4);
-          for (int kb = 0; kb < p.kbx; ++kb) {
-            const int at = kb * TC_KBLOCK_BYTES + chunk * 16;
-            const bool in = r >= 0 && at < p.in_bytes;
-            cp_async16(dst + (uint32_t)kb * FU_XBLOCK, in ? from + at : p.x, in ? 16u : 0u);
-          }
+          const int r = __shfl_sync(0xffffffffu, row[q], i * 4 + (lane >> 3));
+          src[i] = reinterpret_cast<const unsigned char *>(p.x) + (int64_t)(r < 0 ? 0 : r) * p.in_bytes + chunk * 16;
+          bytes[i] = r < 0 ? 0u : 16u;
         }
+        const uint32_t dst = to + (uint32_t)q * 4096u + (uint32_t)(lane >> 3) * TC_KBLOCK_BYTES;
+        const uint32_t even = dst + (uint32_t)((chunk ^ (lane >> 3)) << 4), odd = dst + (uint32_t)((chunk ^ (4 + (lane >> 3))) << 4);
+        for (int kb = 0; kb < p.kbx; ++kb) {
+          const bool in = kb * TC_KBLOCK_BYTES + chunk * 16 < p.in_bytes;
+#pragma unroll
+          for (int i = 0; i < 8; ++i)
+            cp_async16(((i & 1) ? odd : even) + (uint32_t)(i * 512) + (uint32_t)kb * FU_XBLOCK, in ? src[i] + kb * TC_KBLOCK_BYTES : src[i] - chunk * 16, in ? bytes[i] : 0u);
+        }
+      }
       cp_async_arrive(&x_full[slot]);
       if (++slot == (uint32_t)p.x_slots) { slot = 0; phase ^= 1u; }
     }
     __syncwarp();
     cp_async_wait_all();
   } else if (warp == FU_W_WARP) {
-    // ------------------------------------------------------------------ weights: W1 of a chunk, then W2 of the one before it
-    uint32_t stage = 0, phase = 0;
-    bool ok = !p.no_loads, came_round = false;
-    auto next_stage = [&](uint32_t bytes) {   // a free stage, armed
+    // ------------------------------------------------------------------ weights: W1 of a chunk, then W2 of the one before it; a ring each
+    struct Ring { uint64_t *full, *empty; uint32_t stages, stage, phase; bool came_round; };
+    Ring r1{w1_full, w1_empty, (uint32_t)p.stages1, 0, 0, false}, r2{w2_full, w2_empty, (uint32_t)p.stages2, 0, 0, false};
+    bool ok = !p.no_loads;
+    auto arm = [&](Ring &r, uint32_t bytes) {   // a free stage
       if (lane == 0) {
-        ok = mbar_wait(&w_empty[stage], phase ^ 1u, abort_flag, p.spin_limit, FU_BACKOFF);
-        if (ok) mbar_arrive_expect_tx(&w_full[stage], bytes);
+        ok = mbar_wait(&r.empty[r.stage], r.phase ^ 1u, abort_flag, p.spin_limit, FU_BACKOFF);
+        if (ok) mbar_arrive_expect_tx(&r.full[r.stage], bytes);
       }
       ok = __shfl_sync(0xffffffffu, (int)ok, 0);
       return ok;
     };
-    auto advance = [&]() {
+    auto advance = [&](Ring &r) {
       __syncwarp();
-      if (++stage == (uint32_t)p.stages) { stage = 0; phase ^= 1u; came_round = true; }
+      if (++r.stage == r.stages) { r.stage = 0; r.phase ^= 1u; r.came_round = true; }
     };
     auto first = [&](int e, int c) {
-      for (int kb = 0; kb < p.kbx; ++kb) {
-        if (!next_stage(FU_STAGE)) return;
-        unsigned char *to = w_s + (size_t)stage * FU_STAGE;
-        if (lane < 128 / BK1) {
-          const int col = GATED ? lane * p.hidden + c * 64 : c * 128 + lane * BK1;
-          tma_load_3d(to + lane * BK1 * TC_KBLOCK_BYTES, &map_w1, col, kb * BK1, e, &w_full[stage]);
+      constexpr int PANELS = 128 / BK1;
+      for (int kb0 = 0; kb0 < p.kbx; kb0 += p.kb1) {
+        const int n = p.kbx - kb0 < p.kb1 ? p.kbx - kb0 : p.kb1;
+        if (!arm(r1, (uint32_t)n * FU_XBLOCK)) return;
+        unsigned char *to = w1_s + (size_t)r1.stage * p.stage1;
+        if (lane < n * PANELS) {
+          const int kb = lane / PANELS, panel = lane % PANELS, col = GATED ? panel * p.hidden + c * 64 : c * 128 + panel * BK1;
+          tma_load_3d(to + lane * BK1 * TC_KBLOCK_BYTES, &map_w1, col, (kb0 + kb) * BK1, e, &w1_full[r1.stage]);
         }
-        advance();
+        advance(r1);
       }
     };
     auto second = [&](int e, int c) {
-      for (int kb = 0; kb < p.chunk_hidden / 64; ++kb)
-        for (int h = 0; h < p.halves; ++h) {
-          const int cols = p.bn - 128 * h < 128 ? p.bn - 128 * h : 128;
-          if (!next_stage((uint32_t)cols * TC_KBLOCK_BYTES)) return;
-          unsigned char *to = w_s + (size_t)stage * FU_STAGE;
-          if (lane < cols / 64) tma_load_3d(to + lane * 64 * TC_KBLOCK_BYTES, &map_w2, 128 * h + lane * 64, c * p.chunk_hidden + kb * 64, e, &w_full[stage]);
-          advance();
+      const int panels = p.bn / 64;
+      for (int kb0 = 0; kb0 < p.chunk_hidden / 64; kb0 += p.kb2) {
+        if (!arm(r2, (uint32_t)p.stage2)) return;
+        unsigned char *to = w2_s + (size_t)r2.stage * p.stage2;
+        if (lane < p.kb2 * panels) {
+          const int kb = lane / panels, panel = lane % panels;
+          tma_load_3d(to + lane * 8192, &map_w2, panel * 64, c * p.chunk_hidden + (kb0 + kb) * 64, e, &w2_full[r2.stage]);
         }
+        advance(r2);
+      }
     };
     int e_before = -1;
     int e_next = (int)blockIdx.x < m_tiles ? p.tile_expert[blockIdx.x] : 0;
@@ -182,77 +203,77 @@ expert_fused_kernel(const __grid_constant__ CUtensorMap map_w1, const __grid_con
     }
     if (ok && e_before >= 0) second(e_before, p.chunks - 1);
     __syncwarp();
-    if (lane == 0) ring_drain(w_full, (uint32_t)p.stages, stage, phase, came_round);
-  } else if (warp == FU_MMA_WARP) {
-    // ------------------------------------------------------------------ MMA issuer
+    if (lane == 0) {
+      ring_drain(w1_full, r1.stages, r1.stage, r1.phase, r1.came_round);
+      ring_drain(w2_full, r2.stages, r2.stage, r2.phase, r2.came_round);
+    }
+  } else if (warp == FU_S_WARP) {
+    // ------------------------------------------------------------------ S = X W1: chunk number g of this CTA into buffer g % 2
     const uint32_t fmt = EIGHT ? 0u : 1u, lead = lane == 0;
-    const uint32_t idesc1 = (1u << 4) | (fmt << 7) | (fmt << 10) | (1u << 16) | ((uint32_t)(FU_S_COLS >> 3) << 17) | ((uint32_t)(TC_BM >> 4) << 24);
-    uint32_t stage = 0, phase = 0, slot = 0, x_phase = 0;
+    const uint32_t idesc = (1u << 4) | (fmt << 7) | (fmt << 10) | (1u << 16) | ((uint32_t)(FU_S_COLS >> 3) << 17) | ((uint32_t)(TC_BM >> 4) << 24);
+    uint32_t stage = 0, phase = 0, slot = 0, x_phase = 0, g = 0;
     bool ok = true;
-    auto weights = [&]() {
-      ok = ex_wait_warp(&w_full[stage], phase, abort_flag, p.spin_limit);
-      tc_fence_after();
-      return ok;
-    };
-    auto advance = [&]() {
-      ex_commit(lead, &w_empty[stage]);
-      if (++stage == (uint32_t)p.stages) { stage = 0; phase ^= 1u; }
-    };
-    // chunk number g of this CTA: its S and P buffer g % 2; tile number t: its O buffer t % o_bufs
-    auto issue_s = [&](uint32_t g, bool first_chunk, bool last_chunk) {
-      if (first_chunk) {
-        ok = ex_wait_warp(&x_full[slot], x_phase, abort_flag, p.spin_limit);
-        if (!ok) return;
-        asm volatile("fence.proxy.async.shared::cta;" ::: "memory");   // the rows were written by other threads' copies
-      }
-      // (P of chunk g - 2 lay where this S goes: its product was issued before)
-      const uint32_t d = tmem_base + s_col + (g & 1u) * FU_S_COLS, x0 = smem_u32(x_s) + slot * (uint32_t)(p.kbx * FU_XBLOCK);
-      for (int kb = 0; kb < p.kbx; ++kb) {
-        if (!weights()) return;
-        const uint64_t a_d = make_desc(x0 + (uint32_t)kb * FU_XBLOCK), b_d = make_desc_mn(smem_u32(w_s) + stage * FU_STAGE, BK1 * TC_KBLOCK_BYTES);
-#pragma unroll
-        for (int k = 0; k < 4; ++k) ex_mma<EIGHT>(lead, d, a_d + k * 2, b_d + k * (BK1 * TC_KBLOCK_BYTES / 64), idesc1, (kb | k) != 0);
-        advance();
-      }
-      ex_commit(lead, &s_full[g & 1u]);
-      if (last_chunk) {
-        ex_commit(lead, &x_empty[slot]);
-        if (++slot == (uint32_t)p.x_slots) { slot = 0; x_phase ^= 1u; }
-      }
-    };
-    auto issue_o = [&](uint32_t g, uint32_t t, bool first_chunk, bool last_chunk) {
-      ok = ex_wait_warp(&p_full[g & 1u], (g >> 1) & 1u, abort_flag, p.spin_limit);
-      if (!ok) return;
-      const uint32_t ob = p.o_bufs == 2 ? t & 1u : 0u, ot = p.o_bufs == 2 ? t >> 1 : t;
-      if (first_chunk) {
-        ok = ex_wait_warp(&o_empty[ob], (ot & 1u) ^ 1u, abort_flag, p.spin_limit);
-        if (!ok) return;
-      }
-      tc_fence_after();
-      const uint32_t pt = tmem_base + s_col + (g & 1u) * FU_S_COLS;
-      for (int kb = 0; kb < p.chunk_hidden / 64; ++kb)
-        for (int h = 0; h < p.halves; ++h) {
-          const int cols = p.bn - 128 * h < 128 ? p.bn - 128 * h : 128;
-          const uint32_t idesc2 = (1u << 4) | (1u << 7) | (1u << 10) | (1u << 16) | ((uint32_t)(cols >> 3) << 17) | ((uint32_t)(TC_BM >> 4) << 24);
-          if (!weights()) return;
-          const uint64_t b_d = make_desc_mn(smem_u32(w_s) + stage * FU_STAGE, 8192);
-          const uint32_t d = tmem_base + ob * (uint32_t)p.bn + 128u * (uint32_t)h;
-#pragma unroll
-          for (int k = 0; k < 4; ++k)   // where the warps that make P leave it: 32 columns of theirs hold 64 hidden columns, gated 16 hold 32
-            ex_mma_tmem_a(lead, d, GATED ? pt + (k >> 1) * 32 + (k & 1) * 8 : pt + kb * 64 + k * 8, b_d + k * 128, idesc2, !first_chunk || (kb | k) != 0);
-          advance();
-        }
-      if (last_chunk) ex_commit(lead, &o_full[ob]);
-    };
-    uint32_t g = 0, t = 0;
-    for (int m = blockIdx.x; m < m_tiles && ok; m += gridDim.x, ++t)
+    for (int m = blockIdx.x; m < m_tiles && ok; m += gridDim.x) {
+      ok = ex_wait_warp(&x_full[slot], x_phase, abort_flag, p.spin_limit);
+      if (!ok) break;
+      asm volatile("fence.proxy.async.shared::cta;" ::: "memory");   // the rows were written by other threads' copies
+      const uint64_t x_d = make_desc(smem_u32(x_s) + slot * (uint32_t)(p.kbx * FU_XBLOCK));
       for (int c = 0; c < p.chunks && ok; ++c, ++g) {
-        issue_s(g, c == 0, c + 1 == p.chunks);
-        if (ok && g > 0) issue_o(g - 1, c > 0 ? t : t - 1, c > 0 ? c == 1 : p.chunks == 1, c == 0);
+        // the chunk before the last one's P lies where this S goes
+        if (g >= 2) ok = ex_wait_warp(&s_free[g & 1u], ((g >> 1) & 1u) ^ 1u, abort_flag, p.spin_limit);
+        const uint32_t d = tmem_base + s_col + (g & 1u) * FU_S_COLS;
+        for (int kb0 = 0; kb0 < p.kbx && ok; kb0 += p.kb1) {
+          ok = ex_wait_warp(&w1_full[stage], phase, abort_flag, p.spin_limit);
+          if (!ok) break;
+          tc_fence_after();
+          const uint64_t b_d = make_desc_mn(smem_u32(w1_s) + stage * (uint32_t)p.stage1, BK1 * TC_KBLOCK_BYTES);
+          for (int i = 0; i < p.kb1 && kb0 + i < p.kbx; ++i) {
+#pragma unroll
+            for (int k = 0; k < 4; ++k)
+              ex_mma<EIGHT>(lead, d, x_d + (kb0 + i) * (FU_XBLOCK / 16) + k * 2, b_d + i * (FU_XBLOCK / 16) + k * (BK1 * TC_KBLOCK_BYTES / 64), idesc, (kb0 | i | k) != 0);
+          }
+          ex_commit(lead, &w1_empty[stage]);
+          if (++stage == (uint32_t)p.stages1) { stage = 0; phase ^= 1u; }
+        }
+        if (ok) ex_commit(lead, &s_full[g & 1u]);
       }
-    if (ok && g > 0) issue_o(g - 1, t - 1, p.chunks == 1, true);
-    ex_commit(lead, mma_done);
-    mbar_drain(mma_done, 0);
+      if (ok) ex_commit(lead, &x_empty[slot]);
+      if (++slot == (uint32_t)p.x_slots) { slot = 0; x_phase ^= 1u; }
+    }
+    ex_commit(lead, &mma_done[0]);
+    mbar_drain(&mma_done[0], 0);
+  } else if (warp == FU_MMA_WARP) {
+    // ------------------------------------------------------------------ O += P W2: tile number t of this CTA into buffer t % o_bufs
+    const uint32_t lead = lane == 0;
+    const uint32_t idesc = (1u << 4) | (1u << 7) | (1u << 10) | (1u << 16) | ((uint32_t)(p.bn >> 3) << 17) | ((uint32_t)(TC_BM >> 4) << 24);
+    uint32_t stage = 0, phase = 0, g = 0, t = 0;
+    bool ok = true;
+    for (int m = blockIdx.x; m < m_tiles && ok; m += gridDim.x, ++t) {
+      const uint32_t ob = p.o_bufs == 2 ? t & 1u : 0u, ot = p.o_bufs == 2 ? t >> 1 : t, d = tmem_base + ob * (uint32_t)p.bn;
+      ok = ex_wait_warp(&o_empty[ob], (ot & 1u) ^ 1u, abort_flag, p.spin_limit);
+      for (int c = 0; c < p.chunks && ok; ++c, ++g) {
+        ok = ex_wait_warp(&p_full[g & 1u], (g >> 1) & 1u, abort_flag, p.spin_limit);
+        const uint32_t pt = tmem_base + s_col + (g & 1u) * FU_S_COLS;
+        for (int kb0 = 0; kb0 < p.chunk_hidden / 64 && ok; kb0 += p.kb2) {
+          ok = ex_wait_warp(&w2_full[stage], phase, abort_flag, p.spin_limit);
+          if (!ok) break;
+          tc_fence_after();
+          const uint64_t b_d = make_desc_mn(smem_u32(w2_s) + stage * (uint32_t)p.stage2, 8192);
+          for (int i = 0; i < p.kb2; ++i) {
+#pragma unroll
+            for (int k = 0; k < 4; ++k)   // where the warps that make P leave it: 32 columns of theirs hold 64 hidden columns, gated 16 hold 32
+              ex_mma_tmem_a(lead, d, GATED ? pt + (k >> 1) * 32 + (k & 1) * 8 : pt + (kb0 + i) * 64 + k * 8, b_d + i * (p.bn * 8) + k * 128, idesc,
+                            (c | kb0 | i | k) != 0);
+          }
+          ex_commit(lead, &w2_empty[stage]);
+          if (++stage == (uint32_t)p.stages2) { stage = 0; phase ^= 1u; }
+        }
+        if (ok) ex_commit(lead, &s_free[g & 1u]);
+      }
+      if (ok) ex_commit(lead, &o_full[ob]);
+    }
+    ex_commit(lead, &mma_done[1]);
+    mbar_drain(&mma_done[1], 0);
   } else if (warp < FU_P_WARP0 + FU_P_WARPS) {
     // ------------------------------------------------------------------ P: a thread per row, 64 accumulator columns a warp (gated: 32 of the gate, 32 gated)
     const int quarter = warp & 3, sub = (warp - FU_P_WARP0) >> 2;   // a warp may only touch TMEM lanes [32 * (warp % 4), +32)
@@ -492,7 +513,7 @@ it_status it_launch_experts_fused(const it_experts_args &a, const it_experts_pla
   p.x = a.x; p.x_scale = a.x_scale; p.w_scale = d.w1_scale; p.b1 = d.b1; p.b2 = d.b2; p.weights = a.weights;
   p.top_k = d.top_k; p.n_experts = d.n_experts; p.in_bytes = d.in_dim * elem; p.kbx = (d.in_dim + BK - 1) / BK;
   p.hidden = d.hidden_dim; p.n1 = a.n1; p.chunk_hidden = gated ? 64 : 128; p.chunks = (d.hidden_dim + p.chunk_hidden - 1) / p.chunk_hidden;
-  p.out = d.out_dim; p.bn = (d.out_dim + 63) / 64 * 64; p.halves = p.bn > 128 ? 2 : 1; p.o_bufs = p.bn <= 128 ? 2 : 1;
+  p.out = d.out_dim; p.bn = (d.out_dim + 63) / 64 * 64; p.o_bufs = p.bn <= 128 ? 2 : 1;
   p.act = d.act; p.dst = dst; p.status = a.status; p.spin_limit = spin_limit ? spin_limit : TC_SPIN_LIMIT; p.no_loads = no_loads;
 
   const cuuint64_t d1[3] = {(cuuint64_t)a.n1, (cuuint64_t)d.in_dim, (cuuint64_t)d.n_experts}, s1[2] = {(cuuint64_t)a.n1 * elem, (cuuint64_t)a.n1 * elem * (cuuint64_t)d.in_dim};
@@ -502,11 +523,14 @@ it_status it_launch_experts_fused(const it_experts_args &a, const it_experts_pla
   IT_TRY(encode(&m1, eight, d.W1, 3, d1, s1, b1));
   IT_TRY(encode(&m2, false, d.W2, 3, d2, s2, b2));
 
-  const int fixed = FU_O_WARPS * (direct ? 4096 : 2048) + FU_P_WARPS * 2 * (eight ? 128 : 64) * 4 + FU_O_WARPS * 256 * 4 + TC_BM * 4 + (2 * FU_MAX_STAGES + 14) * 8;
-  p.x_slots = 2;
-  p.stages = (227 * 1024 - fixed - p.x_slots * p.kbx * FU_XBLOCK) / FU_STAGE;
-  if (p.stages > FU_MAX_STAGES) p.stages = FU_MAX_STAGES;
-  const int smem = fixed + p.x_slots * p.kbx * FU_XBLOCK + p.stages * FU_STAGE;
+  const int fixed = FU_O_WARPS * (direct ? 4096 : 2048) + FU_P_WARPS * 2 * (eight ? 128 : 64) * 4 + FU_O_WARPS * 256 * 4 + TC_BM * 4 + (4 * FU_MAX_STAGES + 17) * 8;
+  // a stage of weights: two k-blocks (W2: of up to 128 columns), or the one there is
+  p.kb1 = p.kbx < 2 ? 1 : 2; p.stage1 = p.kb1 * FU_XBLOCK;
+  p.kb2 = gated || p.bn > 128 ? 1 : 2; p.stage2 = p.kb2 * p.bn * TC_KBLOCK_BYTES;
+  p.x_slots = p.kbx <= 2 ? 2 : 1;
+  const int room = (227 * 1024 - fixed - p.x_slots * p.kbx * FU_XBLOCK) / (p.stage1 + p.stage2);
+  p.stages1 = p.stages2 = room < FU_MAX_STAGES ? room : FU_MAX_STAGES;
+  const int smem = fixed + p.x_slots * p.kbx * FU_XBLOCK + p.stages1 * p.stage1 + p.stages2 * p.stage2;
   const int grid = (int)(q.tiles_max < a.sms ? q.tiles_max : a.sms);
   const double places = (double)a.n * d.top_k;
   const double flops = 2.0 * places * ((double)d.in_dim * a.n1 + (double)d.hidden_dim * d.out_dim), bytes = places * (p.in_bytes + (double)d.out_dim * (direct ? 2 : 4));
