@@ -4,10 +4,10 @@
 // Gated: a chunk is 64 columns of the gate and the 64 that it gates.  With the hidden row in memory the two products of 1M vertices, 2 of 16,
 // 128-512-128, moved 6 GB, 4 of them hidden rows, and took 1160 us at 5.2 TB/s.
 //
-// Warps: 0 fetches rows of X by place (16-byte asynchronous copies, a tile ahead), 1 the weights (TMA, W1 of chunk g + 1 before W2 of chunk g), 2 and 3
-// issue the MMAs of S and of O, 4-11 make P, 12-15 store O: sixteen, which leave 128 registers a thread.  S and O have a warp each because a
-// wait costs an issuing warp some 160 cycles and a commit 95, as much together as the products of a chunk (128 columns in and out) take: issued by one
-// warp, with a stage of weights per k-block, a chunk took 3300 cycles.
+// Warps: 0 and 1 fetch W1 and W2 (TMA), 2 and 3 issue the MMAs of S and of O, 4-11 make P, 12-15 fetch the rows of X by place (16-byte asynchronous
+// copies) and store O: sixteen, which leave 128 registers a thread.  Nearly every one of these was the slowest once: one issuing warp for S and O with
+// a stage of weights per k-block 3300 cycles a chunk (a wait costs it some 160, a commit 95), one warp for the rows 2500 (100 a copy), one
+// producer for both weights 570 of waiting for W2 behind W1, rows fetched by the warps that make P 400.
 // S and P are buffered twice, O twice where it has at most 128 columns.
 // Waits are bounded as in the other products.
 #include <type_traits>
@@ -16,7 +16,7 @@
 
 namespace {
 
-constexpr int FU_FETCH_WARP = 0, FU_W_WARP = 1, FU_S_WARP = 2, FU_MMA_WARP = 3 /* of O */, FU_P_WARP0 = 4, FU_P_WARPS = 8, FU_O_WARP0 = 12, FU_O_WARPS = 4;
+constexpr int FU_W1_WARP = 0, FU_W2_WARP = 1, FU_S_WARP = 2, FU_MMA_WARP = 3 /* of O */, FU_P_WARP0 = 4, FU_P_WARPS = 8, FU_O_WARP0 = 12, FU_O_WARPS = 4;
 constexpr int FU_THREADS = 32 * (FU_O_WARP0 + FU_O_WARPS);
 constexpr int FU_XBLOCK = TC_BM * TC_KBLOCK_BYTES;
 constexpr int FU_MAX_STAGES = 4;     // of either ring of weights
@@ -47,7 +47,7 @@ expert_fused_kernel(const __grid_constant__ CUtensorMap map_w1, const __grid_con
   extern __shared__ __align__(1024) unsigned char base[];
   const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
   constexpr int BK1 = EIGHT ? 128 : 64;              // elements of a k-block of X, and columns of a panel of W1
-  constexpr int STAGING = DIRECT ? 4096 : 2048;      // per storing warp: 32 rows of 128 or 64 bytes
+  constexpr int STAGING = 4096;                      // per storing warp: 32 rows of 128 bytes
   unsigned char *x_s = base;
   unsigned char *w1_s = x_s + (size_t)p.x_slots * p.kbx * FU_XBLOCK;
   unsigned char *w2_s = w1_s + (size_t)p.stages1 * p.stage1;
@@ -78,10 +78,10 @@ expert_fused_kernel(const __grid_constant__ CUtensorMap map_w1, const __grid_con
       mbar_init(&w2_empty[s], 1);
     }
     for (int a = 0; a < 2; ++a) {
-      mbar_init(&x_full[a], 32);
+      mbar_init(&x_full[a], 32 * FU_O_WARPS);
+      mbar_init(&x_empty[a], 1);
       mbar_init(&s_free[a], 1);
       mbar_init(&mma_done[a], 1);
-      mbar_init(&x_empty[a], 1);
       mbar_init(&s_full[a], 1);
       mbar_init(&p_full[a], FU_P_WARPS);
       mbar_init(&o_full[a], 1);
@@ -103,110 +103,41 @@ expert_fused_kernel(const __grid_constant__ CUtensorMap map_w1, const __grid_con
   int m_tiles = *p.n_tiles;
   m_tiles = m_tiles < p.tiles_max ? m_tiles : p.tiles_max;
 
-  if (warp == FU_FETCH_WARP) {
-    // ------------------------------------------------------------------ rows of X, by place
-    constexpr int GROUPS = TC_BM / 32;   // of 32 rows
-    const int chunk = lane & 7;
-    uint32_t slot = 0, phase = 0;
-    int place_next[GROUPS];
-    auto look = [&](int m) {
-#pragma unroll
-      for (int q = 0; q < GROUPS; ++q)
-        if (m < m_tiles) place_next[q] = p.order[(int64_t)m * TC_BM + q * 32 + lane];
-    };
-    look(blockIdx.x);
-    for (int m = blockIdx.x; m < m_tiles && !p.no_loads; m += gridDim.x) {
-      int row[GROUPS];
-#pragma unroll
-      for (int q = 0; q < GROUPS; ++q) row[q] = place_next[q] < 0 ? -1 : place_next[q] / p.top_k;
-      look(m + gridDim.x);
-      const int ok = lane == 0 ? mbar_wait(&x_empty[slot], phase ^ 1u, abort_flag, p.spin_limit, FU_BACKOFF) : 1;
-      if (!__shfl_sync(0xffffffffu, ok, 0)) break;
-      const uint32_t to = smem_u32(x_s) + slot * (uint32_t)(p.kbx * FU_XBLOCK);
-      // (addresses of eight rows first, then their copies one behind the other: a warp that makes them row by row waits for itself)
-#pragma unroll
-      for (int q = 0; q < GROUPS; ++q) {
-        const unsigned char *src[8];
-        uint32_t bytes[8];
-#pragma unroll
-        for (int i = 0; i < 8; ++i) {
-          const int r = __shfl_sync(0xffffffffu, row[q], i * 4 + (lane >> 3));
-          src[i] = reinterpret_cast<const unsigned char *>(p.x) + (int64_t)(r < 0 ? 0 : r) * p.in_bytes + chunk * 16;
-          bytes[i] = r < 0 ? 0u : 16u;
-        }
-        const uint32_t dst = to + (uint32_t)q * 4096u + (uint32_t)(lane >> 3) * TC_KBLOCK_BYTES;
-        const uint32_t even = dst + (uint32_t)((chunk ^ (lane >> 3)) << 4), odd = dst + (uint32_t)((chunk ^ (4 + (lane >> 3))) << 4);
-        for (int kb = 0; kb < p.kbx; ++kb) {
-          const bool in = kb * TC_KBLOCK_BYTES + chunk * 16 < p.in_bytes;
-#pragma unroll
-          for (int i = 0; i < 8; ++i)
-            cp_async16(((i & 1) ? odd : even) + (uint32_t)(i * 512) + (uint32_t)kb * FU_XBLOCK, in ? src[i] + kb * TC_KBLOCK_BYTES : src[i] - chunk * 16, in ? bytes[i] : 0u);
-        }
-      }
-      cp_async_arrive(&x_full[slot]);
-      if (++slot == (uint32_t)p.x_slots) { slot = 0; phase ^= 1u; }
-    }
-    __syncwarp();
-    cp_async_wait_all();
-  } else if (warp == FU_W_WARP) {
-    // ------------------------------------------------------------------ weights: W1 of a chunk, then W2 of the one before it; a ring each
-    struct Ring { uint64_t *full, *empty; uint32_t stages, stage, phase; bool came_round; };
-    Ring r1{w1_full, w1_empty, (uint32_t)p.stages1, 0, 0, false}, r2{w2_full, w2_empty, (uint32_t)p.stages2, 0, 0, false};
-    bool ok = !p.no_loads;
-    auto arm = [&](Ring &r, uint32_t bytes) {   // a free stage
-      if (lane == 0) {
-        ok = mbar_wait(&r.empty[r.stage], r.phase ^ 1u, abort_flag, p.spin_limit, FU_BACKOFF);
-        if (ok) mbar_arrive_expect_tx(&r.full[r.stage], bytes);
-      }
-      ok = __shfl_sync(0xffffffffu, (int)ok, 0);
-      return ok;
-    };
-    auto advance = [&](Ring &r) {
-      __syncwarp();
-      if (++r.stage == r.stages) { r.stage = 0; r.phase ^= 1u; r.came_round = true; }
-    };
-    auto first = [&](int e, int c) {
-      constexpr int PANELS = 128 / BK1;
-      for (int kb0 = 0; kb0 < p.kbx; kb0 += p.kb1) {
-        const int n = p.kbx - kb0 < p.kb1 ? p.kbx - kb0 : p.kb1;
-        if (!arm(r1, (uint32_t)n * FU_XBLOCK)) return;
-        unsigned char *to = w1_s + (size_t)r1.stage * p.stage1;
-        if (lane < n * PANELS) {
-          const int kb = lane / PANELS, panel = lane % PANELS, col = GATED ? panel * p.hidden + c * 64 : c * 128 + panel * BK1;
-          tma_load_3d(to + lane * BK1 * TC_KBLOCK_BYTES, &map_w1, col, (kb0 + kb) * BK1, e, &w1_full[r1.stage]);
-        }
-        advance(r1);
-      }
-    };
-    auto second = [&](int e, int c) {
-      const int panels = p.bn / 64;
-      for (int kb0 = 0; kb0 < p.chunk_hidden / 64; kb0 += p.kb2) {
-        if (!arm(r2, (uint32_t)p.stage2)) return;
-        unsigned char *to = w2_s + (size_t)r2.stage * p.stage2;
-        if (lane < p.kb2 * panels) {
-          const int kb = lane / panels, panel = lane % panels;
-          tma_load_3d(to + lane * 8192, &map_w2, panel * 64, c * p.chunk_hidden + (kb0 + kb) * 64, e, &w2_full[r2.stage]);
-        }
-        advance(r2);
-      }
-    };
-    int e_before = -1;
+  if (warp == FU_W1_WARP || warp == FU_W2_WARP) {
+    // ------------------------------------------------------------------ weights: one of the two, a ring each
+    const bool first = warp == FU_W1_WARP;
+    uint64_t *full = first ? w1_full : w2_full, *empty = first ? w1_empty : w2_empty;
+    const uint32_t stages = (uint32_t)(first ? p.stages1 : p.stages2), stage_bytes = (uint32_t)(first ? p.stage1 : p.stage2);
+    unsigned char *ring = first ? w1_s : w2_s;
+    const int kbs = first ? p.kbx : p.chunk_hidden / 64, per_stage = first ? p.kb1 : p.kb2;   // k-blocks of a chunk, of a stage
+    const int panels = first ? 128 / BK1 : p.bn / 64, block_bytes = first ? FU_XBLOCK : p.bn * TC_KBLOCK_BYTES, panel_bytes = block_bytes / panels;
+    const int kb_lane = lane / panels, panel = lane % panels;
+    uint32_t stage = 0, phase = 0;
+    bool ok = !p.no_loads, came_round = false;
     int e_next = (int)blockIdx.x < m_tiles ? p.tile_expert[blockIdx.x] : 0;
     for (int m = blockIdx.x; m < m_tiles && ok; m += gridDim.x) {
       const int e = e_next;
       if (m + (int)gridDim.x < m_tiles) e_next = p.tile_expert[m + gridDim.x];
-      for (int c = 0; c < p.chunks && ok; ++c) {
-        first(e, c);
-        if (ok && (c > 0 || e_before >= 0)) second(c > 0 ? e : e_before, c > 0 ? c - 1 : p.chunks - 1);
-      }
-      e_before = e;
+      for (int c = 0; c < p.chunks && ok; ++c)
+        for (int kb0 = 0; kb0 < kbs; kb0 += per_stage) {
+          const int n = kbs - kb0 < per_stage ? kbs - kb0 : per_stage;
+          if (lane == 0) {
+            ok = mbar_wait(&empty[stage], phase ^ 1u, abort_flag, p.spin_limit, FU_BACKOFF);
+            if (ok) mbar_arrive_expect_tx(&full[stage], (uint32_t)(n * block_bytes));
+          }
+          ok = __shfl_sync(0xffffffffu, (int)ok, 0);
+          if (!ok) break;
+          if (kb_lane < n) {
+            unsigned char *to = ring + (size_t)stage * stage_bytes + lane * panel_bytes;
+            if (first) tma_load_3d(to, &map_w1, GATED ? panel * p.hidden + c * 64 : c * 128 + panel * BK1, (kb0 + kb_lane) * BK1, e, &full[stage]);
+            else tma_load_3d(to, &map_w2, panel * 64, c * p.chunk_hidden + (kb0 + kb_lane) * 64, e, &full[stage]);
+          }
+          __syncwarp();
+          if (++stage == stages) { stage = 0; phase ^= 1u; came_round = true; }
+        }
     }
-    if (ok && e_before >= 0) second(e_before, p.chunks - 1);
     __syncwarp();
-    if (lane == 0) {
-      ring_drain(w1_full, r1.stages, r1.stage, r1.phase, r1.came_round);
-      ring_drain(w2_full, r2.stages, r2.stage, r2.phase, r2.came_round);
-    }
+    if (lane == 0) ring_drain(full, stages, stage, phase, came_round);
   } else if (warp == FU_S_WARP) {
     // ------------------------------------------------------------------ S = X W1: chunk number g of this CTA into buffer g % 2
     const uint32_t fmt = EIGHT ? 0u : 1u, lead = lane == 0;
@@ -371,20 +302,18 @@ expert_fused_kernel(const __grid_constant__ CUtensorMap map_w1, const __grid_con
           pack(v, w, false);
           tmem_st16(st + (uint32_t)(sub * 32), w);
         } else {
-          uint32_t r[32], w[16];
-          uint64_t v[16];
-          tmem_ld32(st + (uint32_t)(sub * 64), r);
-          tmem_ld_wait();
-          scaled(r, 0, v);
-          tmem_ld32(st + (uint32_t)(sub * 64 + 32), r);   // (all 64 are read before P takes the place of the first 32)
-          if (p.act != IT_ACT_RELU) expert_act(v, p.act);
-          pack(v, w, true);
-          tmem_ld_wait();
-          tmem_st16(st + (uint32_t)(sub * 64), w);
-          scaled(r, 32, v);
-          if (p.act != IT_ACT_RELU) expert_act(v, p.act);
-          pack(v, w, true);
-          tmem_st16(st + (uint32_t)(sub * 64 + 16), w);
+          // (P of the first 32 columns takes the place of 16 of them, which have been read)
+#pragma unroll
+          for (int h = 0; h < 2; ++h) {
+            uint32_t r[32], w[16];
+            uint64_t v[16];
+            tmem_ld32(st + (uint32_t)(sub * 64 + h * 32), r);
+            tmem_ld_wait();
+            scaled(r, h * 32, v);
+            if (p.act != IT_ACT_RELU) expert_act(v, p.act);
+            pack(v, w, true);
+            tmem_st16(st + (uint32_t)(sub * 64 + h * 16), w);
+          }
         }
         tmem_st_wait();
         tc_fence_before();
@@ -393,18 +322,53 @@ expert_fused_kernel(const __grid_constant__ CUtensorMap map_w1, const __grid_con
       }
     }
   } else {
-    // ------------------------------------------------------------------ O: rows of the result, through a staging tile
+    // ------------------------------------------------------------------ rows of X, by place; and O: rows of the result, through a staging tile
     const int quarter = warp & 3;
-    constexpr int ESIZE = DIRECT ? 2 : 4, ROW = DIRECT ? 128 : 64, PIECES = ROW / 16, AT_ONCE = 32 / PIECES;
+    constexpr int ESIZE = DIRECT ? 2 : 4, ROW = 128;
     const uint32_t stage_s = smem_u32(staging) + (uint32_t)(warp - FU_O_WARP0) * STAGING;
-    const int row0 = lane / PIECES, piece = lane % PIECES;
-    const uint32_t put = stage_s + (uint32_t)lane * ROW + (uint32_t)((DIRECT ? lane & 7 : (lane >> 1) & 3) << 4);
+    const int row0 = lane >> 3, piece = lane & 7;
+    const uint32_t put = stage_s + (uint32_t)lane * ROW + (uint32_t)((lane & 7) << 4);
+    const uint32_t row4 = 4u * (uint32_t)p.out * ESIZE;
     float *bias = o_consts + (warp - FU_O_WARP0) * 256;
     int32_t *places = o_place + quarter * 32;
-    uint32_t t = 0;
-    for (int m = blockIdx.x; m < m_tiles; m += gridDim.x, ++t) {
+    // 32 rows of tile number t into slot t % x_slots.  Two slots: tile t + 2 once O of tile t is there, whose rows are read then; one: tile t + 1
+    // once the last S of tile t is.
+    int x_place = -1;   // of the rows that are fetched next
+    auto look_x = [&](int m) {
+      if (m < m_tiles) x_place = p.order[(int64_t)m * TC_BM + quarter * 32 + lane];
+    };
+    auto fetch_x = [&](uint32_t slot) {
+      const int row = x_place < 0 ? -1 : x_place / p.top_k;
+      const uint32_t to = smem_u32(x_s) + slot * (uint32_t)(p.kbx * FU_XBLOCK) + (uint32_t)(quarter * 32 + row0) * TC_KBLOCK_BYTES;
+      const uint32_t even = to + (uint32_t)((piece ^ row0) << 4), odd = to + (uint32_t)((piece ^ (4 + row0)) << 4);
+      const unsigned char *src[8];
+      uint32_t bytes[8];
+#pragma unroll
+      for (int i = 0; i < 8; ++i) {
+        const int r = __shfl_sync(0xffffffffu, row, i * 4 + row0);
+        src[i] = reinterpret_cast<const unsigned char *>(p.x) + (int64_t)(r < 0 ? 0 : r) * p.in_bytes + piece * 16;
+        bytes[i] = r < 0 ? 0u : 16u;
+      }
+      for (int kb = 0; kb < p.kbx; ++kb) {
+        const bool in = kb * TC_KBLOCK_BYTES + piece * 16 < p.in_bytes;
+#pragma unroll
+        for (int i = 0; i < 8; ++i)
+          cp_async16(((i & 1) ? odd : even) + (uint32_t)(i * 512) + (uint32_t)kb * FU_XBLOCK, in ? src[i] + kb * TC_KBLOCK_BYTES : src[i] - piece * 16, in ? bytes[i] : 0u);
+      }
+      cp_async_arrive(&x_full[slot]);
+    };
+    const int stride = (int)gridDim.x, ahead = p.x_slots;   // tiles that the rows are ahead
+    for (int i = 0; i < ahead; ++i)
+      if ((int64_t)blockIdx.x + (int64_t)i * stride < m_tiles && !p.no_loads) {
+        look_x(blockIdx.x + i * stride);
+        fetch_x((uint32_t)i);
+      }
+    uint32_t t = 0, x_slot = 0, x_phase = 0;
+    for (int m = blockIdx.x; m < m_tiles; m += stride, ++t) {
       const int64_t pos0 = (int64_t)m * TC_BM + quarter * 32;
       const int place = p.order[pos0 + lane], e = p.tile_expert[m];
+      const bool more = (int64_t)m + (int64_t)ahead * stride < m_tiles;
+      if (more) look_x(m + ahead * stride);
       const float weight = DIRECT && place >= 0 ? p.weights[place] : 1.f;
       const uint64_t weight2 = pack2(__float_as_uint(weight), __float_as_uint(weight));
       __syncwarp();
@@ -416,22 +380,29 @@ expert_fused_kernel(const __grid_constant__ CUtensorMap map_w1, const __grid_con
       }
       __syncwarp();
       const uint32_t ob = p.o_bufs == 2 ? t & 1u : 0u, ot = p.o_bufs == 2 ? t >> 1 : t;
-      const bool ok = mbar_wait(&o_full[ob], ot & 1u, abort_flag, p.spin_limit, 4 * FU_BACKOFF);
+      bool ok = true;
+      if (ahead == 2) ok = mbar_wait(&o_full[ob], ot & 1u, abort_flag, p.spin_limit, 4 * FU_BACKOFF);
+      if (ok && more) ok = mbar_wait(&x_empty[x_slot], x_phase, abort_flag, p.spin_limit, FU_BACKOFF);
+      if (!__all_sync(0xffffffffu, ok)) break;
+      if (more) fetch_x(x_slot);
+      if (++x_slot == (uint32_t)p.x_slots) { x_slot = 0; x_phase ^= 1u; }
+      if (ahead != 2) ok = mbar_wait(&o_full[ob], ot & 1u, abort_flag, p.spin_limit, 4 * FU_BACKOFF);
       if (!__all_sync(0xffffffffu, ok)) break;
       tc_fence_after();
       const uint32_t taddr = tmem_base + ((uint32_t)(quarter * 32) << 16) + ob * (uint32_t)p.bn;
+      unsigned char *to = reinterpret_cast<unsigned char *>(p.dst) + (DIRECT ? 0 : (pos0 + row0) * p.out) * ESIZE + piece * 16;
+      const unsigned real = __ballot_sync(0xffffffffu, place >= 0) >> row0;   // bit 4 i: whether the i-th row that this lane stores parts of is one
       auto flush = [&](int c, bool both) {   // the staged pieces of rows, from column c on
         __syncwarp();
-        const bool in = c + piece * (16 / ESIZE) < p.out && (!DIRECT || both || piece < 4);
+        const bool in = c + piece * (16 / ESIZE) < p.out && (both || piece < 4);
+        const uint32_t even = stage_s + (uint32_t)row0 * ROW + (uint32_t)((piece ^ row0) << 4), odd = stage_s + (uint32_t)row0 * ROW + (uint32_t)((piece ^ (4 + row0)) << 4);
+        uint4 d[8];
 #pragma unroll
-        for (int i = 0; i < 32 / AT_ONCE; ++i) {
-          const int row = AT_ONCE * i + row0, at = places[row];
-          uint4 d;
-          asm volatile("ld.shared.v4.b32 {%0, %1, %2, %3}, [%4];" : "=r"(d.x), "=r"(d.y), "=r"(d.z), "=r"(d.w)
-                       : "r"(stage_s + (uint32_t)row * ROW + (uint32_t)((piece ^ (DIRECT ? row & 7 : (row >> 1) & 3)) << 4)) : "memory");
-          if (in && at >= 0)
-            *reinterpret_cast<uint4 *>(reinterpret_cast<unsigned char *>(p.dst) + ((DIRECT ? (int64_t)at : pos0 + row) * p.out + c) * ESIZE + piece * 16) = d;
-        }
+        for (int i = 0; i < 8; ++i)
+          asm volatile("ld.shared.v4.b32 {%0, %1, %2, %3}, [%4];" : "=r"(d[i].x), "=r"(d[i].y), "=r"(d[i].z), "=r"(d[i].w) : "r"(((i & 1) ? odd : even) + 512u * i) : "memory");
+#pragma unroll
+        for (int i = 0; i < 8; ++i)
+          if (in && ((real >> (4 * i)) & 1u)) *reinterpret_cast<uint4 *>(to + (DIRECT ? (int64_t)places[4 * i + row0] * p.out * ESIZE : (int64_t)((uint64_t)i * row4)) + c * ESIZE) = d[i];
         __syncwarp();
       };
       for (int c = 0; c < p.out; c += 32) {
@@ -459,21 +430,19 @@ expert_fused_kernel(const __grid_constant__ CUtensorMap map_w1, const __grid_con
           if (half == 1 || c + 32 >= p.out) flush(c - 32 * half, half == 1);
         } else {
 #pragma unroll
-          for (int h = 0; h < 2; ++h) {
-            if (c + 16 * h >= p.out) break;
-#pragma unroll
-            for (int i = 0; i < 4; ++i) {
-              const float2 f0 = unpack2(v[8 * h + 2 * i]), f1 = unpack2(v[8 * h + 2 * i + 1]);
-              st_shared_v4(put ^ (16u * i), __float_as_uint(f0.x), __float_as_uint(f0.y), __float_as_uint(f1.x), __float_as_uint(f1.y));
-            }
-            flush(c + 16 * h, false);
+          for (int i = 0; i < 8; ++i) {
+            const float2 f0 = unpack2(v[2 * i]), f1 = unpack2(v[2 * i + 1]);
+            st_shared_v4(put ^ (16u * i), __float_as_uint(f0.x), __float_as_uint(f0.y), __float_as_uint(f1.x), __float_as_uint(f1.y));
           }
+          flush(c, true);
         }
       }
       tc_fence_before();
       __syncwarp();
       if (lane == 0) mbar_arrive(&o_empty[ob]);
     }
+    __syncwarp();
+    cp_async_wait_all();
   }
 
   // ------------------------------------------------------------------ teardown
@@ -523,7 +492,7 @@ it_status it_launch_experts_fused(const it_experts_args &a, const it_experts_pla
   IT_TRY(encode(&m1, eight, d.W1, 3, d1, s1, b1));
   IT_TRY(encode(&m2, false, d.W2, 3, d2, s2, b2));
 
-  const int fixed = FU_O_WARPS * (direct ? 4096 : 2048) + FU_P_WARPS * 2 * (eight ? 128 : 64) * 4 + FU_O_WARPS * 256 * 4 + TC_BM * 4 + (4 * FU_MAX_STAGES + 17) * 8;
+  const int fixed = FU_O_WARPS * 4096 + FU_P_WARPS * 2 * (eight ? 128 : 64) * 4 + FU_O_WARPS * 256 * 4 + TC_BM * 4 + (4 * FU_MAX_STAGES + 17) * 8;
   // a stage of weights: two k-blocks (W2: of up to 128 columns), or the one there is
   p.kb1 = p.kbx < 2 ? 1 : 2; p.stage1 = p.kb1 * FU_XBLOCK;
   p.kb2 = gated || p.bn > 128 ? 1 : 2; p.stage2 = p.kb2 * p.bn * TC_KBLOCK_BYTES;
