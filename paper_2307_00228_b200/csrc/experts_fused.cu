@@ -150,11 +150,11 @@ expert_fused_kernel(const __grid_constant__ CUtensorMap map_w1, const __grid_con
       asm volatile("fence.proxy.async.shared::cta;" ::: "memory");   // the rows were written by other threads' copies
       const uint64_t x_d = make_desc(smem_u32(x_s) + slot * (uint32_t)(p.kbx * FU_XBLOCK));
       for (int c = 0; c < p.chunks && ok; ++c, ++g) {
-        // the chunk before the last one's P lies where this S goes
-        if (g >= 2) ok = ex_wait_warp(&s_free[g & 1u], ((g >> 1) & 1u) ^ 1u, abort_flag, p.spin_limit);
         const uint32_t d = tmem_base + s_col + (g & 1u) * FU_S_COLS;
         for (int kb0 = 0; kb0 < p.kbx && ok; kb0 += p.kb1) {
           ok = ex_wait_warp(&w1_full[stage], phase, abort_flag, p.spin_limit);
+          // the chunk before the last one's P lies where this S goes (waited for last: the weights are long there, and a wait takes its time)
+          if (ok && kb0 == 0 && g >= 2) ok = ex_wait_warp(&s_free[g & 1u], ((g >> 1) & 1u) ^ 1u, abort_flag, p.spin_limit);
           if (!ok) break;
           tc_fence_after();
           const uint64_t b_d = make_desc_mn(smem_u32(w1_s) + stage * (uint32_t)p.stage1, BK1 * TC_KBLOCK_BYTES);
@@ -183,10 +183,10 @@ expert_fused_kernel(const __grid_constant__ CUtensorMap map_w1, const __grid_con
       const uint32_t ob = p.o_bufs == 2 ? t & 1u : 0u, ot = p.o_bufs == 2 ? t >> 1 : t, d = tmem_base + ob * (uint32_t)p.bn;
       ok = ex_wait_warp(&o_empty[ob], (ot & 1u) ^ 1u, abort_flag, p.spin_limit);
       for (int c = 0; c < p.chunks && ok; ++c, ++g) {
-        ok = ex_wait_warp(&p_full[g & 1u], (g >> 1) & 1u, abort_flag, p.spin_limit);
         const uint32_t pt = tmem_base + s_col + (g & 1u) * FU_S_COLS;
         for (int kb0 = 0; kb0 < p.chunk_hidden / 64 && ok; kb0 += p.kb2) {
           ok = ex_wait_warp(&w2_full[stage], phase, abort_flag, p.spin_limit);
+          if (ok && kb0 == 0) ok = ex_wait_warp(&p_full[g & 1u], (g >> 1) & 1u, abort_flag, p.spin_limit);
           if (!ok) break;
           tc_fence_after();
           const uint64_t b_d = make_desc_mn(smem_u32(w2_s) + stage * (uint32_t)p.stage2, 8192);
