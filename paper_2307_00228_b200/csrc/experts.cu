@@ -274,7 +274,7 @@ it_status check(const it_experts_desc *d, int64_t n) {
              "widths must be multiples of 8, rows of e4m3 of 16 (in %d, hidden %d, out %d)", d->in_dim, d->hidden_dim, d->out_dim);
   IT_REQUIRE(d->in_dim <= kMaxDim && d->hidden_dim <= kMaxDim && d->out_dim <= kMaxDim, IT_ERR_UNSUPPORTED, "more than %d columns", kMaxDim);
   IT_REQUIRE(d->n_experts <= kMaxExperts, IT_ERR_UNSUPPORTED, "%d experts, at most %d", d->n_experts, kMaxExperts);
-  const int64_t places = INT32_MAX / (d->feat_dtype == IT_F32 ? 3 : 1) - 128 * (int64_t)d->n_experts;
+  const int64_t places = INT32_MAX / (d->feat_dtype == IT_F32 ? 3 : 1) - 256 * (int64_t)d->n_experts;
   IT_REQUIRE(places > 0 && n <= places / d->top_k, IT_ERR_UNSUPPORTED, "%lld vertices with %d places each: too many rows for 32 bits", (long long)n, d->top_k);
   return IT_OK;
 }
@@ -282,8 +282,24 @@ it_status check(const it_experts_desc *d, int64_t n) {
 // Few places keep the form by place.  FEW_PLACES
 constexpr int64_t kFewPlaces = 64;
 
+// Products that are not fused and take their rows more than once, for several tiles of columns, have them put in order first: fetched by place, a
+// k-block of 128 rows takes 1000 cycles, twice the product's (40k vertices, 4 of 32, 768-1024 gated: ROWSFIG).
+bool rows_in_order(const it_experts_desc &d) {
+  if (it_experts_fused(d)) return false;
+  const int cols = d.hidden_dim > 0 ? d.hidden_dim : d.out_dim;
+  return d.feat_dtype == IT_F32 || cols > (d.gated ? 128 : 256);
+}
+
+// Two CTAs share the weights of 256 places: half the bytes of them, for products that take rows in order, where the padding (128 places of an expert
+// on average) is small.  PAIRS
+bool in_pairs(const it_experts_desc &d, int64_t places) {
+  // (a CTA's half of the columns is whole panels of 64, in e4m3 of 128)
+  const bool narrow = d.in_dtype == IT_E4M3 && (d.hidden_dim > 0 ? d.hidden_dim * (d.gated ? 2 : 1) : d.out_dim) <= 128;
+  return rows_in_order(d) && !narrow && places >= 1024 * (int64_t)d.n_experts;
+}
+
 struct ExpertsWs {
-  bool few;
+  bool few, pairs, sorted;
   size_t off_rows;                                   // few: fp32 rows by place
   size_t off_order, off_position, off_tiles, off_counts, off_hidden, off_sums, off_x, off_w1, off_w2;   // (tiles: the number of tiles, then their experts)
   int64_t tiles_max;
@@ -303,7 +319,8 @@ it_status plan(const it_experts_desc *d, int64_t n, ExpertsWs *w) {
     w->off_rows = take((size_t)places * cols * 4);
   } else {
     const bool f32 = d->feat_dtype == IT_F32;
-    w->tiles_max = it_experts_tiles_max(places, d->n_experts);
+    w->pairs = in_pairs(*d, places);
+    w->tiles_max = it_experts_tiles_max(places, d->n_experts, w->pairs);
     const size_t rows = (size_t)w->tiles_max * 128, E = (size_t)d->n_experts, n1 = cols * (d->gated ? 2 : 1);
     w->off_order = take(rows * 4);
     w->off_position = take((size_t)places * 4);
@@ -311,7 +328,8 @@ it_status plan(const it_experts_desc *d, int64_t n, ExpertsWs *w) {
     w->off_counts = take(it_experts_count_words(places, d->n_experts) * 4);
     w->off_hidden = take(d->hidden_dim > 0 && !it_experts_fused(*d) ? rows * cols * (f32 ? 6 : 2) : 0);
     w->off_sums = take(d->top_k > 1 ? rows * (size_t)d->out_dim * 4 : 0);
-    w->off_x = take(f32 ? (size_t)n * d->in_dim * 6 : 0);
+    w->sorted = rows_in_order(*d);
+    w->off_x = take(w->sorted ? rows * (size_t)d->in_dim * (f32 ? 6 : (d->in_dtype == IT_E4M3 ? 1 : 2)) : 0);
     w->off_w1 = take(f32 ? E * d->in_dim * n1 * 6 : 0);
     w->off_w2 = take(f32 ? E * d->hidden_dim * d->out_dim * 6 : 0);
   }
@@ -324,6 +342,7 @@ it_status many_places(const it_experts_args &a, const ExpertsWs &w, char *ws, ui
   const it_experts_desc &d = a.d;
   const bool f32 = d.feat_dtype == IT_F32, two = d.hidden_dim > 0;
   it_experts_plan q{};
+  q.pairs = w.pairs;
   q.order = (int32_t *)(ws + w.off_order); q.position = (int32_t *)(ws + w.off_position); q.n_tiles = (int32_t *)(ws + w.off_tiles);
   q.tile_expert = q.n_tiles + 1; q.counts = (int32_t *)(ws + w.off_counts); q.tiles_max = w.tiles_max;
   IT_TRY(it_launch_experts_plan(a, q, st));
@@ -334,10 +353,14 @@ it_status many_places(const it_experts_args &a, const ExpertsWs &w, char *ws, ui
       parts.src[parts.count] = (const float *)src; parts.dst[parts.count] = (__nv_bfloat16 *)(ws + off); parts.elems[parts.count++] = elems;
       return (const void *)(ws + off);
     };
-    x = part(a.x, w.off_x, a.n * d.in_dim);
+    x = part(a.x, w.off_x, w.tiles_max * 128 * d.in_dim);
+    parts.order = q.order; parts.n_tiles = q.n_tiles; parts.row = d.in_dim; parts.top_k = d.top_k;
     W1 = part(d.W1, w.off_w1, (int64_t)d.n_experts * d.in_dim * a.n1);
     if (two) W2 = part(d.W2, w.off_w2, (int64_t)d.n_experts * d.hidden_dim * d.out_dim);
     IT_TRY(it_launch_experts_parts(parts, a.sms, st));
+  } else if (w.sorted) {
+    IT_TRY(it_launch_experts_rows(a, q, ws + w.off_x, st));
+    x = ws + w.off_x;
   }
   const it_expert_store last = d.top_k > 1 ? IT_EXPERT_SUMS : (f32 ? IT_EXPERT_OUT_F32 : IT_EXPERT_OUT_BF16);
   void *result = d.top_k > 1 ? (void *)(ws + w.off_sums) : a.out;
@@ -347,7 +370,7 @@ it_status many_places(const it_experts_args &a, const ExpertsWs &w, char *ws, ui
   }
   it_expert_gemm g{};
   g.parts = f32 ? 3 : 1; g.spin_limit = spin_limit; g.no_loads = no_loads;
-  g.A = x; g.gather = 1; g.a_rows = a.n; g.W = W1; g.K = d.in_dim; g.w_cols = a.n1; g.cols = two ? d.hidden_dim : d.out_dim;
+  g.A = x; g.gather = !w.sorted; g.a_rows = w.sorted ? w.tiles_max * 128 : a.n; g.W = W1; g.K = d.in_dim; g.w_cols = a.n1; g.cols = two ? d.hidden_dim : d.out_dim;
   g.eight = d.in_dtype == IT_E4M3; g.act = d.act; g.gated = d.gated != 0; g.bias = d.b1; g.w_scale = d.w1_scale; g.x_scale = a.x_scale;
   g.store = two ? (f32 ? IT_EXPERT_PARTS : IT_EXPERT_HIDDEN) : last;
   g.dst = two ? (void *)(ws + w.off_hidden) : result;

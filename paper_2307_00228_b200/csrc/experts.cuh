@@ -17,8 +17,9 @@ struct it_experts_args {
 };
 
 // ----------------------------------------------------------------------------- experts_plan.cu
-// Places sorted by expert: every expert's places fill whole tiles of 128 positions, the last one padded with -1.
+// Places sorted by expert: every expert's places fill whole tiles of 128 positions, the last one padded with -1 (pairs: an even number of tiles).
 struct it_experts_plan {
+  bool pairs;
   int32_t *order;          // [tiles_max * 128] the place at a position, or -1
   int32_t *position;       // [places] where a place went (places of no expert: undefined)
   int32_t *tile_expert;    // [tiles_max]
@@ -26,13 +27,18 @@ struct it_experts_plan {
   int32_t *counts;         // [blocks][n_experts] scratch
   int64_t tiles_max;
 };
-int64_t it_experts_tiles_max(int64_t places, int n_experts);
+int64_t it_experts_tiles_max(int64_t places, int n_experts, bool pairs);
 size_t it_experts_count_words(int64_t places, int n_experts);
 // Also zeroes a.status and, where a vertex has one place only, the rows of `out` whose id is no expert.
 it_status it_launch_experts_plan(const it_experts_args &a, const it_experts_plan &q, cudaStream_t st);
 // fp32 matrices as three bf16 parts each (24 bits: 8 a part, cut off, so that the parts add up exactly): dst[i] is [3, elems[i]].
-struct it_experts_parts { const float *src[3]; __nv_bfloat16 *dst[3]; int64_t elems[3]; int count; };
+struct it_experts_parts {
+  const float *src[3]; __nv_bfloat16 *dst[3]; int64_t elems[3]; int count;
+  const int32_t *order, *n_tiles; int row, top_k;   // src[0]: rows of `row` elements, found by the place at each position
+};
 it_status it_launch_experts_parts(const it_experts_parts &q, int sms, cudaStream_t st);
+// Rows of x in the order of the positions.
+it_status it_launch_experts_rows(const it_experts_args &a, const it_experts_plan &q, void *to, cudaStream_t st);
 
 // ----------------------------------------------------------------------------- experts_tc.cu
 enum it_expert_store {

@@ -47,12 +47,17 @@ __device__ __forceinline__ int block_scan(int v, int *warp_sums, int *total) {
   return s - v + (warp ? warp_sums[warp - 1] : 0);
 }
 
+__device__ __forceinline__ int plan_tiles(const PlanParams &p, int places) {
+  const int tiles = (places + PLAN_TILE - 1) / PLAN_TILE;
+  return p.q.pairs ? (tiles + 1) & ~1 : tiles;
+}
+
 // count[e] (shared): places of every expert -> first position of every expert; tiles, padding and the number of tiles are written.
 // first: as many words of shared memory.
 __device__ void lay_out(const PlanParams &p, int *count, int *first, int *warp_sums) {
   int tiles_before = 0;
   for (int e0 = 0; e0 < p.n_experts; e0 += PLAN_THREADS) {
-    const int e = e0 + threadIdx.x, tiles = e < p.n_experts ? (count[e] + PLAN_TILE - 1) / PLAN_TILE : 0;
+    const int e = e0 + threadIdx.x, tiles = e < p.n_experts ? plan_tiles(p, count[e]) : 0;
     int total;
     const int at = tiles_before + block_scan(tiles, warp_sums, &total);
     if (e < p.n_experts) first[e] = at;
@@ -61,7 +66,7 @@ __device__ void lay_out(const PlanParams &p, int *count, int *first, int *warp_s
   if (threadIdx.x == 0) *p.q.n_tiles = tiles_before;
   __syncthreads();
   for (int e = threadIdx.x >> 5; e < p.n_experts; e += PLAN_THREADS / 32) {
-    const int lane = threadIdx.x & 31, c = count[e], t0 = first[e], t1 = t0 + (c + PLAN_TILE - 1) / PLAN_TILE;
+    const int lane = threadIdx.x & 31, c = count[e], t0 = first[e], t1 = t0 + plan_tiles(p, c);
     for (int t = t0 + lane; t < t1; t += 32) p.q.tile_expert[t] = e;
     for (int64_t i = (int64_t)t0 * PLAN_TILE + c + lane; i < (int64_t)t1 * PLAN_TILE; i += 32) p.q.order[i] = -1;
     __syncwarp();
@@ -189,25 +194,55 @@ __device__ __forceinline__ void split3(float v, uint32_t &a, uint32_t &b, uint32
   c = __float_as_uint(r1 - __uint_as_float(u1 & 0xffff0000u)) >> 16;
 }
 
+// src[0] is gathered where q.order is given: row r of dst[0] is row order[r] / top_k of it (and left as it is for a position of no place).
 __global__ void __launch_bounds__(256) parts_kernel(const it_experts_parts q) {
   it_allow_next();
   it_wait_prior();
   const float *src = q.src[blockIdx.y];
   __nv_bfloat16 *dst = q.dst[blockIdx.y];
-  const int64_t n = q.elems[blockIdx.y];
+  const bool gather = q.order != nullptr && blockIdx.y == 0;
+  int64_t n = q.elems[blockIdx.y];
+  if (gather) {
+    const int64_t met = (int64_t)*q.n_tiles * PLAN_TILE * q.row;
+    n = met < n ? met : n;
+  }
   for (int64_t i = (blockIdx.x * (int64_t)blockDim.x + threadIdx.x) * 4; i < n; i += (int64_t)gridDim.x * blockDim.x * 4) {
-    const float4 v = *reinterpret_cast<const float4 *>(src + i);
+    int64_t from = i;
+    if (gather) {
+      const int64_t r = i / q.row;
+      const int place = q.order[r];
+      if (place < 0) continue;
+      from = (int64_t)(place / q.top_k) * q.row + (i - r * q.row);
+    }
+    const float4 v = *reinterpret_cast<const float4 *>(src + from);
     uint32_t w[3][4];
     split3(v.x, w[0][0], w[1][0], w[2][0]); split3(v.y, w[0][1], w[1][1], w[2][1]);
     split3(v.z, w[0][2], w[1][2], w[2][2]); split3(v.w, w[0][3], w[1][3], w[2][3]);
 #pragma unroll
-    for (int k = 0; k < 3; ++k) *reinterpret_cast<uint2 *>(dst + k * n + i) = make_uint2(w[k][0] | (w[k][1] << 16), w[k][2] | (w[k][3] << 16));
+    for (int k = 0; k < 3; ++k) *reinterpret_cast<uint2 *>(dst + k * q.elems[blockIdx.y] + i) = make_uint2(w[k][0] | (w[k][1] << 16), w[k][2] | (w[k][3] << 16));
+  }
+}
+
+// Rows of x in the order of the positions, 16 bytes a thread.
+__global__ void __launch_bounds__(256) rows_kernel(const uint4 *x, uint4 *to, int row16, int top_k, const int32_t *order, const int32_t *n_tiles, int64_t tiles_max) {
+  it_allow_next();
+  it_wait_prior();
+  int64_t tiles = *n_tiles;
+  tiles = tiles < tiles_max ? tiles : tiles_max;
+  const int64_t n = tiles * PLAN_TILE * row16;
+  for (int64_t i = blockIdx.x * (int64_t)blockDim.x + threadIdx.x; i < n; i += (int64_t)gridDim.x * blockDim.x) {
+    const int64_t r = i / row16;
+    const int place = order[r];
+    if (place >= 0) to[i] = __ldg(x + (int64_t)(place / top_k) * row16 + (i - r * row16));
   }
 }
 
 }  // namespace
 
-int64_t it_experts_tiles_max(int64_t places, int n_experts) { return places / PLAN_TILE + (places < n_experts ? places : n_experts); }
+int64_t it_experts_tiles_max(int64_t places, int n_experts, bool pairs) {
+  const int64_t met = places < n_experts ? places : n_experts;   // each of them rounds up
+  return pairs ? 2 * (places / (2 * PLAN_TILE) + met) : places / PLAN_TILE + met;
+}
 size_t it_experts_count_words(int64_t places, int n_experts) {
   return places <= PLAN_ONE_BLOCK ? 0 : (size_t)plan_blocks(places) * (size_t)n_experts;
 }
@@ -236,5 +271,14 @@ it_status it_launch_experts_parts(const it_experts_parts &q, int sms, cudaStream
   const int64_t blocks = (most / 4 + 255) / 256, cap = (int64_t)sms * 8;
   IT_LAUNCH(IT_K_EXPERT_PARTS, 10.0 * total, 0, st,
             IT_CUDA_TRY(it_launch_pdl(parts_kernel, dim3((unsigned)(blocks < cap ? blocks : cap), q.count), dim3(256), 0, st, q)));
+  return IT_OK;
+}
+
+it_status it_launch_experts_rows(const it_experts_args &a, const it_experts_plan &q, void *to, cudaStream_t st) {
+  const int row16 = a.d.in_dim * (a.d.in_dtype == IT_E4M3 ? 1 : it_dtype_size(a.d.in_dtype)) / 16;
+  const int64_t blocks = (q.tiles_max * PLAN_TILE * row16 + 255) / 256, cap = (int64_t)a.sms * 16;
+  IT_LAUNCH(IT_K_EXPERT_PARTS, 32.0 * a.n * a.d.top_k * row16, 0, st,
+            IT_CUDA_TRY(it_launch_pdl(rows_kernel, dim3((unsigned)(blocks < cap ? blocks : cap)), dim3(256), 0, st, (const uint4 *)a.x, (uint4 *)to, row16, a.d.top_k,
+                                      (const int32_t *)q.order, (const int32_t *)q.n_tiles, q.tiles_max)));
   return IT_OK;
 }

@@ -62,6 +62,17 @@ def test_many_vertices(kind):
     check_experts(c, run_experts(c), device="cuda")
 
 
+@pytest.mark.parametrize("kind,a,h,o,k,gated", [("bf16", 320, 384, 320, 2, False), ("bf16", 272, 136, 264, 3, True), ("bf16", 64, 0, 96, 1, False), ("bf16", 136, 0, 520, 2, False),
+                                                ("eight", 256, 0, 256, 1, False), ("eight", 528, 400, 48, 2, False), ("eight", 144, 272, 512, 1, True),
+                                                ("f32", 40, 0, 72, 1, False), ("f32", 104, 200, 64, 2, True), ("f32", 64, 320, 136, 1, False), ("bf16", 768, 1024, 768, 2, True)])
+@pytest.mark.parametrize("E,n", [(2, 4001), (5, 9000)])
+def test_many_places_an_expert(kind, a, h, o, k, gated, E, n):
+    """Rows of two tiles side by side: odd numbers of tiles, experts of few places, widths that leave a half of the columns empty."""
+    c = experts_case(a + o + E, n, E, k, a, h, o, F32 if kind == "f32" else BF16, eight=kind == "eight", gated=gated, act="silu", masked=0.05, repeat=k > E, skew=0.7 if E == 5 else None)
+    c["ids"][(c["ids"] == 3)] = 0   # an expert without a place
+    check_experts(c, run_experts(c), device="cuda")
+
+
 @pytest.mark.parametrize("E", [1, 300, 1500])
 def test_numbers_of_experts(E):
     c = experts_case(13, 4000, E, 2, 32, 48, 32, BF16, repeat=True)
