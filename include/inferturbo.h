@@ -359,7 +359,7 @@ it_status it_route(const it_route_desc *d, int64_t n, const void *logits, int32_
  *   (fp32, one per column of W1).  W2 is feat_dtype; b1, b2, weights are fp32.
  *   An id outside [0, n_experts) is no expert, whatever its weight; an expert may be named twice.
  *   in_dim, hidden_dim and out_dim are multiples of 8 (in_dim and the width of F's first product of 16 with IT_E4M3), n_experts <= 4096.  The
- *   places of all vertices, padded for every expert, are counted in 32 bits: n * top_k + 256 * n_experts < 2^31 (fp32: a third of that).
+ *   places of all vertices, padded for every expert, are counted in 32 bits: n * top_k + 128 * n_experts < 2^31 (fp32: a third of that).
  *   The products run on the tensor cores with fp32 accumulators (fp32 operands as three bf16 parts, six products: an infinity in them gives
  *   NaN); the hidden row between the two products is stored in feat_dtype, the places of a vertex are added in fp32, in their order, and
  *   rounded once.  Few places take products of their own, in fp32 throughout.

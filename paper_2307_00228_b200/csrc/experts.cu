@@ -274,7 +274,7 @@ it_status check(const it_experts_desc *d, int64_t n) {
              "widths must be multiples of 8, rows of e4m3 of 16 (in %d, hidden %d, out %d)", d->in_dim, d->hidden_dim, d->out_dim);
   IT_REQUIRE(d->in_dim <= kMaxDim && d->hidden_dim <= kMaxDim && d->out_dim <= kMaxDim, IT_ERR_UNSUPPORTED, "more than %d columns", kMaxDim);
   IT_REQUIRE(d->n_experts <= kMaxExperts, IT_ERR_UNSUPPORTED, "%d experts, at most %d", d->n_experts, kMaxExperts);
-  const int64_t places = INT32_MAX / (d->feat_dtype == IT_F32 ? 3 : 1) - 256 * (int64_t)d->n_experts;
+  const int64_t places = INT32_MAX / (d->feat_dtype == IT_F32 ? 3 : 1) - 128 * (int64_t)d->n_experts;
   IT_REQUIRE(places > 0 && n <= places / d->top_k, IT_ERR_UNSUPPORTED, "%lld vertices with %d places each: too many rows for 32 bits", (long long)n, d->top_k);
   return IT_OK;
 }
@@ -290,16 +290,8 @@ bool rows_in_order(const it_experts_desc &d) {
   return d.feat_dtype == IT_F32 || cols > (d.gated ? 128 : 256);
 }
 
-// Two CTAs share the weights of 256 places: half the bytes of them, for products that take rows in order, where the padding (128 places of an expert
-// on average) is small.  PAIRS
-bool in_pairs(const it_experts_desc &d, int64_t places) {
-  // (a CTA's half of the columns is whole panels of 64, in e4m3 of 128)
-  const bool narrow = d.in_dtype == IT_E4M3 && (d.hidden_dim > 0 ? d.hidden_dim * (d.gated ? 2 : 1) : d.out_dim) <= 128;
-  return rows_in_order(d) && !narrow && places >= 1024 * (int64_t)d.n_experts;
-}
-
 struct ExpertsWs {
-  bool few, pairs, sorted;
+  bool few, sorted;
   size_t off_rows;                                   // few: fp32 rows by place
   size_t off_order, off_position, off_tiles, off_counts, off_hidden, off_sums, off_x, off_w1, off_w2;   // (tiles: the number of tiles, then their experts)
   int64_t tiles_max;
@@ -319,8 +311,7 @@ it_status plan(const it_experts_desc *d, int64_t n, ExpertsWs *w) {
     w->off_rows = take((size_t)places * cols * 4);
   } else {
     const bool f32 = d->feat_dtype == IT_F32;
-    w->pairs = in_pairs(*d, places);
-    w->tiles_max = it_experts_tiles_max(places, d->n_experts, w->pairs);
+    w->tiles_max = it_experts_tiles_max(places, d->n_experts);
     const size_t rows = (size_t)w->tiles_max * 128, E = (size_t)d->n_experts, n1 = cols * (d->gated ? 2 : 1);
     w->off_order = take(rows * 4);
     w->off_position = take((size_t)places * 4);
@@ -342,7 +333,6 @@ it_status many_places(const it_experts_args &a, const ExpertsWs &w, char *ws, ui
   const it_experts_desc &d = a.d;
   const bool f32 = d.feat_dtype == IT_F32, two = d.hidden_dim > 0;
   it_experts_plan q{};
-  q.pairs = w.pairs;
   q.order = (int32_t *)(ws + w.off_order); q.position = (int32_t *)(ws + w.off_position); q.n_tiles = (int32_t *)(ws + w.off_tiles);
   q.tile_expert = q.n_tiles + 1; q.counts = (int32_t *)(ws + w.off_counts); q.tiles_max = w.tiles_max;
   IT_TRY(it_launch_experts_plan(a, q, st));

@@ -17,9 +17,8 @@ struct it_experts_args {
 };
 
 // ----------------------------------------------------------------------------- experts_plan.cu
-// Places sorted by expert: every expert's places fill whole tiles of 128 positions, the last one padded with -1 (pairs: an even number of tiles).
+// Places sorted by expert: every expert's places fill whole tiles of 128 positions, the last one padded with -1.
 struct it_experts_plan {
-  bool pairs;
   int32_t *order;          // [tiles_max * 128] the place at a position, or -1
   int32_t *position;       // [places] where a place went (places of no expert: undefined)
   int32_t *tile_expert;    // [tiles_max]
@@ -27,7 +26,7 @@ struct it_experts_plan {
   int32_t *counts;         // [blocks][n_experts] scratch
   int64_t tiles_max;
 };
-int64_t it_experts_tiles_max(int64_t places, int n_experts, bool pairs);
+int64_t it_experts_tiles_max(int64_t places, int n_experts);
 size_t it_experts_count_words(int64_t places, int n_experts);
 // Also zeroes a.status and, where a vertex has one place only, the rows of `out` whose id is no expert.
 it_status it_launch_experts_plan(const it_experts_args &a, const it_experts_plan &q, cudaStream_t st);

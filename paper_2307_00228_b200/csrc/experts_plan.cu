@@ -47,17 +47,12 @@ __device__ __forceinline__ int block_scan(int v, int *warp_sums, int *total) {
   return s - v + (warp ? warp_sums[warp - 1] : 0);
 }
 
-__device__ __forceinline__ int plan_tiles(const PlanParams &p, int places) {
-  const int tiles = (places + PLAN_TILE - 1) / PLAN_TILE;
-  return p.q.pairs ? (tiles + 1) & ~1 : tiles;
-}
-
 // count[e] (shared): places of every expert -> first position of every expert; tiles, padding and the number of tiles are written.
 // first: as many words of shared memory.
 __device__ void lay_out(const PlanParams &p, int *count, int *first, int *warp_sums) {
   int tiles_before = 0;
   for (int e0 = 0; e0 < p.n_experts; e0 += PLAN_THREADS) {
-    const int e = e0 + threadIdx.x, tiles = e < p.n_experts ? plan_tiles(p, count[e]) : 0;
+    const int e = e0 + threadIdx.x, tiles = e < p.n_experts ? (count[e] + PLAN_TILE - 1) / PLAN_TILE : 0;
     int total;
     const int at = tiles_before + block_scan(tiles, warp_sums, &total);
     if (e < p.n_experts) first[e] = at;
@@ -66,7 +61,7 @@ __device__ void lay_out(const PlanParams &p, int *count, int *first, int *warp_s
   if (threadIdx.x == 0) *p.q.n_tiles = tiles_before;
   __syncthreads();
   for (int e = threadIdx.x >> 5; e < p.n_experts; e += PLAN_THREADS / 32) {
-    const int lane = threadIdx.x & 31, c = count[e], t0 = first[e], t1 = t0 + plan_tiles(p, c);
+    const int lane = threadIdx.x & 31, c = count[e], t0 = first[e], t1 = t0 + (c + PLAN_TILE - 1) / PLAN_TILE;
     for (int t = t0 + lane; t < t1; t += 32) p.q.tile_expert[t] = e;
     for (int64_t i = (int64_t)t0 * PLAN_TILE + c + lane; i < (int64_t)t1 * PLAN_TILE; i += 32) p.q.order[i] = -1;
     __syncwarp();
@@ -239,10 +234,7 @@ __global__ void __launch_bounds__(256) rows_kernel(const uint4 *x, uint4 *to, in
 
 }  // namespace
 
-int64_t it_experts_tiles_max(int64_t places, int n_experts, bool pairs) {
-  const int64_t met = places < n_experts ? places : n_experts;   // each of them rounds up
-  return pairs ? 2 * (places / (2 * PLAN_TILE) + met) : places / PLAN_TILE + met;
-}
+int64_t it_experts_tiles_max(int64_t places, int n_experts) { return places / PLAN_TILE + (places < n_experts ? places : n_experts); }
 size_t it_experts_count_words(int64_t places, int n_experts) {
   return places <= PLAN_ONE_BLOCK ? 0 : (size_t)plan_blocks(places) * (size_t)n_experts;
 }

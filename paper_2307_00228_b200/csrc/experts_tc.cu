@@ -58,15 +58,14 @@ __device__ __forceinline__ void pass_parts(int passes, int i, int *pa, int *pb) 
   *pb = passes == 1 ? 0 : (int)((B >> (4 * i)) & 15u);
 }
 
-template <bool EIGHT, it_expert_store STORE, bool GATED, bool PAIR>
+template <bool EIGHT, it_expert_store STORE, bool GATED>
 __global__ void __launch_bounds__(EX_THREADS, 1)
 expert_gemm_kernel(const __grid_constant__ CUtensorMap map_a, const __grid_constant__ CUtensorMap map_w, const ExParams p) {
   extern __shared__ __align__(1024) unsigned char base[];   // (the swizzle goes by addresses: stages start at multiples of 1024)
   const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
   constexpr int BK = EIGHT ? 128 : 64;                  // elements of a k-block, and columns of a panel
   constexpr int PANEL = BK * TC_KBLOCK_BYTES;           // bytes of a panel of W: BK rows x 128 bytes
-  const int b_bytes = p.bn / (PAIR ? 2 : 1) * TC_KBLOCK_BYTES, stage_bytes = EX_STAGE_A + b_bytes;   // (a pair: half the columns in either CTA)
-  const uint32_t rank = PAIR ? cluster_rank() : 0u, team = PAIR ? blockIdx.x >> 1 : blockIdx.x, teams = PAIR ? gridDim.x >> 1 : gridDim.x;
+  const int b_bytes = p.bn * TC_KBLOCK_BYTES, stage_bytes = EX_STAGE_A + b_bytes;
 
   unsigned char *staging = base + (size_t)p.stages * stage_bytes;
   using Meta = std::conditional_t<EIGHT, ExMetaEight, ExMeta>;
@@ -84,47 +83,40 @@ expert_gemm_kernel(const __grid_constant__ CUtensorMap map_a, const __grid_const
 
   if (threadIdx.x == 0) {
     for (int s = 0; s < p.stages; ++s) {
-      mbar_init(&full[s], p.gather_div ? 32 * EX_FETCH_WARPS + 1 : 1);   // (a pair's copies count at the barriers of rank 0)
+      mbar_init(&full[s], p.gather_div ? 32 * EX_FETCH_WARPS + 1 : 1);
       mbar_init(&empty[s], 1);
     }
     for (int a = 0; a < 2; ++a) {
       mbar_init(&acc_full[a], 1);
       mbar_init(&meta_full[a], 1);
-      mbar_init(&acc_empty[a], EX_EPI_WARPS + (PAIR ? (rank == 0 ? EX_EPI_WARPS : 0) : 0));
+      mbar_init(&acc_empty[a], EX_EPI_WARPS);
     }
     mbar_init(mma_done, 1);
     *abort_flag = 0;
     asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");
   }
   if (warp == EX_MMA_WARP) {
-    if constexpr (PAIR) {
-      tmem_alloc_pair(tmem_slot, tmem_cols);
-      tmem_relinquish_pair();
-    } else {
-      tmem_alloc(tmem_slot, tmem_cols);
-      tmem_relinquish();
-    }
+    tmem_alloc(tmem_slot, tmem_cols);
+    tmem_relinquish();
   }
   it_allow_next();
   it_wait_prior();
   tc_fence_before();
   __syncthreads();
-  if constexpr (PAIR) cluster_sync();   // the other CTA's barriers are set up
   tc_fence_after();
   const uint32_t tmem_base = *tmem_slot;
   int m_tiles = *p.n_tiles;
   m_tiles = m_tiles < p.tiles_max ? m_tiles : p.tiles_max;
-  const uint32_t splits = (uint32_t)p.n_splits, n_tiles = (uint32_t)(PAIR ? m_tiles / 2 : m_tiles) * splits;   // (below 2^31; a pair takes two row tiles of an expert)
+  const uint32_t splits = (uint32_t)p.n_splits, n_tiles = (uint32_t)m_tiles * splits;   // (below 2^31)
   const int KB = p.kb * p.passes;
-  auto row_tile = [&](uint32_t tile) { return PAIR ? 2 * (tile / splits) + rank : tile / splits; };
 
   if (warp < EX_FETCH_WARPS) {
     // ------------------------------------------------------------------ producers: rows found by place by all four warps, 16 bytes a lane;
     // weights, and rows in order, by TMA from the first
     uint32_t stage = 0, phase = 0;
-    const bool gather = !PAIR && p.gather_div > 0;
+    const bool gather = p.gather_div > 0;
     bool ok = !p.no_loads && (warp == 0 || gather), came_round = false;
-    const uint32_t tma_bytes = ((gather ? 0 : EX_STAGE_A) + b_bytes) * (PAIR ? 2 : 1);
+    const uint32_t tma_bytes = (gather ? 0 : EX_STAGE_A) + b_bytes;
     const int chunk = lane & 7;
     uint32_t dst[8];   // where this lane's 16 bytes of its eight rows go in a stage (128-byte swizzle)
 #pragma unroll
@@ -135,16 +127,16 @@ expert_gemm_kernel(const __grid_constant__ CUtensorMap map_a, const __grid_const
     // (what a tile is about is looked up while the tile before it is fetched)
     auto lookup = [&](uint32_t tile, int &e, int &place) {
       if (tile >= n_tiles) return;
-      const uint32_t m = row_tile(tile);
+      const uint32_t m = tile / splits;
       e = p.tile_expert[m];
       if (gather) place = p.order[(int64_t)m * TC_BM + warp * 32 + lane];
     };
     int e_next = 0, place_next = -1;
-    lookup(team, e_next, place_next);
-    for (uint32_t tile = team; tile < n_tiles && ok; tile += teams) {
-      const int m = (int)row_tile(tile), c0 = (int)(tile % splits) * p.cols_per_tile;
+    lookup(blockIdx.x, e_next, place_next);
+    for (uint32_t tile = blockIdx.x; tile < n_tiles && ok; tile += gridDim.x) {
+      const int m = (int)(tile / splits), c0 = (int)(tile % splits) * p.cols_per_tile;
       const int e = e_next, place = place_next;
-      lookup(tile + teams, e_next, place_next);
+      lookup(tile + gridDim.x, e_next, place_next);
       const unsigned char *src[8];
       uint32_t real = 0;   // bit i: row i of this lane's has a place
       if (gather) {
@@ -162,32 +154,21 @@ expert_gemm_kernel(const __grid_constant__ CUtensorMap map_a, const __grid_const
         for (int kb = 0; kb < p.kb; ++kb) {
           if (lane == 0) {
             ok = mbar_wait(&empty[stage], phase ^ 1u, abort_flag, p.spin_limit, EX_TMA_BACKOFF);
-            if (ok && warp == 0 && rank == 0) mbar_arrive_expect_tx(&full[stage], tma_bytes);
+            if (ok && warp == 0) mbar_arrive_expect_tx(&full[stage], tma_bytes);
           }
           ok = __shfl_sync(0xffffffffu, (int)ok, 0);
           if (!ok) break;
           unsigned char *to = base + (size_t)stage * stage_bytes;
           if (warp == 0) {
-            const uint32_t bar = PAIR ? leader_bar(&full[stage]) : 0u;
-            const int a_row = pa * p.a_rows + m * TC_BM, w_mat = pb * p.n_experts + e;
-            if (lane == 8 && !gather) {
-              if constexpr (PAIR) tma_load_2d_pair(to, &map_a, kb * BK, a_row, bar);
-              else tma_load_2d(to, &map_a, kb * BK, a_row, &full[stage]);
-            }
+            if (lane == 8 && !gather) tma_load_2d(to, &map_a, kb * BK, pa * p.a_rows + m * TC_BM, &full[stage]);
+            const int w_mat = pb * p.n_experts + e;
             if (p.box_panels > 0) {   // runs of panels in a copy each
-              if (lane == 16 || (GATED && !PAIR && lane == 17)) {
-                const bool second = GATED && (PAIR ? rank != 0 : lane == 17);
-                const int col = second ? p.cols + c0 : c0 + (PAIR && !GATED ? (int)rank * (p.bn / 2) : 0);
-                unsigned char *wt = to + EX_STAGE_A + (lane - 16) * p.box_panels * PANEL;
-                if constexpr (PAIR) tma_load_4d_pair(wt, &map_w, 0, kb * BK, col / BK, w_mat, bar);
-                else tma_load_4d(wt, &map_w, 0, kb * BK, col / BK, w_mat, &full[stage]);
-              }
-            } else if (lane >= 16 && lane - 16 < p.bn / (PAIR ? 2 : 1) / BK) {   // a panel of the weights a lane (a pair: of this CTA's half)
               // gated: the first half of the panels are columns of the gate, the second of what it gates
-              const int c = (lane - 16) * BK + (PAIR ? (int)rank * (p.bn / 2) : 0), col = GATED && c >= p.cols_per_tile ? p.cols + c0 + c - p.cols_per_tile : c0 + c;
-              unsigned char *wt = to + EX_STAGE_A + (lane - 16) * PANEL;
-              if constexpr (PAIR) tma_load_3d_pair(wt, &map_w, col, kb * BK, w_mat, bar);
-              else tma_load_3d(wt, &map_w, col, kb * BK, w_mat, &full[stage]);
+              if (lane == 16 || (GATED && lane == 17))
+                tma_load_4d(to + EX_STAGE_A + (lane - 16) * p.box_panels * PANEL, &map_w, 0, kb * BK, (lane == 17 ? p.cols + c0 : c0) / BK, w_mat, &full[stage]);
+            } else if (lane >= 16 && lane - 16 < p.bn / BK) {   // a panel of the weights a lane
+              const int c = (lane - 16) * BK, col = GATED && c >= p.cols_per_tile ? p.cols + c0 + c - p.cols_per_tile : c0 + c;
+              tma_load_3d(to + EX_STAGE_A + (lane - 16) * PANEL, &map_w, col, kb * BK, w_mat, &full[stage]);
             }
             __syncwarp();
           }
@@ -205,45 +186,37 @@ expert_gemm_kernel(const __grid_constant__ CUtensorMap map_a, const __grid_const
     __syncwarp();
     cp_async_wait_all();
     // (after an abort a stage may lack another warp's arrivals: the wait for the copies in flight then ends by its limit)
-    if (lane == 0 && warp == 0 && rank == 0) ring_drain(full, (uint32_t)p.stages, stage, phase, came_round);
+    if (lane == 0 && warp == 0) ring_drain(full, (uint32_t)p.stages, stage, phase, came_round);
   } else if (warp == EX_MMA_WARP) {
     // ------------------------------------------------------------------ MMA issuer
-    // D = fp32, A K-major, B MN-major (bit 16), N = bn, M = 128 (a pair 256); operands bf16 (1) or e4m3 (0)
+    // D = fp32, A K-major, B MN-major (bit 16), N = bn, M = 128; operands bf16 (1) or e4m3 (0)
     const uint32_t fmt = EIGHT ? 0u : 1u, lead = lane == 0;
-    const uint32_t idesc = (1u << 4) | (fmt << 7) | (fmt << 10) | (1u << 16) | ((uint32_t)(p.bn >> 3) << 17) | ((uint32_t)((PAIR ? 2 * TC_BM : TC_BM) >> 4) << 24);
+    const uint32_t idesc = (1u << 4) | (fmt << 7) | (fmt << 10) | (1u << 16) | ((uint32_t)(p.bn >> 3) << 17) | ((uint32_t)(TC_BM >> 4) << 24);
     uint32_t stage = 0, phase = 0, acc = 0, acc_phase = 0;
     bool ok = true;
-    if (!PAIR || rank == 0) {   // (of a pair, the CTA of rank 0 issues)
-      for (uint32_t tile = team; tile < n_tiles && ok; tile += teams) {
-        ok = PAIR ? ex_wait_warp_cluster(&acc_empty[acc], acc_phase ^ 1u, abort_flag, p.spin_limit) : ex_wait_warp(&acc_empty[acc], acc_phase ^ 1u, abort_flag, p.spin_limit);
+    for (uint32_t tile = blockIdx.x; tile < n_tiles && ok; tile += gridDim.x) {
+      ok = ex_wait_warp(&acc_empty[acc], acc_phase ^ 1u, abort_flag, p.spin_limit);
+      if (!ok) break;
+      tc_fence_after();
+      const uint32_t d_tmem = tmem_base + acc * (uint32_t)p.bn;
+      for (int kb = 0; kb < KB; ++kb) {
+        ok = ex_wait_warp(&full[stage], phase, abort_flag, p.spin_limit);
         if (!ok) break;
-        tc_fence_after();
-        const uint32_t d_tmem = tmem_base + acc * (uint32_t)p.bn;
-        for (int kb = 0; kb < KB; ++kb) {
-          ok = PAIR ? ex_wait_warp_cluster(&full[stage], phase, abort_flag, p.spin_limit) : ex_wait_warp(&full[stage], phase, abort_flag, p.spin_limit);
-          if (!ok) break;
-          // gathered rows were written by the threads of the other warps: what follows reads them through the tensor core's path
-          if (!PAIR && p.gather_div) asm volatile("fence.proxy.async.shared::cta;" ::: "memory");
-          tc_fence_after();
-          const uint32_t a_s = smem_u32(base) + stage * (uint32_t)stage_bytes;
-          const uint64_t a_d = make_desc(a_s), b_d = make_desc_mn(a_s + EX_STAGE_A, PANEL);
+        // gathered rows were written by the threads of the other warps: what follows reads them through the tensor core's path
+        if (p.gather_div) asm volatile("fence.proxy.async.shared::cta;" ::: "memory");
+        const uint32_t a_s = smem_u32(base) + stage * (uint32_t)stage_bytes;
+        const uint64_t a_d = make_desc(a_s), b_d = make_desc_mn(a_s + EX_STAGE_A, PANEL);
 #pragma unroll
-          for (int k = 0; k < 4; ++k) {   // four steps of 32 bytes of K: a quarter of the k-block's rows of W
-            if constexpr (PAIR) ex_mma_pair<EIGHT>(lead, d_tmem, a_d + k * 2, b_d + k * (PANEL / 64), idesc, (kb | k) != 0);
-            else ex_mma<EIGHT>(lead, d_tmem, a_d + k * 2, b_d + k * (PANEL / 64), idesc, (kb | k) != 0);
-          }
-          if constexpr (PAIR) ex_commit_pair(lead, &empty[stage]);
-          else ex_commit(lead, &empty[stage]);
-          if (++stage == (uint32_t)p.stages) { stage = 0; phase ^= 1u; }
-        }
-        if (!ok) break;
-        if constexpr (PAIR) ex_commit_pair(lead, &acc_full[acc]);
-        else ex_commit(lead, &acc_full[acc]);
-        if (++acc == 2) { acc = 0; acc_phase ^= 1u; }
+        for (int k = 0; k < 4; ++k)   // four steps of 32 bytes of K: a quarter of the k-block's rows of W
+          ex_mma<EIGHT>(lead, d_tmem, a_d + k * 2, b_d + k * (PANEL / 64), idesc, (kb | k) != 0);
+        ex_commit(lead, &empty[stage]);
+        if (++stage == (uint32_t)p.stages) { stage = 0; phase ^= 1u; }
       }
-      if constexpr (PAIR) ex_commit_pair(lead, mma_done);
-      else ex_commit(lead, mma_done);
+      if (!ok) break;
+      ex_commit(lead, &acc_full[acc]);
+      if (++acc == 2) { acc = 0; acc_phase ^= 1u; }
     }
+    ex_commit(lead, mma_done);
     mbar_drain(mma_done, 0);
   } else if (warp == EX_META_WARP) {
     // ------------------------------------------------------------------ what the epilogue needs, ahead of it: two loads, one behind the other, for
@@ -253,16 +226,16 @@ expert_gemm_kernel(const __grid_constant__ CUtensorMap map_a, const __grid_const
     int e_next = 0;
     auto look = [&](uint32_t tile) {
       if (tile >= n_tiles) return;
-      const uint32_t m = row_tile(tile);
+      const uint32_t m = tile / splits;
       place_next = *reinterpret_cast<const int4 *>(p.order + (int64_t)m * TC_BM + lane * 4);
       e_next = p.tile_expert[m];
     };
-    look(team);
-    for (uint32_t tile = team; tile < n_tiles; tile += teams) {
+    look(blockIdx.x);
+    for (uint32_t tile = blockIdx.x; tile < n_tiles; tile += gridDim.x) {
       const int4 place = place_next;
       const int64_t w_row = (int64_t)e_next * p.w_cols;
       const int c_tile = (int)(tile % splits) * p.cols_per_tile;
-      look(tile + teams);
+      look(tile + gridDim.x);
       float4 weight = make_float4(1.f, 1.f, 1.f, 1.f), xs = weight, bias[2], scale[2];
       if (STORE == IT_EXPERT_OUT_BF16 || STORE == IT_EXPERT_OUT_F32) {
         weight.x = place.x < 0 ? 0.f : p.weights[place.x]; weight.y = place.y < 0 ? 0.f : p.weights[place.y];
@@ -312,8 +285,8 @@ expert_gemm_kernel(const __grid_constant__ CUtensorMap map_a, const __grid_const
     const uint32_t row8 = 8u * (uint32_t)p.cols * ESIZE;
     const uint32_t floor2 = p.act == IT_ACT_RELU ? 0u : 0xff80ff80u;   // bf16 pair: 0, or minus infinity where nothing is cut off
     uint32_t acc = 0, acc_phase = 0;
-    for (uint32_t tile = team; tile < n_tiles; tile += teams) {
-      const int m = (int)row_tile(tile), c_tile = (int)(tile % splits) * p.cols_per_tile;
+    for (uint32_t tile = blockIdx.x; tile < n_tiles; tile += gridDim.x) {
+      const int m = (int)(tile / splits), c_tile = (int)(tile % splits) * p.cols_per_tile;
       const int64_t pos0 = (int64_t)m * TC_BM + quarter * 32;
       const bool ok = mbar_wait(&meta_full[acc], acc_phase, abort_flag, p.spin_limit, EX_EPI_BACKOFF) &&
                       mbar_wait(&acc_full[acc], acc_phase, abort_flag, p.spin_limit, EX_EPI_BACKOFF);
@@ -453,10 +426,7 @@ expert_gemm_kernel(const __grid_constant__ CUtensorMap map_a, const __grid_const
       }
       tc_fence_before();
       __syncwarp();
-      if (lane == 0) {
-        mbar_arrive(&acc_empty[acc]);   // (of a pair: the MMAs of the other CTA wait too)
-        if (PAIR && rank != 0) mbar_arrive_leader(&acc_empty[acc]);
-      }
+      if (lane == 0) mbar_arrive(&acc_empty[acc]);
       if (++acc == 2) { acc = 0; acc_phase ^= 1u; }
     }
   }
@@ -466,32 +436,18 @@ expert_gemm_kernel(const __grid_constant__ CUtensorMap map_a, const __grid_const
   tc_fence_before();
   __syncthreads();
   if (threadIdx.x == 0 && *abort_flag) atomicExch(p.status, 1);
-  if constexpr (PAIR) cluster_sync();   // nobody leaves while the other's MMAs read here, or arrivals are on their way
   if (warp == EX_MMA_WARP) {
     tc_fence_after();
-    if constexpr (PAIR) tmem_dealloc_pair(tmem_base, tmem_cols);
-    else tmem_dealloc(tmem_base, tmem_cols);
+    tmem_dealloc(tmem_base, tmem_cols);
   }
 }
 
 // ----------------------------------------------------------------------------- host side
-template <bool EIGHT, it_expert_store STORE, bool GATED, bool PAIR>
-it_status launch_as(const CUtensorMap &ma, const CUtensorMap &mw, const ExParams &p, int grid, int smem, double bytes, double flops, cudaStream_t st) {
-  auto *kernel = expert_gemm_kernel<EIGHT, STORE, GATED, PAIR>;
-  IT_CUDA_TRY(cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, smem));
-  cudaLaunchAttribute attr[2] = {};
-  attr[0].id = cudaLaunchAttributeProgrammaticStreamSerialization;
-  attr[0].val.programmaticStreamSerializationAllowed = 1;
-  attr[1].id = cudaLaunchAttributeClusterDimension;
-  attr[1].val.clusterDim.x = 2; attr[1].val.clusterDim.y = 1; attr[1].val.clusterDim.z = 1;
-  cudaLaunchConfig_t cfg{};
-  cfg.gridDim = dim3((unsigned)grid); cfg.blockDim = dim3(EX_THREADS); cfg.dynamicSmemBytes = (size_t)smem; cfg.stream = st; cfg.attrs = attr; cfg.numAttrs = PAIR ? 2 : 1;
-  IT_LAUNCH(IT_K_EXPERT_GEMM, bytes, flops, st, IT_CUDA_TRY(cudaLaunchKernelEx(&cfg, kernel, ma, mw, p)));
-  return IT_OK;
-}
 template <bool EIGHT, it_expert_store STORE, bool GATED>
-it_status launch(const CUtensorMap &ma, const CUtensorMap &mw, const ExParams &p, bool pair, int grid, int smem, double bytes, double flops, cudaStream_t st) {
-  return pair ? launch_as<EIGHT, STORE, GATED, true>(ma, mw, p, grid, smem, bytes, flops, st) : launch_as<EIGHT, STORE, GATED, false>(ma, mw, p, grid, smem, bytes, flops, st);
+it_status launch(const CUtensorMap &ma, const CUtensorMap &mw, const ExParams &p, int grid, int smem, double bytes, double flops, cudaStream_t st) {
+  IT_CUDA_TRY(cudaFuncSetAttribute(expert_gemm_kernel<EIGHT, STORE, GATED>, cudaFuncAttributeMaxDynamicSharedMemorySize, smem));
+  IT_LAUNCH(IT_K_EXPERT_GEMM, bytes, flops, st, IT_CUDA_TRY(it_launch_pdl(expert_gemm_kernel<EIGHT, STORE, GATED>, dim3((unsigned)grid), dim3(EX_THREADS), smem, st, ma, mw, p)));
+  return IT_OK;
 }
 
 }  // namespace
@@ -512,20 +468,17 @@ it_status it_launch_expert_gemm(const it_experts_args &a, const it_experts_plan 
   p.cols_per_tile = ((g.cols + p.n_splits - 1) / p.n_splits + BK - 1) / BK * BK;
   p.n_splits = (g.cols + p.cols_per_tile - 1) / p.cols_per_tile;
   p.bn = g.gated ? 2 * p.cols_per_tile : p.cols_per_tile;
-  // Either CTA of a pair holds half an accumulator's columns of the weights, in whole panels.
-  const bool pair = q.pairs;
-  if (pair && p.bn % (2 * BK) != 0) { p.cols_per_tile = (p.cols_per_tile + 2 * BK - 1) / (2 * BK) * (2 * BK); p.bn = p.cols_per_tile; }
 
   const cuuint64_t da[2] = {(cuuint64_t)g.K, (cuuint64_t)(g.a_rows * g.parts)}, sa[1] = {(cuuint64_t)g.K * elem};
   const cuuint32_t ba[2] = {(cuuint32_t)BK, (cuuint32_t)TC_BM};
   CUtensorMap ma, mw;
   IT_TRY(encode(&ma, g.eight, g.A, 2, da, sa, ba));
-  // Columns in whole panels: W as [experts][panels][K][panel's columns], of which one copy fetches what a CTA keeps of a k-block (gated: of
+  // Columns in whole panels: W as [experts][panels][K][panel's columns], of which one copy fetches what a tile takes of a k-block (gated: of
   // either half).  Otherwise a copy per panel, which fills what lies beyond a row with zeros.
   const cuuint64_t n_mats = (cuuint64_t)a.d.n_experts * g.parts, row = (cuuint64_t)g.w_cols * elem;
   p.box_panels = 0;
   if (g.w_cols % BK == 0 && g.cols % BK == 0) {
-    p.box_panels = (g.gated ? p.cols_per_tile : p.bn / (pair ? 2 : 1)) / BK;
+    p.box_panels = (g.gated ? p.cols_per_tile : p.bn) / BK;
     const cuuint64_t dw[4] = {(cuuint64_t)BK, (cuuint64_t)g.K, (cuuint64_t)(g.w_cols / BK), n_mats}, sw[3] = {row, TC_KBLOCK_BYTES, row * (cuuint64_t)g.K};
     const cuuint32_t bw[4] = {(cuuint32_t)BK, (cuuint32_t)BK, (cuuint32_t)p.box_panels, 1};
     IT_TRY(encode(&mw, g.eight, g.W, 4, dw, sw, bw));
@@ -535,17 +488,16 @@ it_status it_launch_expert_gemm(const it_experts_args &a, const it_experts_plan 
     IT_TRY(encode(&mw, g.eight, g.W, 3, dw, sw, bw));
   }
 
-  const int stage = EX_STAGE_A + p.bn / (pair ? 2 : 1) * TC_KBLOCK_BYTES, fixed = EX_EPI_WARPS * ex_staging(g.store) + 2 * (int)(g.eight ? sizeof(ExMetaEight) : sizeof(ExMeta)) + (2 * EX_MAX_STAGES + 9) * 8;
+  const int stage = EX_STAGE_A + p.bn * TC_KBLOCK_BYTES, fixed = EX_EPI_WARPS * ex_staging(g.store) + 2 * (int)(g.eight ? sizeof(ExMetaEight) : sizeof(ExMeta)) + (2 * EX_MAX_STAGES + 9) * 8;
   p.stages = (227 * 1024 - fixed) / stage;
   if (p.stages > EX_MAX_STAGES) p.stages = EX_MAX_STAGES;
   const int smem = fixed + p.stages * stage;
   const int64_t tiles = q.tiles_max * p.n_splits;
   IT_REQUIRE(tiles + 3 * (int64_t)a.sms <= INT32_MAX, IT_ERR_UNSUPPORTED, "too many places and columns for one launch");
-  const int64_t teams = pair ? tiles / 2 : tiles, side_by_side = pair ? a.sms / 2 : a.sms;
-  const int grid = (int)(teams < side_by_side ? teams : side_by_side) * (pair ? 2 : 1);
+  const int grid = (int)(tiles < a.sms ? tiles : a.sms);
   const int64_t places = a.n * a.d.top_k;
   const double flops = 2.0 * places * g.K * (double)g.w_cols, bytes = (double)places * (g.K * elem * g.parts + g.cols * 4.0);
-#define IT_EX_LAUNCH(EIGHT, STORE, GATED) return launch<EIGHT, STORE, GATED>(ma, mw, p, pair, grid, smem, bytes, flops, st)
+#define IT_EX_LAUNCH(EIGHT, STORE, GATED) return launch<EIGHT, STORE, GATED>(ma, mw, p, grid, smem, bytes, flops, st)
   switch (g.store) {
     case IT_EXPERT_HIDDEN:
       if (g.eight) { if (g.gated) IT_EX_LAUNCH(true, IT_EXPERT_HIDDEN, true); else IT_EX_LAUNCH(true, IT_EXPERT_HIDDEN, false); }
