@@ -343,8 +343,9 @@ it_status many_places(const it_experts_args &a, const ExpertsWs &w, char *ws, ui
       parts.src[parts.count] = (const float *)src; parts.dst[parts.count] = (__nv_bfloat16 *)(ws + off); parts.elems[parts.count++] = elems;
       return (const void *)(ws + off);
     };
-    x = part(a.x, w.off_x, w.tiles_max * 128 * d.in_dim);
-    parts.order = q.order; parts.n_tiles = q.n_tiles; parts.row = d.in_dim; parts.top_k = d.top_k;
+    x = ws + w.off_x;
+    parts.x = (const float *)a.x; parts.x_parts = (__nv_bfloat16 *)(ws + w.off_x); parts.row = d.in_dim; parts.top_k = d.top_k;
+    parts.order = q.order; parts.n_tiles = q.n_tiles; parts.tiles_max = q.tiles_max;
     W1 = part(d.W1, w.off_w1, (int64_t)d.n_experts * d.in_dim * a.n1);
     if (two) W2 = part(d.W2, w.off_w2, (int64_t)d.n_experts * d.hidden_dim * d.out_dim);
     IT_TRY(it_launch_experts_parts(parts, a.sms, st));

@@ -30,10 +30,11 @@ int64_t it_experts_tiles_max(int64_t places, int n_experts);
 size_t it_experts_count_words(int64_t places, int n_experts);
 // Also zeroes a.status and, where a vertex has one place only, the rows of `out` whose id is no expert.
 it_status it_launch_experts_plan(const it_experts_args &a, const it_experts_plan &q, cudaStream_t st);
-// fp32 matrices as three bf16 parts each (24 bits: 8 a part, cut off, so that the parts add up exactly): dst[i] is [3, elems[i]].
+// fp32 values as three bf16 parts each (24 bits: 8 a part, cut off, so that the parts add up exactly): dst[i] is [3, elems[i]], x_parts [3, positions, row]
+// with the rows of x in the order of the positions.
 struct it_experts_parts {
-  const float *src[3]; __nv_bfloat16 *dst[3]; int64_t elems[3]; int count;
-  const int32_t *order, *n_tiles; int row, top_k;   // src[0]: rows of `row` elements, found by the place at each position
+  const float *src[2]; __nv_bfloat16 *dst[2]; int64_t elems[2]; int count;
+  const float *x; __nv_bfloat16 *x_parts; int row, top_k; const int32_t *order, *n_tiles; int64_t tiles_max;
 };
 it_status it_launch_experts_parts(const it_experts_parts &q, int sms, cudaStream_t st);
 // Rows of x in the order of the positions.

@@ -189,47 +189,51 @@ __device__ __forceinline__ void split3(float v, uint32_t &a, uint32_t &b, uint32
   c = __float_as_uint(r1 - __uint_as_float(u1 & 0xffff0000u)) >> 16;
 }
 
-// src[0] is gathered where q.order is given: row r of dst[0] is row order[r] / top_k of it (and left as it is for a position of no place).
-__global__ void __launch_bounds__(256) parts_kernel(const it_experts_parts q) {
-  it_allow_next();
-  it_wait_prior();
-  const float *src = q.src[blockIdx.y];
-  __nv_bfloat16 *dst = q.dst[blockIdx.y];
-  const bool gather = q.order != nullptr && blockIdx.y == 0;
-  int64_t n = q.elems[blockIdx.y];
-  if (gather) {
-    const int64_t met = (int64_t)*q.n_tiles * PLAN_TILE * q.row;
-    n = met < n ? met : n;
-  }
-  for (int64_t i = (blockIdx.x * (int64_t)blockDim.x + threadIdx.x) * 4; i < n; i += (int64_t)gridDim.x * blockDim.x * 4) {
-    int64_t from = i;
-    if (gather) {
-      const int64_t r = i / q.row;
-      const int place = q.order[r];
-      if (place < 0) continue;
-      from = (int64_t)(place / q.top_k) * q.row + (i - r * q.row);
-    }
-    const float4 v = *reinterpret_cast<const float4 *>(src + from);
-    uint32_t w[3][4];
-    split3(v.x, w[0][0], w[1][0], w[2][0]); split3(v.y, w[0][1], w[1][1], w[2][1]);
-    split3(v.z, w[0][2], w[1][2], w[2][2]); split3(v.w, w[0][3], w[1][3], w[2][3]);
-#pragma unroll
-    for (int k = 0; k < 3; ++k) *reinterpret_cast<uint2 *>(dst + k * q.elems[blockIdx.y] + i) = make_uint2(w[k][0] | (w[k][1] << 16), w[k][2] | (w[k][3] << 16));
+// Rows of x in the order of the positions: f(position, vertex, piece) for every piece of every row that has a place, a group of lanes a row.
+template <typename F>
+__device__ __forceinline__ void it_experts_rows_walk(const int32_t *order, const int32_t *n_tiles, int64_t tiles_max, int top_k, int pieces, F f) {
+  int64_t tiles = *n_tiles;
+  tiles = tiles < tiles_max ? tiles : tiles_max;
+  int lanes = 1;
+  while (lanes < 32 && lanes < pieces) lanes <<= 1;
+  const int per_block = 256 / lanes, gl = threadIdx.x % lanes;
+  for (int64_t r = blockIdx.x * (int64_t)per_block + threadIdx.x / lanes; r < tiles * PLAN_TILE; r += (int64_t)gridDim.x * per_block) {
+    const int place = order[r];
+    if (place < 0) continue;
+    const int64_t v = place / top_k;
+    for (int c = gl; c < pieces; c += lanes) f(r, v, c);
   }
 }
 
-// Rows of x in the order of the positions, 16 bytes a thread.
+__device__ __forceinline__ void split_store(const float4 &v, __nv_bfloat16 *dst, int64_t part) {
+  uint32_t w[3][4];
+  split3(v.x, w[0][0], w[1][0], w[2][0]); split3(v.y, w[0][1], w[1][1], w[2][1]);
+  split3(v.z, w[0][2], w[1][2], w[2][2]); split3(v.w, w[0][3], w[1][3], w[2][3]);
+#pragma unroll
+  for (int k = 0; k < 3; ++k) *reinterpret_cast<uint2 *>(dst + k * part) = make_uint2(w[k][0] | (w[k][1] << 16), w[k][2] | (w[k][3] << 16));
+}
+
+// blockIdx.y: the matrix of weights, or (the last one) the rows of x.
+__global__ void __launch_bounds__(256) parts_kernel(const __grid_constant__ it_experts_parts q) {
+  it_allow_next();
+  it_wait_prior();
+  if ((int)blockIdx.y < q.count) {
+    const float *src = blockIdx.y == 0 ? q.src[0] : q.src[1];
+    __nv_bfloat16 *dst = blockIdx.y == 0 ? q.dst[0] : q.dst[1];
+    const int64_t n = blockIdx.y == 0 ? q.elems[0] : q.elems[1];
+    for (int64_t i = (blockIdx.x * (int64_t)blockDim.x + threadIdx.x) * 4; i < n; i += (int64_t)gridDim.x * blockDim.x * 4)
+      split_store(*reinterpret_cast<const float4 *>(src + i), dst + i, n);
+    return;
+  }
+  it_experts_rows_walk(q.order, q.n_tiles, q.tiles_max, q.top_k, q.row / 4, [&](int64_t r, int64_t v, int c) {
+    split_store(*reinterpret_cast<const float4 *>(q.x + v * q.row + c * 4), q.x_parts + r * q.row + c * 4, q.tiles_max * PLAN_TILE * q.row);
+  });
+}
+
 __global__ void __launch_bounds__(256) rows_kernel(const uint4 *x, uint4 *to, int row16, int top_k, const int32_t *order, const int32_t *n_tiles, int64_t tiles_max) {
   it_allow_next();
   it_wait_prior();
-  int64_t tiles = *n_tiles;
-  tiles = tiles < tiles_max ? tiles : tiles_max;
-  const int64_t n = tiles * PLAN_TILE * row16;
-  for (int64_t i = blockIdx.x * (int64_t)blockDim.x + threadIdx.x; i < n; i += (int64_t)gridDim.x * blockDim.x) {
-    const int64_t r = i / row16;
-    const int place = order[r];
-    if (place >= 0) to[i] = __ldg(x + (int64_t)(place / top_k) * row16 + (i - r * row16));
-  }
+  it_experts_rows_walk(order, n_tiles, tiles_max, top_k, row16, [&](int64_t r, int64_t v, int c) { to[r * row16 + c] = __ldg(x + v * row16 + c); });
 }
 
 }  // namespace
@@ -258,11 +262,12 @@ it_status it_launch_experts_plan(const it_experts_args &a, const it_experts_plan
 }
 
 it_status it_launch_experts_parts(const it_experts_parts &q, int sms, cudaStream_t st) {
-  int64_t most = 0, total = 0;
+  const int64_t rows = q.tiles_max * PLAN_TILE * q.row;
+  int64_t most = rows, total = rows;
   for (int i = 0; i < q.count; ++i) { most = q.elems[i] > most ? q.elems[i] : most; total += q.elems[i]; }
   const int64_t blocks = (most / 4 + 255) / 256, cap = (int64_t)sms * 8;
   IT_LAUNCH(IT_K_EXPERT_PARTS, 10.0 * total, 0, st,
-            IT_CUDA_TRY(it_launch_pdl(parts_kernel, dim3((unsigned)(blocks < cap ? blocks : cap), q.count), dim3(256), 0, st, q)));
+            IT_CUDA_TRY(it_launch_pdl(parts_kernel, dim3((unsigned)(blocks < cap ? blocks : cap), q.count + 1), dim3(256), 0, st, q)));
   return IT_OK;
 }
 
