@@ -38,6 +38,7 @@ struct ExParams {
   int n_splits, bn, cols_per_tile;   // column tiles; columns of an accumulator; columns of the result in a tile (gated: bn / 2)
   int K, kb, passes;                 // k-blocks of a pass; passes: 1, or the six products of fp32 parts
   int stages;
+  int halves;                        // 2: either half of K has an accumulator of its own, and a tile both of them (fp32)
   int box_panels;                    // panels of W that one copy fetches, or 0: a copy each
   int gather_div;                    // > 0: row of A = place / gather_div; 0: row = position
   int a_rows;                        // rows of one part of A
@@ -109,6 +110,7 @@ expert_gemm_kernel(const __grid_constant__ CUtensorMap map_a, const __grid_const
   m_tiles = m_tiles < p.tiles_max ? m_tiles : p.tiles_max;
   const uint32_t splits = (uint32_t)p.n_splits, n_tiles = (uint32_t)m_tiles * splits;   // (below 2^31)
   const int KB = p.kb * p.passes;
+  const uint32_t bufs = p.halves == 2 ? 1u : 2u;   // accumulators of tiles in flight
 
   if (warp < EX_FETCH_WARPS) {
     // ------------------------------------------------------------------ producers: rows found by place by all four warps, 16 bytes a lane;
@@ -198,7 +200,7 @@ expert_gemm_kernel(const __grid_constant__ CUtensorMap map_a, const __grid_const
       ok = ex_wait_warp(&acc_empty[acc], acc_phase ^ 1u, abort_flag, p.spin_limit);
       if (!ok) break;
       tc_fence_after();
-      const uint32_t d_tmem = tmem_base + acc * (uint32_t)p.bn;
+      int kb_in_pass = 0;
       for (int kb = 0; kb < KB; ++kb) {
         ok = ex_wait_warp(&full[stage], phase, abort_flag, p.spin_limit);
         if (!ok) break;
@@ -206,15 +208,21 @@ expert_gemm_kernel(const __grid_constant__ CUtensorMap map_a, const __grid_const
         if (p.gather_div) asm volatile("fence.proxy.async.shared::cta;" ::: "memory");
         const uint32_t a_s = smem_u32(base) + stage * (uint32_t)stage_bytes;
         const uint64_t a_d = make_desc(a_s), b_d = make_desc_mn(a_s + EX_STAGE_A, PANEL);
+        // (two halves: the first product into either of them is the first pass's)
+        const int half_at = p.kb / 2;
+        const bool second = p.halves == 2 && kb_in_pass >= half_at;
+        const uint32_t d_tmem = tmem_base + (p.halves == 2 ? (second ? (uint32_t)p.bn : 0u) : acc * (uint32_t)p.bn);
+        const bool begun = second ? kb > half_at : kb > 0;
 #pragma unroll
         for (int k = 0; k < 4; ++k)   // four steps of 32 bytes of K: a quarter of the k-block's rows of W
-          ex_mma<EIGHT>(lead, d_tmem, a_d + k * 2, b_d + k * (PANEL / 64), idesc, (kb | k) != 0);
+          ex_mma<EIGHT>(lead, d_tmem, a_d + k * 2, b_d + k * (PANEL / 64), idesc, begun || k != 0);
+        if (++kb_in_pass == p.kb) kb_in_pass = 0;
         ex_commit(lead, &empty[stage]);
         if (++stage == (uint32_t)p.stages) { stage = 0; phase ^= 1u; }
       }
       if (!ok) break;
       ex_commit(lead, &acc_full[acc]);
-      if (++acc == 2) { acc = 0; acc_phase ^= 1u; }
+      if (++acc == bufs) { acc = 0; acc_phase ^= 1u; }
     }
     ex_commit(lead, mma_done);
     mbar_drain(mma_done, 0);
@@ -269,7 +277,7 @@ expert_gemm_kernel(const __grid_constant__ CUtensorMap map_a, const __grid_const
       }
       __syncwarp();
       if (lane == 0) mbar_arrive(&meta_full[acc]);
-      if (++acc == 2) { acc = 0; acc_phase ^= 1u; }
+      if (++acc == bufs) { acc = 0; acc_phase ^= 1u; }
     }
   } else {
     // ------------------------------------------------------------------ epilogue: a thread per row of the tile, a warp per 32 rows and step of columns
@@ -277,6 +285,7 @@ expert_gemm_kernel(const __grid_constant__ CUtensorMap map_a, const __grid_const
     constexpr bool F32_OUT = STORE == IT_EXPERT_SUMS || STORE == IT_EXPERT_OUT_F32, DIRECT = STORE == IT_EXPERT_OUT_BF16 || STORE == IT_EXPERT_OUT_F32;
     constexpr int ESIZE = F32_OUT ? 4 : 2, COLS = 64 / ESIZE;   // 64 bytes of a row are staged at a time
     constexpr int PLANES = STORE == IT_EXPERT_PARTS ? 3 : 1;
+    constexpr bool MAY_SPLIT = !EIGHT && (STORE == IT_EXPERT_PARTS || F32_OUT);
     constexpr int ROW = DIRECT ? 128 : 64, PIECES = ROW / 16, AT_ONCE = 32 / PIECES;   // staging tile: bytes of a row, its lanes, rows that a warp stores at once
     const uint32_t stage_s = smem_u32(staging) + (uint32_t)(warp - EX_EPI_WARP0) * ex_staging(STORE);
     // 16-byte pieces are swizzled: this lane's row as it writes it (piece i: put ^ 16 i), and its piece of every row that it stores
@@ -417,17 +426,28 @@ expert_gemm_kernel(const __grid_constant__ CUtensorMap map_a, const __grid_const
         }
       };
       // (the next 32 columns read ahead would take registers that are not there: with them spilled the epilogue took twice as long)
+      auto read = [&](int col, uint32_t (&r)[32]) {
+        tmem_ld32(taddr + (uint32_t)col, r);
+        if (MAY_SPLIT && p.halves == 2) {
+          uint32_t q[32];
+          tmem_ld32(taddr + (uint32_t)(p.bn + col), q);
+          tmem_ld_wait();
+#pragma unroll
+          for (int i = 0; i < 32; ++i) r[i] = __float_as_uint(__uint_as_float(r[i]) + __uint_as_float(q[i]));
+        } else {
+          tmem_ld_wait();
+        }
+      };
       uint32_t r[32], r2[GATED ? 32 : 1];
       for (int c = lo; c < hi; c += 32) {
-        tmem_ld32(taddr + (uint32_t)c, r);
-        if constexpr (GATED) tmem_ld32(taddr + (uint32_t)(p.cols_per_tile + c), r2);
-        tmem_ld_wait();
+        read(c, r);
+        if constexpr (GATED) read(p.cols_per_tile + c, r2);
         finish(r, r2, c);
       }
       tc_fence_before();
       __syncwarp();
       if (lane == 0) mbar_arrive(&acc_empty[acc]);
-      if (++acc == 2) { acc = 0; acc_phase ^= 1u; }
+      if (++acc == bufs) { acc = 0; acc_phase ^= 1u; }
     }
   }
 
@@ -468,6 +488,9 @@ it_status it_launch_expert_gemm(const it_experts_args &a, const it_experts_plan 
   p.cols_per_tile = ((g.cols + p.n_splits - 1) / p.n_splits + BK - 1) / BK * BK;
   p.n_splits = (g.cols + p.cols_per_tile - 1) / p.cols_per_tile;
   p.bn = g.gated ? 2 * p.cols_per_tile : p.cols_per_tile;
+  // A tensor core cuts off what it adds to an accumulator, which pulls long sums towards zero: fp32, 2-norm of the error for K = 256, 512, 1024, 2048
+  // 3.5e-7, 6.1e-7, 1.2e-6, 2.1e-6 (a library's fp32 product 3e-7 to 7e-7).  Above K = 512 either half of K has an accumulator of its own (K = 1024, 2048: 6.9e-7, 9.8e-7).
+  p.halves = g.parts == 3 && g.K > 512 ? 2 : 1;
 
   const cuuint64_t da[2] = {(cuuint64_t)g.K, (cuuint64_t)(g.a_rows * g.parts)}, sa[1] = {(cuuint64_t)g.K * elem};
   const cuuint32_t ba[2] = {(cuuint32_t)BK, (cuuint32_t)TC_BM};
