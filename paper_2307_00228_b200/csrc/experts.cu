@@ -64,6 +64,16 @@ __global__ void __launch_bounds__(ROWS_THREADS) expert_rows_kernel(const RowsPar
   const int col = c0 + cl * N;
   if (SECOND) {
     it_allow_next();
+    // the weights are on their way while the hidden rows are made (the first product starts this kernel when all before it is over)
+    // (of few vertices: of many the copies are in the way, fp32 256-1024-256, 256 places 78.6 -> 88 us)
+    if (p.units <= 8 && cl == 0 && col < p.cols)
+      for (int j = 0; j < p.k; ++j) {
+        const int e = p.ids[unit * p.k + j];
+        if ((unsigned)e >= (unsigned)p.n_experts) continue;
+        const int lo = (int)((int64_t)p.K * share / shares), hi = (int)((int64_t)p.K * (share + 1) / shares);
+        for (int r = lo + warp * (32 / ROWS_COL_LANES) + rl; r < hi; r += ROWS_STEP)
+          asm volatile("prefetch.global.L2 [%0];" ::"l"(reinterpret_cast<const TW *>(p.W) + ((int64_t)e * p.K + r) * p.w_cols + col));
+      }
     it_wait_prior();   // the hidden rows
   } else {
     it_wait_prior();
@@ -279,11 +289,19 @@ it_status check(const it_experts_desc *d, int64_t n) {
   return IT_OK;
 }
 
-// Few places keep the form by place.  FEW_PLACES
-constexpr int64_t kFewPlaces = 64;
+// Few places keep the form by place, whose time grows with the weights that its places read.  By place against sorted, us (captured): bf16 64-256-64
+// 64 places 8.3 / 10.2, 128 10.8 / 10.7; 256-256 64 6.9 / 9.5, 128 10.6 / 9.7; 128-512-128 (64 experts) 64 11.3 / 14.2, 128 19.6 / 14.4; 256-1024-256
+// 64 22.4 / 24.1, 128 31.9 / 24.2; gated 768-1024-768 16 26.7 / 30.3, 32 40.6 / 33.0.  fp32, whose sorted form splits all weights first:
+// 64-256-64 256 21.9 / 30.9, 512 32.0 / 32.3; 256-1024-256 128 44.9 / 80.9, 256 78.6 / 82.2.
+bool few_form(const it_experts_desc &d, int64_t places) {
+  const bool f32 = d.feat_dtype == IT_F32;
+  const int64_t first = d.hidden_dim > 0 ? (int64_t)d.hidden_dim * (d.gated ? 2 : 1) : d.out_dim;
+  const int64_t bytes = (int64_t)d.in_dim * first * (f32 ? 4 : (d.in_dtype == IT_E4M3 ? 1 : 2)) + (int64_t)d.hidden_dim * d.out_dim * (f32 ? 4 : 2);
+  return places <= (f32 ? 448 : 96) && places * bytes <= (f32 ? (int64_t)512 << 20 : (int64_t)80 << 20);
+}
 
 // Products that are not fused and take their rows more than once, for several tiles of columns, have them put in order first: fetched by place, a
-// k-block of 128 rows takes 1000 cycles, twice the product's (40k vertices, 4 of 32, 768-1024 gated: ROWSFIG).
+// k-block of 128 rows takes 1000 cycles, twice the product's (40k vertices, 4 of 32, 768-1024-768 gated, rows in order and both products 837 -> 794 us).
 bool rows_in_order(const it_experts_desc &d) {
   if (it_experts_fused(d)) return false;
   const int cols = d.hidden_dim > 0 ? d.hidden_dim : d.out_dim;
@@ -306,7 +324,7 @@ it_status plan(const it_experts_desc *d, int64_t n, ExpertsWs *w) {
   const size_t cols = (size_t)(d->hidden_dim > 0 ? d->hidden_dim : d->out_dim);
   size_t off = kStatusBytes;
   auto take = [&](size_t bytes) { const size_t o = off; off += it_align_up(bytes); return o; };
-  w->few = places <= kFewPlaces;
+  w->few = few_form(*d, places);
   if (w->few) {
     w->off_rows = take((size_t)places * cols * 4);
   } else {
