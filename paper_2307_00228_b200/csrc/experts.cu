@@ -268,7 +268,7 @@ it_status few_places(const it_experts_args &a, float *hidden, cudaStream_t st) {
 }
 
 // ----------------------------------------------------------------------------- checks and scratch
-constexpr int kMaxDim = 1 << 20, kMaxExperts = 4096;
+constexpr int kMaxDim = 1 << 16, kMaxExperts = 4096;
 
 it_status check(const it_experts_desc *d, int64_t n) {
   IT_REQUIRE(d != nullptr, IT_ERR_INVALID_ARG, "description is NULL");

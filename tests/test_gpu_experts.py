@@ -163,3 +163,31 @@ def test_waits_that_run_out_are_reported_and_over(kind, h, k):
     with pytest.raises(B.ItError, match="IT_ERR_TIMEOUT"):
         B.it_experts_check(ws)
     check_experts(c, run_experts(c, desc=d, workspace=ws))
+
+
+def test_offsets_past_32_bits():
+    """Typed vertices whose rows lie beyond 2^31 elements, in and out."""
+    n, a, o = (1 << 31) // 128 + 1500, 128, 128
+    c = experts_case(23, 1000, 2, 1, a, 0, o, BF16)
+    x = torch.zeros(n, a, dtype=BF16, device="cuda")
+    ids, w = torch.zeros(n, 1, dtype=torch.int32, device="cuda"), torch.ones(n, 1, device="cuda")
+    x[-1000:], ids[-1000:], w[-1000:] = c["x"].cuda(), c["ids"].cuda(), c["weights"].cuda()
+    d = experts_desc(c)
+    out = torch.full((n, o), float("nan"), dtype=BF16, device="cuda")
+    ws = torch.empty(B.it_experts_workspace_bytes(d, n), dtype=torch.uint8, device="cuda")
+    B.it_experts_forward(d, x, ids, w, out, ws)
+    B.it_experts_check(ws)
+    check_experts(c, out[-1000:])
+    first = run_experts({**c, "n": 8, "x": c["x"][:8] * 0, "ids": c["ids"][:8] * 0, "weights": c["weights"][:8] * 0 + 1}, desc=d)
+    assert torch.equal(out[:8], first[:8])
+
+
+@pytest.mark.parametrize("kind", ["bf16", "f32"])
+def test_one_workspace_for_calls_in_turn(kind):
+    """Different sizes and forms one after the other in the same scratch, large enough for each."""
+    cs = [experts_case(30 + n, n, 4, 2, 64, 128, 64, F32 if kind == "f32" else BF16) for n in (3, 900, 40, 5000, 3)]
+    ds = [experts_desc(c) for c in cs]
+    ws = torch.full((max(B.it_experts_workspace_bytes(d, c["n"]) for c, d in zip(cs, ds)),), 0xff, dtype=torch.uint8, device="cuda")
+    for _ in range(2):
+        for c, d in zip(cs, ds):
+            check_experts(c, run_experts(c, desc=d, workspace=ws))

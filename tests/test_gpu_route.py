@@ -153,3 +153,15 @@ def test_other_stream_and_captured_replays():
 def test_no_rows():
     l = torch.empty(0, 8, device="cuda")
     B.it_route(B.RouteDesc(n_experts=8, top_k=2, logit_dtype=F32), l, torch.empty(0, 2, dtype=torch.int32, device="cuda"), torch.empty(0, 2, device="cuda"))
+
+
+def test_offsets_past_32_bits():
+    n, e = (1 << 31) // 16 + 100, 16
+    l = torch.zeros(n, e, dtype=BF16, device="cuda")
+    l[-50:] = _logits(7, 50, e, BF16)
+    d = B.RouteDesc(n_experts=e, top_k=1, logit_dtype=BF16)
+    ids, w = torch.empty(n, 1, dtype=torch.int32, device="cuda"), torch.empty(n, 1, device="cuda")
+    B.it_route(d, l, ids, w)
+    rid, rw = route_reference(d, l[-60:].float().cpu().numpy(), None)
+    assert np.array_equal(ids[-60:].cpu().numpy(), rid) and np.allclose(w[-60:].cpu().numpy(), rw, rtol=RTOL)
+    assert (ids[:1000] == 0).all()
