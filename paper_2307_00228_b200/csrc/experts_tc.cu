@@ -59,14 +59,16 @@ __device__ __forceinline__ void pass_parts(int passes, int i, int *pa, int *pb) 
   *pb = passes == 1 ? 0 : (int)((B >> (4 * i)) & 15u);
 }
 
-template <bool EIGHT, it_expert_store STORE, bool GATED>
+// TRI (fp32, K up to 512): a stage holds the three parts of a k-block of either operand, and an accumulator of its own takes the small products.
+template <bool EIGHT, it_expert_store STORE, bool GATED, bool TRI>
 __global__ void __launch_bounds__(EX_THREADS, 1)
 expert_gemm_kernel(const __grid_constant__ CUtensorMap map_a, const __grid_constant__ CUtensorMap map_w, const ExParams p) {
   extern __shared__ __align__(1024) unsigned char base[];   // (the swizzle goes by addresses: stages start at multiples of 1024)
   const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
   constexpr int BK = EIGHT ? 128 : 64;                  // elements of a k-block, and columns of a panel
   constexpr int PANEL = BK * TC_KBLOCK_BYTES;           // bytes of a panel of W: BK rows x 128 bytes
-  const int b_bytes = p.bn * TC_KBLOCK_BYTES, stage_bytes = EX_STAGE_A + b_bytes;
+  constexpr int P = TRI ? 3 : 1;                        // parts in a stage: of A, then of W
+  const int b_bytes = p.bn * TC_KBLOCK_BYTES, stage_bytes = P * (EX_STAGE_A + b_bytes);
 
   unsigned char *staging = base + (size_t)p.stages * stage_bytes;
   using Meta = std::conditional_t<EIGHT, ExMetaEight, ExMeta>;
@@ -80,7 +82,7 @@ expert_gemm_kernel(const __grid_constant__ CUtensorMap map_a, const __grid_const
   uint32_t *tmem_slot = reinterpret_cast<uint32_t *>(mma_done + 1);
   volatile int *abort_flag = reinterpret_cast<volatile int *>(tmem_slot + 1);
   uint32_t tmem_cols = 32;
-  while (tmem_cols < 2u * (uint32_t)p.bn) tmem_cols <<= 1;
+  while (tmem_cols < (TRI ? 4u : 2u) * (uint32_t)p.bn) tmem_cols <<= 1;
 
   if (threadIdx.x == 0) {
     for (int s = 0; s < p.stages; ++s) {
@@ -109,16 +111,16 @@ expert_gemm_kernel(const __grid_constant__ CUtensorMap map_a, const __grid_const
   int m_tiles = *p.n_tiles;
   m_tiles = m_tiles < p.tiles_max ? m_tiles : p.tiles_max;
   const uint32_t splits = (uint32_t)p.n_splits, n_tiles = (uint32_t)m_tiles * splits;   // (below 2^31)
-  const int KB = p.kb * p.passes;
-  const uint32_t bufs = p.halves == 2 ? 1u : 2u;   // accumulators of tiles in flight
+  const int passes = TRI ? 1 : p.passes, KB = p.kb * passes;
+  const uint32_t bufs = !TRI && p.halves == 2 ? 1u : 2u, acc_stride = (uint32_t)p.bn * (TRI ? 2u : 1u);   // accumulators of tiles in flight
 
   if (warp < EX_FETCH_WARPS) {
     // ------------------------------------------------------------------ producers: rows found by place by all four warps, 16 bytes a lane;
     // weights, and rows in order, by TMA from the first
     uint32_t stage = 0, phase = 0;
-    const bool gather = p.gather_div > 0;
+    const bool gather = !TRI && p.gather_div > 0;
     bool ok = !p.no_loads && (warp == 0 || gather), came_round = false;
-    const uint32_t tma_bytes = (gather ? 0 : EX_STAGE_A) + b_bytes;
+    const uint32_t tma_bytes = P * ((gather ? 0 : EX_STAGE_A) + b_bytes);
     const int chunk = lane & 7;
     uint32_t dst[8];   // where this lane's 16 bytes of its eight rows go in a stage (128-byte swizzle)
 #pragma unroll
@@ -150,9 +152,9 @@ expert_gemm_kernel(const __grid_constant__ CUtensorMap map_a, const __grid_const
           real |= (r >= 0 ? 1u : 0u) << i;
         }
       }
-      for (int pass = 0; pass < p.passes && ok; ++pass) {
+      for (int pass = 0; pass < passes && ok; ++pass) {
         int pa, pb;
-        pass_parts(p.passes, pass, &pa, &pb);
+        pass_parts(passes, pass, &pa, &pb);
         for (int kb = 0; kb < p.kb; ++kb) {
           if (lane == 0) {
             ok = mbar_wait(&empty[stage], phase ^ 1u, abort_flag, p.spin_limit, EX_TMA_BACKOFF);
@@ -162,15 +164,19 @@ expert_gemm_kernel(const __grid_constant__ CUtensorMap map_a, const __grid_const
           if (!ok) break;
           unsigned char *to = base + (size_t)stage * stage_bytes;
           if (warp == 0) {
-            if (lane == 8 && !gather) tma_load_2d(to, &map_a, kb * BK, pa * p.a_rows + m * TC_BM, &full[stage]);
-            const int w_mat = pb * p.n_experts + e;
+            if (lane >= 8 && lane < 8 + P && !gather) tma_load_2d(to + (lane - 8) * EX_STAGE_A, &map_a, kb * BK, (TRI ? lane - 8 : pa) * p.a_rows + m * TC_BM, &full[stage]);
+            unsigned char *to_w = to + P * EX_STAGE_A;
             if (p.box_panels > 0) {   // runs of panels in a copy each
               // gated: the first half of the panels are columns of the gate, the second of what it gates
-              if (lane == 16 || (GATED && lane == 17))
-                tma_load_4d(to + EX_STAGE_A + (lane - 16) * p.box_panels * PANEL, &map_w, 0, kb * BK, (lane == 17 ? p.cols + c0 : c0) / BK, w_mat, &full[stage]);
-            } else if (lane >= 16 && lane - 16 < p.bn / BK) {   // a panel of the weights a lane
-              const int c = (lane - 16) * BK, col = GATED && c >= p.cols_per_tile ? p.cols + c0 + c - p.cols_per_tile : c0 + c;
-              tma_load_3d(to + EX_STAGE_A + (lane - 16) * PANEL, &map_w, col, kb * BK, w_mat, &full[stage]);
+              constexpr int RUNS = GATED ? 2 : 1;
+              if (lane >= 16 && lane < 16 + RUNS * P) {
+                const int run = (lane - 16) % RUNS, part = (lane - 16) / RUNS;
+                tma_load_4d(to_w + part * b_bytes + run * p.box_panels * PANEL, &map_w, 0, kb * BK, (run ? p.cols + c0 : c0) / BK, (TRI ? part : pb) * p.n_experts + e, &full[stage]);
+              }
+            } else if (lane >= 16 && lane - 16 < P * p.bn / BK) {   // a panel of the weights a lane
+              const int panels = p.bn / BK, part = (lane - 16) / panels, c = (lane - 16) % panels * BK;
+              const int col = GATED && c >= p.cols_per_tile ? p.cols + c0 + c - p.cols_per_tile : c0 + c;
+              tma_load_3d(to_w + (lane - 16) * PANEL, &map_w, col, kb * BK, (TRI ? part : pb) * p.n_experts + e, &full[stage]);
             }
             __syncwarp();
           }
@@ -207,16 +213,29 @@ expert_gemm_kernel(const __grid_constant__ CUtensorMap map_a, const __grid_const
         // gathered rows were written by the threads of the other warps: what follows reads them through the tensor core's path
         if (p.gather_div) asm volatile("fence.proxy.async.shared::cta;" ::: "memory");
         const uint32_t a_s = smem_u32(base) + stage * (uint32_t)stage_bytes;
-        const uint64_t a_d = make_desc(a_s), b_d = make_desc_mn(a_s + EX_STAGE_A, PANEL);
-        // (two halves: the first product into either of them is the first pass's)
-        const int half_at = p.kb / 2;
-        const bool second = p.halves == 2 && kb_in_pass >= half_at;
-        const uint32_t d_tmem = tmem_base + (p.halves == 2 ? (second ? (uint32_t)p.bn : 0u) : acc * (uint32_t)p.bn);
-        const bool begun = second ? kb > half_at : kb > 0;
+        if constexpr (TRI) {
+          const uint32_t d_main = tmem_base + acc * acc_stride, d_small = d_main + (uint32_t)p.bn;
 #pragma unroll
-        for (int k = 0; k < 4; ++k)   // four steps of 32 bytes of K: a quarter of the k-block's rows of W
-          ex_mma<EIGHT>(lead, d_tmem, a_d + k * 2, b_d + k * (PANEL / 64), idesc, begun || k != 0);
-        if (++kb_in_pass == p.kb) kb_in_pass = 0;
+          for (int pass = 0; pass < 6; ++pass) {
+            int pa, pb;
+            pass_parts(6, pass, &pa, &pb);
+            const uint64_t a_d = make_desc(a_s + pa * EX_STAGE_A), b_d = make_desc_mn(a_s + 3 * EX_STAGE_A + (uint32_t)(pb * b_bytes), PANEL);
+#pragma unroll
+            for (int k = 0; k < 4; ++k)
+              ex_mma<false>(lead, pass == 5 ? d_main : d_small, a_d + k * 2, b_d + k * (PANEL / 64), idesc, kb > 0 || k != 0 || (pass != 0 && pass != 5));
+          }
+        } else {
+          const uint64_t a_d = make_desc(a_s), b_d = make_desc_mn(a_s + EX_STAGE_A, PANEL);
+          // (two halves: the first product into either of them is the first pass's)
+          const int half_at = p.kb / 2;
+          const bool second = p.halves == 2 && kb_in_pass >= half_at;
+          const uint32_t d_tmem = tmem_base + (p.halves == 2 ? (second ? (uint32_t)p.bn : 0u) : acc * acc_stride);
+          const bool begun = second ? kb > half_at : kb > 0;
+#pragma unroll
+          for (int k = 0; k < 4; ++k)   // four steps of 32 bytes of K: a quarter of the k-block's rows of W
+            ex_mma<EIGHT>(lead, d_tmem, a_d + k * 2, b_d + k * (PANEL / 64), idesc, begun || k != 0);
+          if (++kb_in_pass == p.kb) kb_in_pass = 0;
+        }
         ex_commit(lead, &empty[stage]);
         if (++stage == (uint32_t)p.stages) { stage = 0; phase ^= 1u; }
       }
@@ -311,7 +330,7 @@ expert_gemm_kernel(const __grid_constant__ CUtensorMap map_a, const __grid_const
 #pragma unroll
         for (int i = 0; i < 4; ++i) real |= (k.place[quarter * 32 + 8 * i + row0] >= 0 ? 1u : 0u) << i;
       }
-      const uint32_t taddr = tmem_base + ((uint32_t)(quarter * 32) << 16) + acc * (uint32_t)p.bn;
+      const uint32_t taddr = tmem_base + ((uint32_t)(quarter * 32) << 16) + acc * acc_stride;
       const int width = p.cols - c_tile < p.cols_per_tile ? p.cols - c_tile : p.cols_per_tile;
       // 64 bytes of this lane's row into the staging tile ...
       auto stage = [&](const uint32_t *w, int half) {
@@ -428,7 +447,7 @@ expert_gemm_kernel(const __grid_constant__ CUtensorMap map_a, const __grid_const
       // (the next 32 columns read ahead would take registers that are not there: with them spilled the epilogue took twice as long)
       auto read = [&](int col, uint32_t (&r)[32]) {
         tmem_ld32(taddr + (uint32_t)col, r);
-        if (MAY_SPLIT && p.halves == 2) {
+        if (TRI || (MAY_SPLIT && p.halves == 2)) {
           uint32_t q[32];
           tmem_ld32(taddr + (uint32_t)(p.bn + col), q);
           tmem_ld_wait();
@@ -463,10 +482,10 @@ expert_gemm_kernel(const __grid_constant__ CUtensorMap map_a, const __grid_const
 }
 
 // ----------------------------------------------------------------------------- host side
-template <bool EIGHT, it_expert_store STORE, bool GATED>
+template <bool EIGHT, it_expert_store STORE, bool GATED, bool TRI = false>
 it_status launch(const CUtensorMap &ma, const CUtensorMap &mw, const ExParams &p, int grid, int smem, double bytes, double flops, cudaStream_t st) {
-  IT_CUDA_TRY(cudaFuncSetAttribute(expert_gemm_kernel<EIGHT, STORE, GATED>, cudaFuncAttributeMaxDynamicSharedMemorySize, smem));
-  IT_LAUNCH(IT_K_EXPERT_GEMM, bytes, flops, st, IT_CUDA_TRY(it_launch_pdl(expert_gemm_kernel<EIGHT, STORE, GATED>, dim3((unsigned)grid), dim3(EX_THREADS), smem, st, ma, mw, p)));
+  IT_CUDA_TRY(cudaFuncSetAttribute(expert_gemm_kernel<EIGHT, STORE, GATED, TRI>, cudaFuncAttributeMaxDynamicSharedMemorySize, smem));
+  IT_LAUNCH(IT_K_EXPERT_GEMM, bytes, flops, st, IT_CUDA_TRY(it_launch_pdl(expert_gemm_kernel<EIGHT, STORE, GATED, TRI>, dim3((unsigned)grid), dim3(EX_THREADS), smem, st, ma, mw, p)));
   return IT_OK;
 }
 
@@ -482,15 +501,19 @@ it_status it_launch_expert_gemm(const it_experts_args &a, const it_experts_plan 
   p.bias = g.bias; p.w_scale = g.w_scale; p.x_scale = g.x_scale; p.weights = a.weights; p.x_div = a.d.top_k;
   p.dst = g.dst; p.part_stride = q.tiles_max * TC_BM * (int64_t)g.cols; p.status = a.status;
   p.spin_limit = g.spin_limit ? g.spin_limit : TC_SPIN_LIMIT; p.no_loads = g.no_loads;
+  // fp32: with the parts of a k-block in one stage they are fetched once instead of twice each, and the six products are issued behind one wait; two stages
+  // and the second accumulator leave 128 columns (64 where rows are stored 128 bytes at a time).
+  const bool tri = g.parts == 3 && g.K <= 512;
   // columns in as few tiles as 256 accumulator columns allow, of equal width in whole panels
-  const int most = g.gated ? 128 : 256;
+  const int most = (tri ? (ex_direct(g.store) ? 64 : 128) : 256) / (g.gated ? 2 : 1);
   p.n_splits = (g.cols + most - 1) / most;
   p.cols_per_tile = ((g.cols + p.n_splits - 1) / p.n_splits + BK - 1) / BK * BK;
   p.n_splits = (g.cols + p.cols_per_tile - 1) / p.cols_per_tile;
   p.bn = g.gated ? 2 * p.cols_per_tile : p.cols_per_tile;
   // A tensor core cuts off what it adds to an accumulator, which pulls long sums towards zero: fp32, 2-norm of the error for K = 256, 512, 1024, 2048
-  // 3.5e-7, 6.1e-7, 1.2e-6, 2.1e-6 (a library's fp32 product 3e-7 to 7e-7).  Above K = 512 either half of K has an accumulator of its own (K = 1024, 2048: 6.9e-7, 9.8e-7).
-  p.halves = g.parts == 3 && g.K > 512 ? 2 : 1;
+  // 3.5e-7, 6.1e-7, 1.2e-6, 2.1e-6 (a library's fp32 product 3e-7 to 7e-7).  Above K = 512 either half of K has an accumulator of its own (K = 1024,
+  // 2048: 6.9e-7, 9.8e-7), and the parts go by one after the other, the smallest products first.
+  p.halves = g.parts == 3 && !tri ? 2 : 1;
 
   const cuuint64_t da[2] = {(cuuint64_t)g.K, (cuuint64_t)(g.a_rows * g.parts)}, sa[1] = {(cuuint64_t)g.K * elem};
   const cuuint32_t ba[2] = {(cuuint32_t)BK, (cuuint32_t)TC_BM};
@@ -511,7 +534,7 @@ it_status it_launch_expert_gemm(const it_experts_args &a, const it_experts_plan 
     IT_TRY(encode(&mw, g.eight, g.W, 3, dw, sw, bw));
   }
 
-  const int stage = EX_STAGE_A + p.bn * TC_KBLOCK_BYTES, fixed = EX_EPI_WARPS * ex_staging(g.store) + 2 * (int)(g.eight ? sizeof(ExMetaEight) : sizeof(ExMeta)) + (2 * EX_MAX_STAGES + 9) * 8;
+  const int stage = (tri ? 3 : 1) * (EX_STAGE_A + p.bn * TC_KBLOCK_BYTES), fixed = EX_EPI_WARPS * ex_staging(g.store) + 2 * (int)(g.eight ? sizeof(ExMetaEight) : sizeof(ExMeta)) + (2 * EX_MAX_STAGES + 9) * 8;
   p.stages = (227 * 1024 - fixed) / stage;
   if (p.stages > EX_MAX_STAGES) p.stages = EX_MAX_STAGES;
   const int smem = fixed + p.stages * stage;
@@ -521,21 +544,27 @@ it_status it_launch_expert_gemm(const it_experts_args &a, const it_experts_plan 
   const int64_t places = a.n * a.d.top_k;
   const double flops = 2.0 * places * g.K * (double)g.w_cols, bytes = (double)places * (g.K * elem * g.parts + g.cols * 4.0);
 #define IT_EX_LAUNCH(EIGHT, STORE, GATED) return launch<EIGHT, STORE, GATED>(ma, mw, p, grid, smem, bytes, flops, st)
+#define IT_EX_TRI(STORE, GATED) if (tri) return launch<false, STORE, GATED, true>(ma, mw, p, grid, smem, bytes, flops, st)
   switch (g.store) {
     case IT_EXPERT_HIDDEN:
       if (g.eight) { if (g.gated) IT_EX_LAUNCH(true, IT_EXPERT_HIDDEN, true); else IT_EX_LAUNCH(true, IT_EXPERT_HIDDEN, false); }
       if (g.gated) IT_EX_LAUNCH(false, IT_EXPERT_HIDDEN, true);
       IT_EX_LAUNCH(false, IT_EXPERT_HIDDEN, false);
     case IT_EXPERT_PARTS:
-      if (g.gated) IT_EX_LAUNCH(false, IT_EXPERT_PARTS, true);
+      if (g.gated) { IT_EX_TRI(IT_EXPERT_PARTS, true); IT_EX_LAUNCH(false, IT_EXPERT_PARTS, true); }
+      IT_EX_TRI(IT_EXPERT_PARTS, false);
       IT_EX_LAUNCH(false, IT_EXPERT_PARTS, false);
     case IT_EXPERT_SUMS:
       if (g.eight) IT_EX_LAUNCH(true, IT_EXPERT_SUMS, false);
+      IT_EX_TRI(IT_EXPERT_SUMS, false);
       IT_EX_LAUNCH(false, IT_EXPERT_SUMS, false);
     case IT_EXPERT_OUT_BF16:
       if (g.eight) IT_EX_LAUNCH(true, IT_EXPERT_OUT_BF16, false);
       IT_EX_LAUNCH(false, IT_EXPERT_OUT_BF16, false);
-    default: IT_EX_LAUNCH(false, IT_EXPERT_OUT_F32, false);
+    default:
+      IT_EX_TRI(IT_EXPERT_OUT_F32, false);
+      IT_EX_LAUNCH(false, IT_EXPERT_OUT_F32, false);
   }
+#undef IT_EX_TRI
 #undef IT_EX_LAUNCH
 }
