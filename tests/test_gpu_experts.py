@@ -191,3 +191,35 @@ def test_one_workspace_for_calls_in_turn(kind):
     for _ in range(2):
         for c, d in zip(cs, ds):
             check_experts(c, run_experts(c, desc=d, workspace=ws))
+
+
+@pytest.mark.parametrize("kind,a,h,o,gated", [("bf16", 136, 200, 136, False), ("bf16", 200, 96, 192, True), ("bf16", 256, 512, 256, False), ("bf16", 248, 136, 72, True),
+                                              ("bf16", 64, 1000, 256, True), ("bf16", 256, 64, 16, False), ("eight", 272, 208, 136, False), ("eight", 400, 144, 64, False),
+                                              ("eight", 512, 272, 256, False), ("eight", 112, 528, 200, False)])
+@pytest.mark.parametrize("n,k", [(700, 1), (2501, 2), (30_003, 2)])
+def test_wide_rows_of_both_products_at_once(kind, a, h, o, gated, n, k):
+    """Rows that fill several panels, results of more than 128 columns, widths that end inside a panel."""
+    c = experts_case(a + h + o + n, n, 6, k, a, h, o, BF16, eight=kind == "eight", gated=gated, act="silu" if gated else "relu", masked=0.1)
+    check_experts(c, run_experts(c), device="cuda")
+
+
+@pytest.mark.parametrize("a,h,o,k,gated", [(256, 1024, 256, 2, False), (544, 0, 72, 1, False), (1024, 520, 136, 2, True), (512, 512, 128, 1, True), (520, 528, 64, 2, False),
+                                           (8, 504, 8, 3, False), (2048, 0, 264, 1, False)])
+@pytest.mark.parametrize("n", [500, 6001])
+def test_long_sums_in_fp32(a, h, o, k, gated, n):
+    """Sums of up to 512 terms and of more take accumulators of different kinds."""
+    c = experts_case(a + h + o + n, n, 5, k, a, h, o, F32, gated=gated, act="elu", masked=0.1)
+    check_experts(c, run_experts(c), device="cuda")
+
+
+@pytest.mark.parametrize("kind,a,h,o,gated", [("f32", 576, 640, 64, True), ("bf16", 256, 192, 256, False), ("bf16", 320, 128, 320, False), ("eight", 512, 64, 136, False)])
+def test_waits_that_run_out_in_wide_rows(kind, a, h, o, gated):
+    c = experts_case(24, 40_000, 4, 2, a, h, o, F32 if kind == "f32" else BF16, eight=kind == "eight", gated=gated)
+    d = experts_desc(c)
+    dev = lambda t: None if t is None else t.cuda()   # noqa: E731
+    out = torch.empty(40_000, o, dtype=c["dtype"], device="cuda")
+    ws = torch.empty(B.it_experts_workspace_bytes(d, 40_000), dtype=torch.uint8, device="cuda")
+    B.it_debug_expire_wait_experts(d, dev(c["x"]), dev(c["ids"]), dev(c["weights"]), out, ws, x_scale=dev(c["x_scale"]))
+    with pytest.raises(B.ItError, match="IT_ERR_TIMEOUT"):
+        B.it_experts_check(ws)
+    check_experts(c, run_experts(c, desc=d, workspace=ws), device="cuda")
