@@ -233,7 +233,7 @@ __global__ void __launch_bounds__(256) parts_kernel(const __grid_constant__ it_e
 __global__ void __launch_bounds__(256) rows_kernel(const uint4 *x, uint4 *to, int row16, int top_k, const int32_t *order, const int32_t *n_tiles, int64_t tiles_max) {
   it_allow_next();
   it_wait_prior();
-  it_experts_rows_walk(order, n_tiles, tiles_max, top_k, row16, [&](int64_t r, int64_t v, int c) { to[r * row16 + c] = __ldg(x + v * row16 + c); });
+  it_experts_rows_walk(order, n_tiles, tiles_max, top_k, row16, [&](int64_t r, int64_t v, int c) { to[r * row16 + c] = x[v * row16 + c]; });
 }
 
 }  // namespace

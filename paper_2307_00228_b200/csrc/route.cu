@@ -187,7 +187,7 @@ __global__ void __launch_bounds__(ROUTE_THREADS, C == 8 ? 8 : 1) route_kernel(co
       if constexpr (N == kVec<T>) {
         if (vec) {
           float v[N];
-          if (e0 < E) vec_to_f32(__ldg(reinterpret_cast<const uint4 *>(from + e0)), v);
+          if (e0 < E) vec_to_f32(*reinterpret_cast<const uint4 *>(from + e0), v);
 #pragma unroll
           for (int i = 0; i < N; ++i) key[c0 + i] = e0 < E ? open_logit(v[i]) : kClosed;
           continue;
@@ -472,7 +472,7 @@ __global__ void __launch_bounds__(ROUTE_THREADS) route_thread_kernel(const Route
 #pragma unroll
       for (int c0 = 0; c0 < C; c0 += N) {
         float v[N];
-        if (c0 < E) vec_to_f32(__ldg(reinterpret_cast<const uint4 *>(from + c0)), v);
+        if (c0 < E) vec_to_f32(*reinterpret_cast<const uint4 *>(from + c0), v);
 #pragma unroll
         for (int i = 0; i < N; ++i) key[c0 + i] = c0 < E ? open_logit(v[i]) : kClosed;
       }
