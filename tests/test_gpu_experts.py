@@ -223,3 +223,16 @@ def test_waits_that_run_out_in_wide_rows(kind, a, h, o, gated):
     with pytest.raises(B.ItError, match="IT_ERR_TIMEOUT"):
         B.it_experts_check(ws)
     check_experts(c, run_experts(c, desc=d, workspace=ws), device="cuda")
+
+
+@pytest.mark.parametrize("kind,a,h,o,gated", [("bf16", 64, 128, 64, False), ("bf16", 128, 72, 40, True), ("eight", 64, 64, 200, False)])
+@pytest.mark.parametrize("n,E,masked,repeat", [(60, 2, 0.0, False), (700, 4, 0.3, False), (700, 3, 0.0, True), (5000, 1, 0.2, True), (9001, 7, 0.5, True), (150_001, 8, 0.1, False)])
+def test_two_places_a_vertex(kind, a, h, o, gated, n, E, masked, repeat):
+    """The two rows of a vertex in the same tile, in tiles of the same time and of different times; one of them or both masked; the same result every time."""
+    c = experts_case(n + a + h, n, E, 2, a, h, o, BF16, eight=kind == "eight", gated=gated, act="silu" if gated else "relu", masked=masked, repeat=repeat)
+    d = experts_desc(c)
+    want = run_experts(c, desc=d)
+    check_experts(c, want, device="cuda")
+    ws = torch.full((B.it_experts_workspace_bytes(d, n),), 0xff, dtype=torch.uint8, device="cuda")
+    for _ in range(4):
+        assert torch.equal(run_experts(c, desc=d, workspace=ws), want)
