@@ -1,14 +1,19 @@
 // The places of it_experts_forward sorted by expert, and fp32 operands split into bf16 parts.
 //
-// A counting sort: counts per block and expert, their prefix sums, places written where they belong.  Few places take one block and one
-// launch.  The order of the places inside an expert differs from run to run (shared-memory atomics); no result depends on it: a row of
-// a product is the same wherever in a tile it lies, and the places of a vertex are added in their own order.
+// A counting sort: counts per block and expert, their prefix sums, places written where they belong.  Few places take one block, more a cluster
+// whose blocks read one another's counts, both in one launch; many a grid, in three.  The order of the places inside an expert differs from run to
+// run (shared-memory atomics); no result depends on it: a row of a product is the same wherever in a tile it lies, and the places of a vertex are
+// added in their own order.
+#include <cooperative_groups.h>
+
 #include "experts.cuh"
+
+namespace cg = cooperative_groups;
 
 namespace {
 
 constexpr int PLAN_THREADS = 1024, PLAN_TILE = 128;
-constexpr int64_t PLAN_ONE_BLOCK = 16384;   // places that one block sorts in one launch
+constexpr int PLAN_CLUSTER = 8, PLAN_CLUSTER_EXPERTS = 1024;   // (a cluster's blocks keep four words of shared memory an expert)
 constexpr int PLAN_BLOCKS = 256;
 
 struct PlanParams {
@@ -48,8 +53,8 @@ __device__ __forceinline__ int block_scan(int v, int *warp_sums, int *total) {
 }
 
 // count[e] (shared): places of every expert -> first position of every expert; tiles, padding and the number of tiles are written.
-// first: as many words of shared memory.
-__device__ void lay_out(const PlanParams &p, int *count, int *first, int *warp_sums) {
+// first: as many words of shared memory.  part of parts: the share of the writing that this block does.
+__device__ void lay_out(const PlanParams &p, int *count, int *first, int *warp_sums, int part = 0, int parts = 1) {
   int tiles_before = 0;
   for (int e0 = 0; e0 < p.n_experts; e0 += PLAN_THREADS) {
     const int e = e0 + threadIdx.x, tiles = e < p.n_experts ? (count[e] + PLAN_TILE - 1) / PLAN_TILE : 0;
@@ -58,15 +63,15 @@ __device__ void lay_out(const PlanParams &p, int *count, int *first, int *warp_s
     if (e < p.n_experts) first[e] = at;
     tiles_before += total;
   }
-  if (threadIdx.x == 0) *p.q.n_tiles = tiles_before;
+  if (threadIdx.x == 0 && part == 0) *p.q.n_tiles = tiles_before;
   __syncthreads();
-  for (int e = threadIdx.x >> 5; e < p.n_experts; e += PLAN_THREADS / 32) {
+  for (int e = part + parts * (threadIdx.x >> 5); e < p.n_experts; e += parts * (PLAN_THREADS / 32)) {
     const int lane = threadIdx.x & 31, c = count[e], t0 = first[e], t1 = t0 + (c + PLAN_TILE - 1) / PLAN_TILE;
     for (int t = t0 + lane; t < t1; t += 32) p.q.tile_expert[t] = e;
     for (int64_t i = (int64_t)t0 * PLAN_TILE + c + lane; i < (int64_t)t1 * PLAN_TILE; i += 32) p.q.order[i] = -1;
-    __syncwarp();
-    if (lane == 0) count[e] = t0 * PLAN_TILE;
   }
+  __syncthreads();
+  for (int e = threadIdx.x; e < p.n_experts; e += PLAN_THREADS) count[e] = first[e] * PLAN_TILE;
 }
 
 __device__ __forceinline__ void zero_row(const PlanParams &p, int64_t v) {
@@ -102,6 +107,86 @@ __global__ void __launch_bounds__(PLAN_THREADS) plan_one_kernel(const PlanParams
   }
 }
 
+// f(place, its id, whether it is one) for the places of this block, by whole warps; the ids of four rounds are fetched at once.
+template <typename F>
+__device__ __forceinline__ void walk_places(const PlanParams &p, F f) {
+  constexpr int AHEAD = 4;
+  const int lane = threadIdx.x & 31;
+  const int64_t lo = blockIdx.x * p.per_block, hi = lo + p.per_block < p.places ? lo + p.per_block : p.places;
+  for (int64_t i0 = lo + (threadIdx.x & ~31); i0 < hi; i0 += AHEAD * PLAN_THREADS) {
+    int e[AHEAD];
+#pragma unroll
+    for (int u = 0; u < AHEAD; ++u) {
+      const int64_t i = i0 + u * PLAN_THREADS + lane;
+      e[u] = i < hi ? p.ids[i] : -1;
+    }
+#pragma unroll
+    for (int u = 0; u < AHEAD; ++u) {
+      const int64_t i = i0 + u * PLAN_THREADS + lane;
+      if (i - lane < hi) f(i, e[u], i < hi);
+    }
+  }
+}
+
+// Adds the places of this block to count[e] (shared).
+__device__ __forceinline__ void count_block(const PlanParams &p, int *count) {
+  const int lane = threadIdx.x & 31;
+  walk_places(p, [&](int64_t, int e, bool) {
+    const unsigned same = __match_any_sync(0xffffffffu, e);   // one addition per expert and warp
+    if ((unsigned)e < (unsigned)p.n_experts && lane == __ffs(same) - 1) atomicAdd(&count[e], __popc(same));
+  });
+}
+
+// Writes the places of this block where they belong: next[e] (shared) is the next position of expert e.
+__device__ __forceinline__ void place_block(const PlanParams &p, int *next) {
+  const int lane = threadIdx.x & 31;
+  walk_places(p, [&](int64_t i, int e, bool in) {
+    const bool real = (unsigned)e < (unsigned)p.n_experts;
+    const unsigned same = __match_any_sync(0xffffffffu, e);
+    const int leader = __ffs(same) - 1;
+    int at = 0;
+    if (real && lane == leader) at = atomicAdd(&next[e], __popc(same));
+    at = __shfl_sync(0xffffffffu, at, leader) + __popc(same & ((1u << lane) - 1u));
+    if (real) {
+      p.q.order[at] = (int32_t)i;
+      p.q.position[i] = at;
+    } else if (p.zero_rows && in) {
+      zero_row(p, i);
+    }
+  });
+}
+
+// counts | of all blocks | first tiles | places of the blocks before, in shared memory.
+__global__ void __launch_bounds__(PLAN_THREADS) plan_cluster_kernel(const PlanParams p) {
+  it_allow_next();
+  it_wait_prior();
+  extern __shared__ int plan_smem[];
+  __shared__ int warp_sums[32];
+  cg::cluster_group cluster = cg::this_cluster();
+  int *count = plan_smem, *total = count + p.n_experts, *first = total + p.n_experts, *before = first + p.n_experts;
+  if (blockIdx.x == 0 && threadIdx.x == 0) *p.status = 0;
+  for (int e = threadIdx.x; e < p.n_experts; e += PLAN_THREADS) count[e] = 0;
+  __syncthreads();
+  count_block(p, count);
+  cluster.sync();
+  for (int e = threadIdx.x; e < p.n_experts; e += PLAN_THREADS) {
+    int sum = 0, mine = 0;
+#pragma unroll
+    for (int b = 0; b < PLAN_CLUSTER; ++b) {
+      if (b == (int)blockIdx.x) mine = sum;
+      sum += cluster.map_shared_rank(count, b)[e];
+    }
+    total[e] = sum;
+    before[e] = mine;
+  }
+  cluster.sync();   // nobody's counts go before they are read
+  lay_out(p, total, first, warp_sums, (int)blockIdx.x, PLAN_CLUSTER);
+  __syncthreads();
+  for (int e = threadIdx.x; e < p.n_experts; e += PLAN_THREADS) total[e] += before[e];
+  __syncthreads();
+  place_block(p, total);
+}
+
 __global__ void __launch_bounds__(PLAN_THREADS) plan_count_kernel(const PlanParams p) {
   it_allow_next();
   it_wait_prior();
@@ -109,13 +194,7 @@ __global__ void __launch_bounds__(PLAN_THREADS) plan_count_kernel(const PlanPara
   if (blockIdx.x == 0 && threadIdx.x == 0) *p.status = 0;
   for (int e = threadIdx.x; e < p.n_experts; e += PLAN_THREADS) plan_smem[e] = 0;
   __syncthreads();
-  const int64_t lo = blockIdx.x * p.per_block, hi = lo + p.per_block < p.places ? lo + p.per_block : p.places;
-  const int lane = threadIdx.x & 31;
-  for (int64_t i0 = lo + (threadIdx.x & ~31); i0 < hi; i0 += PLAN_THREADS) {   // (whole warps)
-    const int e = i0 + lane < hi ? p.ids[i0 + lane] : -1;
-    const unsigned same = __match_any_sync(0xffffffffu, e);   // one addition per expert and warp
-    if ((unsigned)e < (unsigned)p.n_experts && lane == __ffs(same) - 1) atomicAdd(&plan_smem[e], __popc(same));
-  }
+  count_block(p, plan_smem);
   __syncthreads();
   for (int e = threadIdx.x; e < p.n_experts; e += PLAN_THREADS) p.q.counts[(int64_t)blockIdx.x * p.n_experts + e] = plan_smem[e];
 }
@@ -154,24 +233,17 @@ __global__ void __launch_bounds__(PLAN_THREADS) plan_place_kernel(const PlanPara
   extern __shared__ int plan_smem[];
   for (int e = threadIdx.x; e < p.n_experts; e += PLAN_THREADS) plan_smem[e] = p.q.counts[(int64_t)blockIdx.x * p.n_experts + e];
   __syncthreads();
-  const int lane = threadIdx.x & 31;
-  const int64_t lo = blockIdx.x * p.per_block, hi = lo + p.per_block < p.places ? lo + p.per_block : p.places;
-  for (int64_t i0 = lo + (threadIdx.x & ~31); i0 < hi; i0 += PLAN_THREADS) {
-    const int64_t i = i0 + lane;
-    const int e = i < hi ? p.ids[i] : -1;
-    const bool real = (unsigned)e < (unsigned)p.n_experts;
-    const unsigned same = __match_any_sync(0xffffffffu, e);
-    const int leader = __ffs(same) - 1;
-    int at = 0;
-    if (real && lane == leader) at = atomicAdd(&plan_smem[e], __popc(same));
-    at = __shfl_sync(0xffffffffu, at, leader) + __popc(same & ((1u << lane) - 1u));
-    if (real) {
-      p.q.order[at] = (int32_t)i;
-      p.q.position[i] = at;
-    } else if (p.zero_rows && i < hi) {
-      zero_row(p, i);
-    }
-  }
+  place_block(p, plan_smem);
+}
+
+// The whole of it_experts_forward on bf16 64-256-64, us (captured), one block / a cluster / a grid: 8 experts, 3000 places 19.1 / 19.9 / -, 6000
+// 20.5 / 20.2 / -, 16000 25.4 / 22.1 / -, 24000 - / 30.8 / 33.1, 40000 - / 40.7 / 41.3, 80000 - / 62.0 / 59.7; 256 experts, 1400 30.7 / 27.8 / -,
+// 16000 41.3 / 32.9 / -, 40000 - / 55.0 / 64.9, 80000 - / 81.5 / 86.2, 130000 - / 112.1 / 111.4.
+enum PlanForm { PLAN_BLOCK, PLAN_CLUSTERED, PLAN_GRID };
+PlanForm plan_form(int64_t places, int n_experts) {
+  if (n_experts > PLAN_CLUSTER_EXPERTS) return places <= 16384 ? PLAN_BLOCK : PLAN_GRID;
+  if (places <= 6144 && n_experts <= 32) return PLAN_BLOCK;
+  return places <= 49152 + 128 * (int64_t)(n_experts < 256 ? n_experts : 256) ? PLAN_CLUSTERED : PLAN_GRID;
 }
 
 int plan_blocks(int64_t places) {
@@ -240,7 +312,7 @@ __global__ void __launch_bounds__(256) rows_kernel(const uint4 *x, uint4 *to, in
 
 int64_t it_experts_tiles_max(int64_t places, int n_experts) { return places / PLAN_TILE + (places < n_experts ? places : n_experts); }
 size_t it_experts_count_words(int64_t places, int n_experts) {
-  return places <= PLAN_ONE_BLOCK ? 0 : (size_t)plan_blocks(places) * (size_t)n_experts;
+  return plan_form(places, n_experts) != PLAN_GRID ? 0 : (size_t)plan_blocks(places) * (size_t)n_experts;
 }
 
 it_status it_launch_experts_plan(const it_experts_args &a, const it_experts_plan &q, cudaStream_t st) {
@@ -249,8 +321,21 @@ it_status it_launch_experts_plan(const it_experts_args &a, const it_experts_plan
   if (a.d.top_k == 1) { p.zero_rows = (char *)a.out; p.row_bytes = a.d.out_dim * it_dtype_size(a.d.feat_dtype); }
   const size_t smem = (size_t)p.n_experts * 8;
   const double bytes = 4.0 * p.places;
-  if (p.places <= PLAN_ONE_BLOCK) {
+  const PlanForm form = plan_form(p.places, p.n_experts);
+  if (form == PLAN_BLOCK) {
     IT_LAUNCH(IT_K_EXPERT_PLAN, 3 * bytes, 0, st, IT_CUDA_TRY(it_launch_pdl(plan_one_kernel, dim3(1), dim3(PLAN_THREADS), smem, st, p)));
+    return IT_OK;
+  }
+  if (form == PLAN_CLUSTERED) {
+    p.per_block = (p.places + PLAN_CLUSTER - 1) / PLAN_CLUSTER;
+    cudaLaunchAttribute attr[2] = {};
+    attr[0].id = cudaLaunchAttributeProgrammaticStreamSerialization;
+    attr[0].val.programmaticStreamSerializationAllowed = 1;
+    attr[1].id = cudaLaunchAttributeClusterDimension;
+    attr[1].val.clusterDim.x = PLAN_CLUSTER; attr[1].val.clusterDim.y = 1; attr[1].val.clusterDim.z = 1;
+    cudaLaunchConfig_t cfg{};
+    cfg.gridDim = dim3(PLAN_CLUSTER); cfg.blockDim = dim3(PLAN_THREADS); cfg.dynamicSmemBytes = 2 * smem; cfg.stream = st; cfg.attrs = attr; cfg.numAttrs = 2;
+    IT_LAUNCH(IT_K_EXPERT_PLAN, 3 * bytes, 0, st, IT_CUDA_TRY((cudaLaunchKernelEx(&cfg, plan_cluster_kernel, p))));
     return IT_OK;
   }
   p.blocks = plan_blocks(p.places);

@@ -236,3 +236,12 @@ def test_two_places_a_vertex(kind, a, h, o, gated, n, E, masked, repeat):
     ws = torch.full((B.it_experts_workspace_bytes(d, n),), 0xff, dtype=torch.uint8, device="cuda")
     for _ in range(4):
         assert torch.equal(run_experts(c, desc=d, workspace=ws), want)
+
+
+@pytest.mark.parametrize("n,E,k", [(1200, 8, 2), (3100, 32, 2), (3100, 33, 2), (700, 300, 3), (25_003, 20, 2), (25_800, 20, 2), (40_500, 256, 2), (41_100, 700, 2), (9000, 1024, 1),
+                                   (16_384, 1025, 1), (16_385, 1025, 1), (3000, 4096, 2), (20_000, 1, 1)])
+def test_sorting_of_places(n, E, k):
+    """Sizes on either side of those where the places are sorted otherwise; experts without a place, one of most of them, masked places."""
+    c = experts_case(n + E, n, E, k, 16, 0, 16, BF16, masked=0.2, repeat=True, skew=0.6 if n % 2 else None)
+    c["ids"][c["ids"] % 5 == 3] = E - 1
+    check_experts(c, run_experts(c), device="cuda")
