@@ -156,6 +156,7 @@ expert_fused_kernel(const __grid_constant__ CUtensorMap map_w1, const __grid_con
           // the chunk before the last one's P lies where this S goes (waited for last: the weights are long there, and a wait takes its time)
           if (ok && kb0 == 0 && g >= 2) ok = ex_wait_warp(&s_free[g & 1u], ((g >> 1) & 1u) ^ 1u, abort_flag, p.spin_limit);
           if (!ok) break;
+          tc_fence_after();   // other warps wrote that P and read it in an MMA: what is issued here stays behind them
           const uint64_t b_d = make_desc_mn(smem_u32(w1_s) + stage * (uint32_t)p.stage1, BK1 * TC_KBLOCK_BYTES);
           for (int i = 0; i < p.kb1 && kb0 + i < p.kbx; ++i) {
 #pragma unroll

@@ -245,3 +245,16 @@ def test_sorting_of_places(n, E, k):
     c = experts_case(n + E, n, E, k, 16, 0, 16, BF16, masked=0.2, repeat=True, skew=0.6 if n % 2 else None)
     c["ids"][c["ids"] % 5 == 3] = E - 1
     check_experts(c, run_experts(c), device="cuda")
+
+
+@pytest.mark.parametrize("kind,gated", [("bf16", False), ("bf16", True), ("eight", False)])
+@pytest.mark.parametrize("a,h,o", [(64, 2048, 64), (256, 1536, 256), (16, 1024, 8)])
+def test_many_chunks_take_turns_in_two_buffers(kind, gated, a, h, o):
+    """A chunk of the hidden row is written where the one before the last was read: long hidden rows, short products between them, the same result every time."""
+    c = experts_case(a + h + o, 20_000, 4, 1, a, h, o, BF16, eight=kind == "eight", gated=gated, act="relu")
+    d = experts_desc(c)
+    ws = torch.full((B.it_experts_workspace_bytes(d, c["n"]),), 0xff, dtype=torch.uint8, device="cuda")
+    want = run_experts(c, desc=d, workspace=ws)
+    check_experts(c, want, device="cuda")
+    for _ in range(4):
+        assert torch.equal(run_experts(c, desc=d, workspace=ws), want)
