@@ -2,8 +2,9 @@
 //
 // The choice has to be that of exact arithmetic, which 32 bits cannot promise next to a border.  Without a bias the order of the scores
 // is the order of the logits, and nothing is rounded.  With one (or where a group is worth a sum) the fast kernel works in fp32 and
-// looks at the gap between every two neighbours of the choice: where it is within the rounding of the two (route_near), the whole warp
-// takes the row again in 64 bits.
+// looks at the gap between every two neighbours of the choice, and between its last key and the best one left out: where it is within the
+// rounding of the two (route_near), the whole warp takes the row again in 64 bits.  Behind the best one left out may be keys that are less
+// exact than it (a large score with a large negative bias), so that gap is held against the largest rounding that a key of the row can have.
 //
 // A row lies in the registers of 1 to 32 lanes (8 experts a lane, 16 and 32 beyond 256 experts), or of one thread where experts and
 // places are few.  Bound by issue slots: the row's bytes are few.
@@ -123,14 +124,16 @@ __device__ void route_row_exact(const RouteParams &p, const void *logits, bool b
 }
 
 // ----------------------------------------------------------------------------- the fast kernel
-// Whether fp32 leaves open which of two keys (or sums of keys) a >= b is larger.  pa, pb: the scores in them, each off by at most 2e-6 of itself
-// (the hardware exponential 2^-22, a reciprocal 2^-23, the sum of a row up to 21 additions, two products); adding a bias rounds once more, by
-// half an ulp of the key.  The exponent is rounded too, twice, by |exponent| * 2^-24: pa and pb come with that share (route_slack), which
-// below 1e-30 would no longer be represented.
-__device__ __forceinline__ bool route_near(float a, float b, float pa, float pb) {
-  return a - b <= 2e-6f * (pa + pb) + 2.5e-7f * (fabsf(a) + fabsf(b)) + 1e-30f;
+// Whether fp32 leaves open which of two keys (or sums of keys) a >= b is larger.  pa, pb: the scores in them, as far as their rounding goes
+// (route_slack); adding a bias rounds once more, by half an ulp of the key.  A score is off by at most `rel` of itself.  A sigmoid, 1e-6: the hardware
+// exponential 2^-22, a sum 2^-24, a reciprocal 2^-23.  A softmax, 4e-6: the exponential 2^-22, that of the row's sum 2^-22, the exponents in that sum
+// ln(1024) times 2.3 * 2^-24, its up to 36 additions and the division 2^-24 each.  The exponent is rounded too (the difference, the factor log2(e), the
+// product: 2.3 * 2^-24 of it): that share, 0.15 rel, is in pa and pb, which below 1e-30 would no longer be represented.
+__device__ __forceinline__ bool route_near(float a, float b, float pa, float pb, float rel) {
+  return a - b <= rel * (pa + pb) + 2.5e-7f * (fabsf(a) + fabsf(b)) + 1e-30f;
 }
-__device__ __forceinline__ float route_slack(float score, float below_top) { return score * fmaf(fabsf(below_top), 0.0625f, 1.f); }
+// (p (1 + 0.15 |x|) of a score p = e^-|x| is largest at x = 0: no score of a row has more slack than 1, or than the softmax's largest score)
+__device__ __forceinline__ float route_slack(float score, float below_top) { return score * fmaf(fminf(fabsf(below_top), 1e30f), 0.15f, 1.f); }
 
 __device__ __forceinline__ float route_rcp(float x) {   // of 1 to infinity
   float r;
@@ -225,9 +228,10 @@ __global__ void __launch_bounds__(ROUTE_THREADS, C == 8 ? 8 : 1) route_kernel(co
         for (int c = 0; c < C; ++c) key[c] = key[c] > kClosed ? fmaf(s[c], inv, bias[c]) : kClosed;
       }
     }
+    const float rel = p.sigmoid ? 1e-6f : 4e-6f;
     const bool exact_worth = !p.bias && p.group_best == 1;
     // a worth with a bias: two scores of at most inv each, whose slack (x e^-x / 16) is below 3 %; without: sums of e^-x with x < 104
-    auto worth_near = [&](float v, float w) { return route_near(v, w, p.bias ? 2.2f * inv : 8.f * v, p.bias ? 2.2f * inv : 8.f * w); };
+    auto worth_near = [&](float v, float w) { return route_near(v, w, p.bias ? 2.2f * inv : 8.f * v, p.bias ? 2.2f * inv : 8.f * w, 2e-6f); };
     auto worth_of = [&](float a, float b) {   // a group's two largest keys
       if (p.group_best == 1 || !(a > kClosed)) return a;
       const float second = b > kClosed ? (p.bias ? b : raw(b, top)) : 0.f;
@@ -422,6 +426,7 @@ __global__ void __launch_bounds__(ROUTE_THREADS, C == 8 ? 8 : 1) route_kernel(co
     unsigned again = 0;   // rows that are taken again, a bit each
     for (int i0 = 0; i0 < R * rounds; i0 += 32) {
       const int i = i0 + lane, rr = R == 1 ? 0 : (i < R * rounds ? i / rounds : 0), j = i - rr * rounds;
+      const float most = __shfl_sync(full, inv, rr * L);   // the largest score that there can be (a sigmoid: 1)
       bool close = false;
       if (i < R * rounds) {
         float sum = 0.f;
@@ -431,7 +436,8 @@ __global__ void __launch_bounds__(ROUTE_THREADS, C == 8 ? 8 : 1) route_kernel(co
         if (p.bias && j > 0 && at_s[i] >= 0) {
           // (-ln of a score is at least its exponent: a softmax divides by 1 or more, a sigmoid by 1 + e^-x)
           const float before = score_s[i - 1];
-          close = route_near(key_s[i - 1], key_i, route_slack(before, __logf(fmaxf(before, 1e-38f))), route_slack(w, __logf(fmaxf(w, 1e-38f))));
+          close = route_near(key_s[i - 1], key_i, route_slack(before, __logf(fmaxf(before, 1e-38f))),
+                             j == p.k ? most : route_slack(w, __logf(fmaxf(w, 1e-38f))), rel);
         }
         if (j < p.k && row0 + rr < p.n) {
           const int64_t to = (row0 + rr) * p.k + j;
@@ -527,7 +533,7 @@ __global__ void __launch_bounds__(ROUTE_THREADS) route_thread_kernel(const Route
       if (j < p.k) sum += w[j];
       if (p.bias && j > 0 && j <= p.k && at[j] >= 0) {
         const float l = open_logit(to_f32(from[at[j - 1]]));
-        near |= route_near(best[j - 1], best[j], route_slack(w[j - 1], p.sigmoid ? fminf(l, 0.f) : l - top), slack);
+        near |= route_near(best[j - 1], best[j], route_slack(w[j - 1], p.sigmoid ? fminf(l, 0.f) : l - top), j == p.k ? inv : slack, p.sigmoid ? 1e-6f : 4e-6f);
       }
     }
     const float f = p.renorm ? (sum > 0.f ? p.scale / sum : 0.f) : p.scale;

@@ -165,3 +165,22 @@ def test_offsets_past_32_bits():
     rid, rw = route_reference(d, l[-60:].float().cpu().numpy(), None)
     assert np.array_equal(ids[-60:].cpu().numpy(), rid) and np.allclose(w[-60:].cpu().numpy(), rw, rtol=RTOL)
     assert (ids[:1000] == 0).all()
+
+
+@pytest.mark.parametrize("score", ["softmax", "sigmoid"])
+@pytest.mark.parametrize("e", [4, 20, 32, 60, 64, 256, 700])
+def test_a_key_behind_the_border_may_be_the_least_exact(score, e):
+    """Two keys of tiny scores at the border of the choice, and behind them one of a score near 1 and a bias near -1, which 32 bits know far less
+    exactly: its exact key passes the others' in some rows and not in others."""
+    a, b, c, d, n = 3, 1, 0, 2, 201
+    l = np.full((n, e), -60.0, np.float32)
+    l[:, [a, b]], l[:, d] = -40.0, 0.0
+    l[:, c] = np.float32(5.2739234) + np.float32(4.7683716e-7) * (np.arange(n, dtype=np.float32) - n // 2)
+    for q in range(12):
+        bias = np.full(e, -8.0, np.float32)
+        bias[a] = np.float32(0.01) + np.float32(q * 1.1e-8)
+        bias[b] = bias[a] - np.float32(7.45e-9)
+        bias[c] = np.float32(0.01) - np.float32(1 / (1 + np.exp(-np.float64(l[n // 2, c]))))   # (a softmax over c, d and next to nothing is that sigmoid)
+        bias = torch.from_numpy(bias)
+        for k in (1, 2):
+            _check(B.RouteDesc(n_experts=e, top_k=k, logit_dtype=F32, score=score, balance_bias=bias.cuda(), renormalise=False), torch.from_numpy(l).cuda(), bias)
