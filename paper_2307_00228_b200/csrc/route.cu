@@ -159,16 +159,16 @@ __global__ void __launch_bounds__(ROUTE_THREADS, C == 8 ? 8 : 1) route_kernel(co
   constexpr unsigned full = 0xffffffffu;
   extern __shared__ double route_smem[];
   const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31, gl = lane % L, r = lane / L;
-  // per warp: expert, key and score of its rows' choices [R][rounds] each, the fp32 keys and worths of its rows (groups); the 64-bit ones of one row
+  // per warp: expert, key and score of its rows' choices [R][rounds] each, the fp32 keys, worths and their slacks of its rows (groups); the 64-bit ones of one row
   const int E = p.experts, per_warp = E + p.n_groups, rounds = p.k + (p.bias && p.k < E ? 1 : 0);
   double *mine64 = route_smem + (size_t)warp * per_warp;
-  const int row_words = E + E / 32 + 1 + p.n_groups;   // a pad word after every 32 keys
+  const int row_words = E + E / 32 + 1 + 2 * p.n_groups;   // a pad word after every 32 keys
   float *after = reinterpret_cast<float *>(route_smem + (size_t)ROUTE_WARPS * per_warp);
   const int warp_words = R * 3 * rounds + (L == 32 ? 64 : 0) + (p.n_groups > 1 ? R * row_words : 0);
   int32_t *at_s = reinterpret_cast<int32_t *>(after + (size_t)warp * warp_words);
   unsigned *order_s = reinterpret_cast<unsigned *>(at_s + R * rounds + 32);   // (one row a warp: 32 candidates, their experts behind the choices)
   float *key_s = reinterpret_cast<float *>(at_s + R * rounds + (L == 32 ? 64 : 0)), *score_s = key_s + R * rounds;
-  float *keys = score_s + R * rounds + (size_t)r * row_words, *worth = keys + E + E / 32 + 1;
+  float *keys = score_s + R * rounds + (size_t)r * row_words, *worth = keys + E + E / 32 + 1, *slack = worth + p.n_groups;
   auto expert = [&](int c) { return ((c / N) * L + gl) * N + c % N; };
   const bool vec = (E * (int)sizeof(T)) % 16 == 0 && N == kVec<T> && ((uintptr_t)p.logits & 15) == 0;
   float bias[C];
@@ -230,8 +230,13 @@ __global__ void __launch_bounds__(ROUTE_THREADS, C == 8 ? 8 : 1) route_kernel(co
     }
     const float rel = p.sigmoid ? 1e-6f : 4e-6f;
     const bool exact_worth = !p.bias && p.group_best == 1;
-    // a worth with a bias: two scores of at most inv each, whose slack (x e^-x / 16) is below 3 %; without: sums of e^-x with x < 104
-    auto worth_near = [&](float v, float w) { return route_near(v, w, p.bias ? 2.2f * inv : 8.f * v, p.bias ? 2.2f * inv : 8.f * w, 2e-6f); };
+    // What a group's worth may be off by, from its two largest keys.  With a bias: two scores of at most inv each, whose slack is at most that, and two keys and
+    // their sum rounded by half an ulp each (large biases of opposite sign leave a small sum).  Without: a sum of e^-x, x < 104, each off by 2^-22 and x 2^-24.
+    // (the borders worth - slack and worth + slack are rounded too: 2.5e-7 is four halves of an ulp)
+    auto worth_slack = [&](float a, float b, float w) {
+      if (!p.bias) return 1.6e-5f * w + 1e-30f;
+      return 2.2f * rel * inv + 2.5e-7f * (fabsf(a) + (p.group_best == 2 && b > kClosed ? fabsf(b) : 0.f)) + 1e-30f;
+    };
     auto worth_of = [&](float a, float b) {   // a group's two largest keys
       if (p.group_best == 1 || !(a > kClosed)) return a;
       const float second = b > kClosed ? (p.bias ? b : raw(b, top)) : 0.f;
@@ -240,7 +245,8 @@ __global__ void __launch_bounds__(ROUTE_THREADS, C == 8 ? 8 : 1) route_kernel(co
     if (p.n_groups > 1 && segments) {
       // groups are runs of lanes in every chunk of N consecutive experts a lane: nothing leaves the registers
       constexpr int CH = C / N;
-      float w[CH], keep = INFINITY, drop = kClosed;   // worth of this lane's group in every chunk; the least that is kept, the most that is not
+      // worth of this lane's group in every chunk, and what it may be off by; the least that a kept one may be worth, the most that one may that is not
+      float w[CH], off[CH], keep = INFINITY, drop = kClosed;
       int rank[CH];
 #pragma unroll
       for (int j = 0; j < CH; ++j) {
@@ -256,6 +262,7 @@ __global__ void __launch_bounds__(ROUTE_THREADS, C == 8 ? 8 : 1) route_kernel(co
           a = fmaxf(a, a2);
         }
         w[j] = worth_of(a, b);
+        off[j] = worth_slack(a, b, w[j]);
         rank[j] = 0;
       }
       const int per_chunk = L / segment, mine = gl / segment;
@@ -270,15 +277,15 @@ __global__ void __launch_bounds__(ROUTE_THREADS, C == 8 ? 8 : 1) route_kernel(co
 #pragma unroll
       for (int j = 0; j < CH; ++j) {
         if (!(w[j] > kClosed)) continue;   // (no open expert, or no group at all)
-        if (rank[j] < p.group_k) keep = fminf(keep, w[j]);
-        else drop = fmaxf(drop, w[j]);
+        if (rank[j] < p.group_k) keep = fminf(keep, w[j] - off[j]);
+        else drop = fmaxf(drop, w[j] + off[j]);
       }
 #pragma unroll
       for (int o = L / 2; o > 0; o >>= 1) {
         keep = fminf(keep, __shfl_xor_sync(full, keep, o));
         drop = fmaxf(drop, __shfl_xor_sync(full, drop, o));
       }
-      if (!exact_worth && drop > kClosed) near |= worth_near(keep, drop);
+      near = !exact_worth && drop >= keep;
 #pragma unroll
       for (int j = 0; j < CH; ++j)
 #pragma unroll
@@ -309,21 +316,34 @@ __global__ void __launch_bounds__(ROUTE_THREADS, C == 8 ? 8 : 1) route_kernel(co
           b = fmaxf(fmaxf(b, b2), fminf(a, a2));
           a = fmaxf(a, a2);
         }
-        if (g < p.n_groups && gl % per_group == 0) worth[g] = worth_of(a, b);
+        if (g < p.n_groups && gl % per_group == 0) {
+          const float w = worth_of(a, b);
+          worth[g] = w;
+          slack[g] = worth_slack(a, b, w);
+        }
       }
       __syncwarp();
       // one flag per group, in place of the keys
+      float keep = INFINITY, drop = kClosed;
       for (int g = gl; g < p.n_groups; g += L) {
         const float w = worth[g];
         int rank = 0;
         for (int o = 0; o < p.n_groups; ++o) {
           const float v = worth[o];
           rank += v > w || (v == w && o < g);
-          if (!exact_worth && o != g && v > kClosed && w > kClosed) near |= v >= w && worth_near(v, w);
         }
         keys[g] = rank < p.group_k ? 1.f : 0.f;
+        if (!(w > kClosed)) continue;
+        if (rank < p.group_k) keep = fminf(keep, w - slack[g]);
+        else drop = fmaxf(drop, w + slack[g]);
       }
       __syncwarp();
+#pragma unroll
+      for (int o = L / 2; o > 0; o >>= 1) {
+        keep = fminf(keep, __shfl_xor_sync(full, keep, o));
+        drop = fmaxf(drop, __shfl_xor_sync(full, drop, o));
+      }
+      near = !exact_worth && drop >= keep;
 #pragma unroll
       for (int c = 0; c < C; ++c) {
         const int e = expert(c);
@@ -571,7 +591,7 @@ template <typename T, int L, int C>
 it_status launch(const RouteParams &p, double bytes, double flops, cudaStream_t st) {
   constexpr int R = 32 / L;
   const size_t warp64 = (size_t)(p.experts + p.n_groups) * 8;
-  const size_t warp32 = ((size_t)R * 3 * (p.k + 1) + (L == 32 ? 64 : 0) + (p.n_groups > 1 ? (size_t)R * (p.experts + p.experts / 32 + 1 + p.n_groups) : 0)) * 4;
+  const size_t warp32 = ((size_t)R * 3 * (p.k + 1) + (L == 32 ? 64 : 0) + (p.n_groups > 1 ? (size_t)R * (p.experts + p.experts / 32 + 1 + 2 * p.n_groups) : 0)) * 4;
   return launch_route(route_kernel<T, L, C>, p, ROUTE_WARPS * R, ROUTE_WARPS * (warp64 + warp32), bytes, flops, st);
 }
 

@@ -184,3 +184,24 @@ def test_a_key_behind_the_border_may_be_the_least_exact(score, e):
         bias = torch.from_numpy(bias)
         for k in (1, 2):
             _check(B.RouteDesc(n_experts=e, top_k=k, logit_dtype=F32, score=score, balance_bias=bias.cuda(), renormalise=False), torch.from_numpy(l).cuda(), bias)
+
+
+@pytest.mark.parametrize("score", ["softmax", "sigmoid"])
+@pytest.mark.parametrize("e,size", [(16, 4), (40, 4), (64, 8), (60, 5), (256, 32), (96, 3), (1024, 64)])
+def test_groups_whose_best_two_nearly_cancel(score, e, size):
+    """The worth of a group is a sum of two keys; large biases of opposite sign leave a small one, which 32 bits know by the size of the keys alone."""
+    g, n = e // size, 64
+    rng = np.random.default_rng(e)
+    for magnitude in (3.0, 40.0, 1000.0):
+        bias = np.full(e, -1e6, np.float32).reshape(g, size)
+        for i in range(g):
+            big = np.float32(magnitude * (1 + 0.1 * rng.random()))
+            two = rng.choice(size, 2, replace=False)
+            bias[i, two[0]], bias[i, two[1]] = big, -big
+        bias = bias.reshape(e)
+        step = np.spacing(np.float32(magnitude))   # scores differ by a few steps of the keys
+        l = (10 * step * (e if score == "softmax" else 1) * rng.normal(size=(n, e))).astype(np.float32)
+        bias = torch.from_numpy(bias)
+        for group_k in (1, g - 1):
+            d = B.RouteDesc(n_experts=e, top_k=2, logit_dtype=F32, score=score, balance_bias=bias.cuda(), n_groups=g, group_k=group_k, group_best=2, renormalise=False)
+            _check(d, torch.from_numpy(l).cuda(), bias)
