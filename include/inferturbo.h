@@ -332,7 +332,8 @@ it_status it_residual_norm(const it_norm_desc *d, int64_t n, const void *x, cons
  *            (and groups) go to the lowest index.
  *   ids      [n, top_k] int32; -1 where no open expert is left (weight 0).
  *   weights  [n, top_k] fp32: the scores of the chosen (without the bias), with renormalise divided by their sum (0 where that is 0),
- *            times weight_scale.
+ *            times weight_scale.  The sum is that of 64 bits: scores too small for fp32 still share it out, and one is 0 only beyond a double's range (a
+ *            sigmoid of less than -709.78, a softmax of 745.13 below the row's largest logit).  Without renormalise a score below 2^-126 may be given as 0.
  *   n_experts <= 1024, top_k <= min(n_experts, 32); n_groups divides n_experts; ids and weights overlap neither each other nor logits.
  */
 typedef enum { IT_SCORE_SOFTMAX = 0, IT_SCORE_SIGMOID = 1 } it_score;

@@ -37,6 +37,21 @@ __device__ __forceinline__ float open_logit(float l) { return l != l ? kClosed :
 __device__ __forceinline__ float open_key(float k) { return k != k ? kClosed : k; }
 __device__ __forceinline__ double open_key(double k) { return k != k ? (double)kClosed : k; }
 
+// Scores end at what 64 bits hold: a softmax's at a logit 745.13 below the row's largest, a sigmoid's at -709.78, where e^-l has no double.
+__device__ __forceinline__ bool route_scored(bool sigmoid, float l, float top) { return sigmoid ? l > -709.7827f : l - top >= -745.13f; }
+// The score of a chosen logit next to those chosen with it, of which `most` is the largest: divided by e^most (softmax) or by e^min(most, 0) (sigmoid), so that
+// the scores of a row's chosen add up to between 1/2 and their number however small they are.
+__device__ __forceinline__ double route_share(bool sigmoid, float l, float top, float most) {
+  if (!(l > kClosed) || !route_scored(sigmoid, l, top)) return 0.0;
+  if (!sigmoid) return exp((double)l - (double)most);
+  return l < 0.f ? exp((double)l - (double)fminf(most, 0.f)) / (1.0 + exp((double)l)) : 1.0 / (1.0 + exp(-(double)l));
+}
+// Whether a chosen score is too small for 32 bits to be divided by the sum of the chosen: the row is then taken again in 64.  (Where the sum is
+// 1 or more, so is what becomes of it.)
+__device__ __forceinline__ bool route_tiny(bool sigmoid, float score, float sum, float l, float top) {
+  return score < 1.2e-37f && sum < 1.f && route_scored(sigmoid, l, top);
+}
+
 // ----------------------------------------------------------------------------- 64 bits, a warp per row
 // key: [experts] doubles of shared memory, then [n_groups] of the groups' worths.
 __device__ void route_row_exact(const RouteParams &p, const void *logits, bool bf16, int64_t row, double *key, int lane) {
@@ -96,7 +111,7 @@ __device__ void route_row_exact(const RouteParams &p, const void *logits, bool b
     __syncwarp();
   }
   int my_id = -1;
-  double my_w = 0.0;
+  float my_l = kClosed;
   for (int j = 0; j < p.k; ++j) {
     double best = (double)kClosed;
     int at = ROUTE_MAX_EXPERTS;
@@ -109,14 +124,23 @@ __device__ void route_row_exact(const RouteParams &p, const void *logits, bool b
       if (b > best || (b == best && a < at)) { best = b; at = a; }
     }
     if (at == ROUTE_MAX_EXPERTS) break;   // (the same for all lanes)
-    if (lane == j) { my_id = at; my_w = score(logit(at)); }
+    if (lane == j) { my_id = at; my_l = logit(at); }
     if (lane == 0) key[at] = (double)kClosed;
     __syncwarp();
   }
-  double sum = my_w;
+  double my_w;
+  if (p.renorm) {
+    float most = my_l;
 #pragma unroll
-  for (int o = 16; o > 0; o >>= 1) sum += __shfl_xor_sync(full, sum, o);
-  if (p.renorm) my_w = sum > 0.0 ? my_w / sum : 0.0;
+    for (int o = 16; o > 0; o >>= 1) most = fmaxf(most, __shfl_xor_sync(full, most, o));
+    my_w = route_share(p.sigmoid, my_l, top, most);
+    double sum = my_w;
+#pragma unroll
+    for (int o = 16; o > 0; o >>= 1) sum += __shfl_xor_sync(full, sum, o);
+    my_w = sum > 0.0 ? my_w / sum : 0.0;
+  } else {
+    my_w = score(my_l);
+  }
   if (lane < p.k) {
     p.ids[row * p.k + lane] = my_id;
     p.weights[row * p.k + lane] = (float)(my_w * (double)p.scale);
@@ -444,9 +468,10 @@ __global__ void __launch_bounds__(ROUTE_THREADS, C == 8 ? 8 : 1) route_kernel(co
     }
     __syncwarp();
     unsigned again = 0;   // rows that are taken again, a bit each
+    const bool may_again = p.bias || p.sigmoid || p.n_groups > 1;   // (a softmax's largest score is else among the chosen)
     for (int i0 = 0; i0 < R * rounds; i0 += 32) {
       const int i = i0 + lane, rr = R == 1 ? 0 : (i < R * rounds ? i / rounds : 0), j = i - rr * rounds;
-      const float most = __shfl_sync(full, inv, rr * L);   // the largest score that there can be (a sigmoid: 1)
+      const float t = __shfl_sync(full, top, rr * L), most = __shfl_sync(full, inv, rr * L);   // most: the largest score that there can be (a sigmoid: 1)
       bool close = false;
       if (i < R * rounds) {
         float sum = 0.f;
@@ -461,11 +486,14 @@ __global__ void __launch_bounds__(ROUTE_THREADS, C == 8 ? 8 : 1) route_kernel(co
         }
         if (j < p.k && row0 + rr < p.n) {
           const int64_t to = (row0 + rr) * p.k + j;
-          p.ids[to] = at_s[i];
-          p.weights[to] = w * (p.renorm ? (sum > 0.f ? p.scale / sum : 0.f) : p.scale);
+          const int e = at_s[i];
+          p.ids[to] = e;
+          p.weights[to] = (p.renorm ? (sum > 0.f ? w / sum : 0.f) : w) * p.scale;
+          if (p.renorm && e >= 0 && w < 1.2e-37f)
+            close |= route_tiny(p.sigmoid, w, sum, open_logit(to_f32(reinterpret_cast<const T *>(p.logits)[(row0 + rr) * E + e])), t);
         }
       }
-      if (p.bias) again |= __reduce_or_sync(full, close ? 1u << rr : 0u);
+      if (may_again) again |= __reduce_or_sync(full, close ? 1u << rr : 0u);
     }
     if (p.n_groups > 1) again |= __reduce_or_sync(full, near ? 1u << r : 0u);
     while (again) {
@@ -556,20 +584,26 @@ __global__ void __launch_bounds__(ROUTE_THREADS) route_thread_kernel(const Route
         near |= route_near(best[j - 1], best[j], route_slack(w[j - 1], p.sigmoid ? fminf(l, 0.f) : l - top), j == p.k ? inv : slack, p.sigmoid ? 1e-6f : 4e-6f);
       }
     }
-    const float f = p.renorm ? (sum > 0.f ? p.scale / sum : 0.f) : p.scale;
+    if (p.renorm && (p.bias || p.sigmoid)) {   // (a softmax's largest score is else among the chosen)
+#pragma unroll
+      for (int j = 0; j < KL; ++j)
+        if (j < p.k && at[j] >= 0 && w[j] < 1.2e-37f) near |= route_tiny(p.sigmoid, w[j], sum, open_logit(to_f32(from[at[j]])), top);
+    }
+#pragma unroll
+    for (int j = 0; j < KL; ++j) w[j] = (p.renorm ? (sum > 0.f ? w[j] / sum : 0.f) : w[j]) * p.scale;
     if (real) {
       int32_t *ids = p.ids + row * p.k;
       float *ws = p.weights + row * p.k;
       if (p.k == 2 && (((uintptr_t)p.ids | (uintptr_t)p.weights) & 7) == 0) {
         *reinterpret_cast<int2 *>(ids) = make_int2(at[0], at[1]);
-        *reinterpret_cast<float2 *>(ws) = make_float2(w[0] * f, w[1] * f);
+        *reinterpret_cast<float2 *>(ws) = make_float2(w[0], w[1]);
       } else {
 #pragma unroll
         for (int j = 0; j < KL; ++j)
-          if (j < p.k) { ids[j] = at[j]; ws[j] = w[j] * f; }
+          if (j < p.k) { ids[j] = at[j]; ws[j] = w[j]; }
       }
     }
-    unsigned again = p.bias ? __ballot_sync(full, near && real) : 0u;
+    unsigned again = p.bias || p.sigmoid ? __ballot_sync(full, near && real) : 0u;
     while (again) {
       const int which = __ffs(again) - 1;
       again &= again - 1;

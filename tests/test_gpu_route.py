@@ -205,3 +205,39 @@ def test_groups_whose_best_two_nearly_cancel(score, e, size):
         for group_k in (1, g - 1):
             d = B.RouteDesc(n_experts=e, top_k=2, logit_dtype=F32, score=score, balance_bias=bias.cuda(), n_groups=g, group_k=group_k, group_best=2, renormalise=False)
             _check(d, torch.from_numpy(l).cuda(), bias)
+
+
+@pytest.mark.parametrize("scale", [1.0, 2.5])
+@pytest.mark.parametrize("e,k,groups", [(2, 1, 1), (8, 2, 1), (16, 4, 1), (30, 3, 1), (32, 8, 1), (60, 4, 1), (64, 6, 8), (60, 6, 5), (256, 8, 1), (256, 8, 8), (700, 20, 1)])
+@pytest.mark.parametrize("score,biased", [("sigmoid", False), ("sigmoid", True), ("softmax", True)])
+def test_weights_of_scores_that_32_bits_do_not_hold(score, biased, e, k, groups, scale):
+    """The chosen share a weight of 1 between them however small their scores are, also where e^-90 and e^-700 are 0 in 32 bits."""
+    g = torch.Generator().manual_seed(e + k)
+    depth = torch.tensor([0.0, 20, 60, 80, 85, 86, 87, 87.5, 88, 88.3, 88.5, 88.7, 89, 90, 95, 100, 103, 104, 110, 130, 200, 400, 600, 680])
+    n = depth.numel()
+    l = 12 * torch.rand(n, e, generator=g) - depth[:, None]
+    bias = None
+    if score == "softmax":   # one expert far above, which the bias keeps out: the chosen lie `depth` below it
+        l[:, e // 2] = 12.0
+    if biased:
+        bias = 3 * torch.rand(e, generator=g)
+        bias[e // 2] = -9.0
+    groups = groups if e > 2 else 1
+    d = B.RouteDesc(n_experts=e, top_k=k, logit_dtype=F32, score=score, balance_bias=None if bias is None else bias.cuda(), n_groups=groups, group_k=max(1, groups // 2),
+                    group_best=2, weight_scale=scale)
+    _check(d, l.cuda(), bias)
+    _, w = _run(d, l.cuda())
+    assert np.allclose(w.sum(1), scale, rtol=1e-5)
+
+
+def test_scores_that_64_bits_do_not_hold_are_0():
+    """As in 64 bits, where 1 / (1 + e^-l) ends at a logit of -709.78 and e^-x at x = 745: weight 0, whatever the others are."""
+    l = torch.tensor([[-709.9, -720.0, -800.0], [-1e4, -3e38, -720.0], [-600.0, -601.0, -700.0]])
+    ids, w = _run(B.RouteDesc(n_experts=3, top_k=2, logit_dtype=F32, score="sigmoid"), l.cuda())
+    assert (ids == [[0, 1], [2, 0], [0, 1]]).all()
+    assert (w[:2] == 0).all() and np.allclose(w[2], [1 / (1 + np.exp(-1)), 1 / (1 + np.exp(1))], rtol=RTOL)
+    bias = torch.tensor([-9.0, 0.25, 0.0])
+    l = torch.tensor([[0.0, -746.0, -747.0], [0.0, -700.0, -701.0], [30.0, -800.0, 0.0]])
+    ids, w = _run(B.RouteDesc(n_experts=3, top_k=2, logit_dtype=F32, balance_bias=bias.cuda()), l.cuda())
+    assert (ids == [1, 2]).all()
+    assert (w[0] == 0).all() and np.allclose(w[1], [1 / (1 + np.exp(-1)), 1 / (1 + np.exp(1))], rtol=RTOL) and (w[2] == [0, 1]).all()
