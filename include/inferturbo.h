@@ -365,7 +365,8 @@ it_status it_route(const it_route_desc *d, int64_t n, const void *logits, int32_
  *   NaN); the hidden row between the two products is rounded to feat_dtype, the places of a vertex are added in fp32, in their order, and
  *   rounded once.  Few places take products of their own, in fp32 throughout.  Which form a call takes depends on its sizes alone: the same call gives the
  *   same bits, but the last ones of a vertex may differ with the number of vertices beside it.
- *   workspace: device, 256-byte aligned, >= it_experts_workspace_bytes; calls that can overlap on the GPU need one each.
+ *   workspace: device, 256-byte aligned, >= it_experts_workspace_bytes (which never falls as n grows: what serves n serves fewer); calls that can overlap on
+ *   the GPU need one each.
  *   x, ids, weights and the expert arrays may not overlap out or the workspace.
  * it_experts_check - waits for `stream` and reports whether the last it_experts_forward with this workspace gave up one of its bounded
  *   device-side waits: IT_ERR_TIMEOUT (out is then not valid), else IT_OK.

@@ -293,11 +293,12 @@ it_status check(const it_experts_desc *d, int64_t n) {
 // 64 places 8.3 / 10.2, 128 10.8 / 10.7; 256-256 64 6.9 / 9.5, 128 10.6 / 9.7; 128-512-128 (64 experts) 64 11.3 / 14.2, 128 19.6 / 14.4; 256-1024-256
 // 64 22.4 / 24.1, 128 31.9 / 24.2; gated 768-1024-768 16 26.7 / 30.3, 32 40.6 / 33.0.  fp32, whose sorted form splits all weights first:
 // 64-256-64 256 21.9 / 30.9, 512 32.0 / 32.3; 256-1024-256 128 44.9 / 80.9, 256 78.6 / 82.2.
-bool few_form(const it_experts_desc &d, int64_t places) {
+int64_t most_few(const it_experts_desc &d) {
   const bool f32 = d.feat_dtype == IT_F32;
   const int64_t first = d.hidden_dim > 0 ? (int64_t)d.hidden_dim * (d.gated ? 2 : 1) : d.out_dim;
   const int64_t bytes = (int64_t)d.in_dim * first * (f32 ? 4 : (d.in_dtype == IT_E4M3 ? 1 : 2)) + (int64_t)d.hidden_dim * d.out_dim * (f32 ? 4 : 2);
-  return places <= (f32 ? 448 : 96) && places * bytes <= (f32 ? (int64_t)512 << 20 : (int64_t)80 << 20);
+  const int64_t by_bytes = (f32 ? (int64_t)512 << 20 : (int64_t)80 << 20) / bytes, most = f32 ? 448 : 96;
+  return by_bytes < most ? by_bytes : most;
 }
 
 // Products that are not fused and take their rows more than once, for several tiles of columns, have them put in order first: fetched by place, a
@@ -324,10 +325,13 @@ it_status plan(const it_experts_desc *d, int64_t n, ExpertsWs *w) {
   const size_t cols = (size_t)(d->hidden_dim > 0 ? d->hidden_dim : d->out_dim);
   size_t off = kStatusBytes;
   auto take = [&](size_t bytes) { const size_t o = off; off += it_align_up(bytes); return o; };
-  w->few = few_form(*d, places);
-  if (w->few) {
-    w->off_rows = take((size_t)places * cols * 4);
-  } else {
+  const int64_t few = most_few(*d);
+  w->few = places <= few;
+  // Scratch for many vertices serves any fewer of them: a sorted call needs nearly none where its products are fused, a few places their hidden rows in fp32.
+  w->off_rows = take((size_t)(places < few ? places : few) * cols * 4);
+  w->bytes = off;
+  if (!w->few) {
+    off = kStatusBytes;
     const bool f32 = d->feat_dtype == IT_F32;
     w->tiles_max = it_experts_tiles_max(places, d->n_experts);
     const size_t rows = (size_t)w->tiles_max * 128, E = (size_t)d->n_experts, n1 = cols * (d->gated ? 2 : 1);
@@ -341,8 +345,8 @@ it_status plan(const it_experts_desc *d, int64_t n, ExpertsWs *w) {
     w->off_x = take(w->sorted ? rows * (size_t)d->in_dim * (f32 ? 6 : (d->in_dtype == IT_E4M3 ? 1 : 2)) : 0);
     w->off_w1 = take(f32 ? E * d->in_dim * n1 * 6 : 0);
     w->off_w2 = take(f32 ? E * d->hidden_dim * d->out_dim * 6 : 0);
+    w->bytes = off > w->bytes ? off : w->bytes;
   }
-  w->bytes = off;
   return IT_OK;
 }
 

@@ -130,3 +130,19 @@ def test_binding_refuses_tensors_that_the_library_could_not_tell():
         B.RouteDesc(n_experts=4, top_k=2, logit_dtype=torch.float32, score="tanh")
     with pytest.raises(ValueError, match="current CUDA device"):
         B.ExpertsDesc(n_experts=2, top_k=1, in_dim=8, out_dim=8, feat_dtype=torch.float32, W1=torch.ones(2, 8, 8))
+
+
+@pytest.mark.parametrize("kw", [dict(in_dim=256, hidden_dim=1024, out_dim=256, top_k=1), dict(in_dim=64, hidden_dim=0, out_dim=4096, top_k=1, W2=None), dict(in_dim=64, hidden_dim=4096, out_dim=8),
+                                dict(in_dim=768, hidden_dim=1024, out_dim=768, gated=1, top_k=4), dict(feat_dtype=0, in_dtype=0, in_dim=8, hidden_dim=2048, out_dim=8, top_k=1),
+                                dict(feat_dtype=0, in_dtype=0, in_dim=1024, hidden_dim=1024, out_dim=1024, top_k=3), dict(in_dtype=2, in_dim=512, hidden_dim=1024, out_dim=256, top_k=1),
+                                dict(in_dim=65536, hidden_dim=65536, out_dim=8, top_k=2)], ids=str)
+@pytest.mark.parametrize("n_experts", [1, 4, 300, 1025])
+def test_scratch_for_many_vertices_serves_fewer(kw, n_experts):
+    """A program sizes its workspace once, for the most vertices that it scores at a time."""
+    d = B.it_experts_desc(**{**dict(n_experts=n_experts, top_k=2, in_dim=64, hidden_dim=128, out_dim=64, feat_dtype=1, in_dtype=1, act=1, gated=0, W1=6 * BIG, b1=None, W2=7 * BIG,
+                                    b2=None, w1_scale=None), **kw})
+    before, size = 0, C.c_size_t()
+    for n in [*range(0, 520), 700, 1000, 6143, 6145, 16384, 16385, 50_000, 60_000, 100_000, 1_000_000]:
+        assert B.lib().it_experts_workspace_bytes(C.byref(d), n, C.byref(size)) == 0
+        assert size.value >= before, n
+        before = size.value
