@@ -433,9 +433,26 @@ def _stream_on(device, stream):
     return _raw_stream(device) if _raw_stream is not None else torch.cuda.current_stream().cuda_stream
 
 
+class _Desc:
+    """A description whose C form is kept from call to call.  The fields do not change, but what a tensor among them stands for may (`.data =`, `set_`, `resize_`, a
+    storage given back): every call looks whether addresses, sizes and layouts are those of the C form, and makes it anew, checks and all, where they are not."""
+
+    def _bind(self, device):
+        c, held = self._form(device)
+        held = [t for t in held if t is not None]
+        probes = [f for t in held for f in (t.data_ptr, t.numel, t.is_contiguous)]
+        for name, value in (("_c", c), ("_ref", C.byref(c)), ("_probes", probes), ("_seen", [f() for f in probes]), ("_on", device)):
+            object.__setattr__(self, name, value)
+
+    def _current(self, device):
+        if self._on != device or [f() for f in self._probes] != self._seen:
+            self._bind(device)
+        return self._ref
+
+
 @dataclass(frozen=True)
-class NormDesc:
-    """it_norm_desc; out_dtype None: feat_dtype.  The C form is made once: the fields do not change."""
+class NormDesc(_Desc):
+    """it_norm_desc; out_dtype None: feat_dtype."""
     dim: int
     feat_dtype: torch.dtype
     weight: torch.Tensor | None = None
@@ -445,16 +462,18 @@ class NormDesc:
     def __post_init__(self):
         out = self.feat_dtype if self.out_dtype is None else self.out_dtype
         object.__setattr__(self, "out_dtype", out)
-        object.__setattr__(self, "_c", it_norm_desc(self.dim, _dtype_code(self.feat_dtype), _dtype_code(out), self.eps,
-                                                    _addr("weight", self.weight, torch.float32, (self.dim,), _device())))
-        object.__setattr__(self, "_ref", C.byref(self._c))
+        self._bind(_device())
+
+    def _form(self, dev):
+        return it_norm_desc(self.dim, _dtype_code(self.feat_dtype), _dtype_code(self.out_dtype), self.eps,
+                            _addr("weight", self.weight, torch.float32, (self.dim,), dev)), [self.weight]
 
 
 def it_residual_norm(d: NormDesc, x, out, residual=None, sum_out=None, scales=None, stream=None):
     """s = x + residual; out = s / sqrt(mean(s^2) + eps) * weight, in feat_dtype or in e4m3 with scales [n]; sum_out = s.  Returns out."""
     n, f, dev = x.shape[0], d.feat_dtype, _device()
     shape = (n, d.dim)
-    status = lib().it_residual_norm(d._ref, n, _addr("x", x, f, shape, dev), _addr("residual", residual, f, shape, dev), _addr("sum_out", sum_out, f, shape, dev),
+    status = lib().it_residual_norm(d._current(dev), n, _addr("x", x, f, shape, dev), _addr("residual", residual, f, shape, dev), _addr("sum_out", sum_out, f, shape, dev),
                                     _addr("out", out, d.out_dtype, shape, dev), _addr("scales", scales, torch.float32, (n,), dev), _stream_on(dev, stream))
     if status:
         _check(status)
@@ -462,8 +481,8 @@ def it_residual_norm(d: NormDesc, x, out, residual=None, sum_out=None, scales=No
 
 
 @dataclass(frozen=True)
-class RouteDesc:
-    """it_route_desc; the C form is made once."""
+class RouteDesc(_Desc):
+    """it_route_desc."""
     n_experts: int
     top_k: int
     logit_dtype: torch.dtype
@@ -476,17 +495,19 @@ class RouteDesc:
     weight_scale: float = 1.0
 
     def __post_init__(self):
-        bias = _addr("balance_bias", self.balance_bias, torch.float32, (self.n_experts,), _device())
-        object.__setattr__(self, "_c", it_route_desc(self.n_experts, self.top_k, _dtype_code(self.logit_dtype), SCORES[self.score], bias, self.n_groups,
-                                                     self.group_k, self.group_best, int(self.renormalise), self.weight_scale))
-        object.__setattr__(self, "_ref", C.byref(self._c))
+        self._bind(_device())
+
+    def _form(self, dev):
+        bias = _addr("balance_bias", self.balance_bias, torch.float32, (self.n_experts,), dev)
+        return it_route_desc(self.n_experts, self.top_k, _dtype_code(self.logit_dtype), SCORES[self.score], bias, self.n_groups,
+                             self.group_k, self.group_best, int(self.renormalise), self.weight_scale), [self.balance_bias]
 
 
 def it_route(d: RouteDesc, logits, ids, weights, stream=None):
     """logits [n, n_experts] -> ids int32 [n, top_k] (-1: none left), weights fp32 [n, top_k].  Returns (ids, weights)."""
     n, dev = logits.shape[0], _device()
     chosen = (n, d.top_k)
-    status = lib().it_route(d._ref, n, _addr("logits", logits, d.logit_dtype, (n, d.n_experts), dev), _addr("ids", ids, torch.int32, chosen, dev),
+    status = lib().it_route(d._current(dev), n, _addr("logits", logits, d.logit_dtype, (n, d.n_experts), dev), _addr("ids", ids, torch.int32, chosen, dev),
                             _addr("weights", weights, torch.float32, chosen, dev), _stream_on(dev, stream))
     if status:
         _check(status)
@@ -494,8 +515,8 @@ def it_route(d: RouteDesc, logits, ids, weights, stream=None):
 
 
 @dataclass(frozen=True)
-class ExpertsDesc:
-    """it_experts_desc; states are e4m3 where W1 is.  The C form is made once."""
+class ExpertsDesc(_Desc):
+    """it_experts_desc; states are e4m3 where W1 is."""
     n_experts: int
     top_k: int
     in_dim: int
@@ -511,17 +532,19 @@ class ExpertsDesc:
     w1_scale: torch.Tensor | None = None
 
     def __post_init__(self):
-        e, h, o = self.n_experts, self.hidden_dim, self.out_dim
-        n1 = h * (2 if self.gated else 1) if h > 0 else o
         eight = self.W1.dtype == torch.float8_e4m3fn
         object.__setattr__(self, "in_dtype", torch.float8_e4m3fn if eight else self.feat_dtype)
-        f32, dev = torch.float32, _device()
+        self._bind(_device())
+
+    def _form(self, dev):
+        e, h, o = self.n_experts, self.hidden_dim, self.out_dim
+        n1 = h * (2 if self.gated else 1) if h > 0 else o
+        f32 = torch.float32
         c = it_experts_desc(e, self.top_k, self.in_dim, h, o, _dtype_code(self.feat_dtype), _dtype_code(self.in_dtype), EXPERT_ACTS[self.act], int(self.gated),
                             _addr("W1", self.W1, self.in_dtype, (e, self.in_dim, n1), dev), _addr("b1", self.b1, f32, (e, n1), dev),
                             _addr("W2", self.W2, self.feat_dtype, (e, h, o), dev), _addr("b2", self.b2, f32, (e, o), dev),
                             _addr("w1_scale", self.w1_scale, f32, (e, n1), dev))
-        object.__setattr__(self, "_c", c)
-        object.__setattr__(self, "_ref", C.byref(c))
+        return c, [self.W1, self.b1, self.W2, self.b2, self.w1_scale]
 
 
 def it_experts_workspace_bytes(d: ExpertsDesc, n: int) -> int:
@@ -545,7 +568,7 @@ def _experts(call, d, x, ids, weights, out, workspace, x_scale, stream):
     chosen = (n, d.top_k)
     if not workspace.is_contiguous() or workspace.get_device() != dev:
         raise ValueError("workspace must be a contiguous tensor on the current CUDA device")
-    status = call(d._ref, n, _addr("x", x, d.in_dtype, (n, d.in_dim), dev), _addr("x_scale", x_scale, f32, (n,), dev), _addr("ids", ids, torch.int32, chosen, dev),
+    status = call(d._current(dev), n, _addr("x", x, d.in_dtype, (n, d.in_dim), dev), _addr("x_scale", x_scale, f32, (n,), dev), _addr("ids", ids, torch.int32, chosen, dev),
                   _addr("weights", weights, f32, chosen, dev), _addr("out", out, d.feat_dtype, (n, d.out_dim), dev), workspace.data_ptr(), _nbytes(workspace),
                   _stream_on(dev, stream))
     if status:

@@ -146,3 +146,91 @@ def test_scratch_for_many_vertices_serves_fewer(kw, n_experts):
         assert B.lib().it_experts_workspace_bytes(C.byref(d), n, C.byref(size)) == 0
         assert size.value >= before, n
         before = size.value
+
+
+class _OnDevice:
+    """What the binding asks of a tensor, with its answers set by the test."""
+
+    def __init__(self, shape, dtype, address, device=0):
+        import torch
+        self.shape, self.dtype, self.address, self.device, self.dense = torch.Size(shape), dtype, address, device, True
+
+    def get_device(self):
+        return self.device
+
+    def is_contiguous(self):
+        return self.dense
+
+    def data_ptr(self):
+        return self.address
+
+    def numel(self):
+        return self.shape.numel()
+
+
+def _descriptions(monkeypatch):
+    """Every description with every tensor it may hold, each tensor's attribute and field, and the call that takes them (nothing is launched: no rows)."""
+    import torch
+    monkeypatch.setattr(B, "_device", lambda: 0)
+    monkeypatch.setattr(B, "_stream_on", lambda device, stream: None)
+    monkeypatch.setattr(B, "_nbytes", lambda t: 1 << 20)
+    f32, bf16, e4m3 = torch.float32, torch.bfloat16, torch.float8_e4m3fn
+    new = lambda shape, dtype: _OnDevice(shape, dtype, new.at.__next__())   # noqa: E731
+    new.at = iter(range(1 << 30, 1 << 40, 1 << 24))
+    norm = B.NormDesc(dim=64, feat_dtype=bf16, weight=new((64,), f32))
+    route = B.RouteDesc(n_experts=8, top_k=2, logit_dtype=f32, balance_bias=new((8,), f32))
+    experts = B.ExpertsDesc(n_experts=4, top_k=2, in_dim=64, hidden_dim=32, out_dim=16, feat_dtype=bf16, W1=new((4, 64, 32), e4m3), b1=new((4, 32), f32), W2=new((4, 32, 16), bf16),
+                            b2=new((4, 16), f32), w1_scale=new((4, 32), f32))
+    calls = {}
+
+    class Library:
+        def __getattr__(self, name):
+            return lambda ref, *args: calls.__setitem__("c", ref._obj) or 0
+    monkeypatch.setattr(B, "lib", lambda: Library())
+    i32 = torch.int32
+    return calls, [(norm, ["weight"], lambda: B.it_residual_norm(norm, new((3, 64), bf16), new((3, 64), bf16))),
+                   (route, ["balance_bias"], lambda: B.it_route(route, new((3, 8), f32), new((3, 2), i32), new((3, 2), f32))),
+                   (experts, ["W1", "b1", "W2", "b2", "w1_scale"],
+                    lambda: B.it_experts_forward(experts, new((3, 64), e4m3), new((3, 2), i32), new((3, 2), f32), new((3, 16), bf16), new((1 << 20,), torch.uint8), x_scale=new((3,), f32)))]
+
+
+def test_descriptions_follow_their_tensors(monkeypatch):
+    """A tensor whose storage was replaced after the description was made: the call takes the new address, not the one that was given back."""
+    calls, every = _descriptions(monkeypatch)
+    for d, fields, call in every:
+        call()
+        for f in fields:
+            t = getattr(d, f)
+            assert getattr(calls["c"], f) == t.address
+            t.address += 1 << 50
+            call()
+            assert getattr(calls["c"], f) == t.address, f
+
+
+def test_descriptions_refuse_what_their_tensors_became(monkeypatch):
+    """Another layout, size or device than the description says: refused by the call, as it would be by a new description."""
+    import torch
+    calls, every = _descriptions(monkeypatch)
+    for d, fields, call in every:
+        for f in fields:
+            t = getattr(d, f)
+            for name, value in (("dense", False), ("shape", torch.Size((3,))), ("device", 1)):
+                was = getattr(t, name)
+                setattr(t, name, value)
+                if name == "device":   # (a tensor's address is another there)
+                    t.address += 1 << 51
+                with pytest.raises(ValueError):
+                    call()
+                setattr(t, name, was)
+                call()
+
+
+def test_descriptions_refuse_another_current_device(monkeypatch):
+    """Made on one device, called on another: its tensors are not there, wherever the call's own are."""
+    calls, every = _descriptions(monkeypatch)
+    monkeypatch.setattr(B, "_device", lambda: 1)
+    there = _OnDevice.__init__
+    monkeypatch.setattr(_OnDevice, "__init__", lambda self, shape, dtype, address: there(self, shape, dtype, address, 1))
+    for d, fields, call in every:
+        with pytest.raises(ValueError, match="current CUDA device"):
+            call()
