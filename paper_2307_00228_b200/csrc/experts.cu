@@ -107,7 +107,7 @@ __global__ void __launch_bounds__(ROWS_THREADS) expert_rows_kernel(const RowsPar
         xv[u] = in ? elem_f32(x + r) * f : 0.f;
 #pragma unroll
         for (int g = 0; g < PARTS; ++g)
-          q[g][u] = in ? __ldg(reinterpret_cast<const uint4 *>(w + (int64_t)r * p.w_cols + g * p.gated_at)) : make_uint4(0, 0, 0, 0);
+          q[g][u] = in ? *reinterpret_cast<const uint4 *>(w + (int64_t)r * p.w_cols + g * p.gated_at) : make_uint4(0, 0, 0, 0);
       }
 #pragma unroll
       for (int u = 0; u < ROWS_UNROLL; ++u) {

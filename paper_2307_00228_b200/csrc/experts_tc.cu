@@ -279,8 +279,8 @@ expert_gemm_kernel(const __grid_constant__ CUtensorMap map_a, const __grid_const
         const int ac = i * 128 + lane * 4, second = GATED && ac >= p.cols_per_tile, c = c_tile + ac - (second ? p.cols_per_tile : 0);
         if (ac >= p.bn || c >= p.cols) continue;
         const int64_t at = w_row + c + (second ? p.cols : 0);
-        if (p.bias) bias[i] = __ldg(reinterpret_cast<const float4 *>(p.bias + at));
-        if constexpr (EIGHT) scale[i] = __ldg(reinterpret_cast<const float4 *>(p.w_scale + at));
+        if (p.bias) bias[i] = *reinterpret_cast<const float4 *>(p.bias + at);
+        if constexpr (EIGHT) scale[i] = *reinterpret_cast<const float4 *>(p.w_scale + at);
       }
       bool ok = lane == 0 ? mbar_wait(&acc_empty[acc], acc_phase ^ 1u, abort_flag, p.spin_limit, EX_EPI_BACKOFF) : true;
       if (!__shfl_sync(0xffffffffu, (int)ok, 0)) break;

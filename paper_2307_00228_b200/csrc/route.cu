@@ -550,7 +550,7 @@ __global__ void __launch_bounds__(ROUTE_THREADS) route_thread_kernel(const Route
       if (p.bias) {
 #pragma unroll
         for (int c = 0; c < C; ++c)
-          if (c < E) key[c] = key[c] > kClosed ? open_key(fmaf(rough(key[c]), inv, __ldg(p.bias + c))) : kClosed;
+          if (c < E) key[c] = key[c] > kClosed ? open_key(fmaf(rough(key[c]), inv, p.bias[c])) : kClosed;
       }
     }
     float best[KL];

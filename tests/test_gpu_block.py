@@ -71,3 +71,57 @@ def test_kernels_are_counted_and_profiled():
     stats = {s["name"]: s for s in B.it_profile_end()}
     assert B.it_kernel_launch_count() == before + 1
     assert stats["residual_norm"]["launches"] == 1 and stats["residual_norm"]["algo_bytes"] == 2 * 100 * 64 * 4
+
+
+@pytest.mark.parametrize("rounds", [12])
+def test_arrays_written_by_the_call_before(rounds):
+    """A kernel of these calls may start while the one before it still runs: the norm writes, each time something else, what the next call takes as its balance
+    bias, as the first weights, their bias or their scales."""
+    g = torch.Generator(device="cuda").manual_seed(3)
+    r = lambda *s: torch.randn(s, generator=g, device="cuda")   # noqa: E731
+    E, n, a, o = 16, 60, 64, 64
+    many = 1500
+    norm = B.NormDesc(dim=64, feat_dtype=F32)
+    one = B.NormDesc(dim=E, feat_dtype=F32)
+    logits, logits2 = r(n, E), r(n, 64)
+    bias, bias2 = torch.zeros(E, device="cuda"), torch.zeros(64, device="cuda")
+    W1, b1 = torch.zeros(E, a, o, device="cuda"), torch.zeros(E, o, device="cuda")
+    eight_W1, eight_scale = (r(E, a, o) * 50).to(E4M3), torch.zeros(E, o, device="cuda")
+    routes = [(B.RouteDesc(n_experts=E, top_k=2, logit_dtype=F32, score="sigmoid", balance_bias=bias), logits, bias, one),
+              (B.RouteDesc(n_experts=64, top_k=6, logit_dtype=F32, score="sigmoid", balance_bias=bias2), logits2, bias2, norm)]
+    full = B.ExpertsDesc(n_experts=E, top_k=2, in_dim=a, out_dim=o, feat_dtype=F32, W1=W1, b1=b1)
+    eight = B.ExpertsDesc(n_experts=E, top_k=2, in_dim=a, out_dim=o, feat_dtype=BF16, W1=eight_W1, w1_scale=eight_scale)
+    ids, w = torch.randint(0, E, (many, 2), generator=g, device="cuda", dtype=torch.int32), torch.rand(many, 2, generator=g, device="cuda")
+    x, x8, xs = r(many, a), (r(many, a) * 50).to(E4M3), torch.full((many,), 0.02, device="cuda")
+    ws = torch.empty(max(B.it_experts_workspace_bytes(d, many) for d in (full, eight)), dtype=torch.uint8, device="cuda")
+
+    def calls(sources, wait):
+        """Every array from its source, then the call that takes it; `wait`: the GPU is waited for in between."""
+        got = []
+        b1.zero_()   # (the first products take it before it is written)
+        sync = torch.cuda.synchronize if wait else lambda: None
+        for (d, l, to, nd), src in zip(routes, sources):
+            i, v = torch.empty(n, d.top_k, dtype=torch.int32, device="cuda"), torch.empty(n, d.top_k, device="cuda")
+            B.it_residual_norm(nd, src, to.view(1, -1)); sync()
+            B.it_route(d, l, i, v); sync()
+            got += [i, v]
+        for count in (n // 4, many):
+            out, out8 = torch.empty(count, o, device="cuda"), torch.empty(count, o, dtype=BF16, device="cuda")
+            B.it_residual_norm(norm, sources[2], W1.view(-1, 64)); sync()
+            B.it_experts_forward(full, x[:count], ids[:count], w[:count], out, ws); sync()
+            got.append(out.clone())
+            B.it_residual_norm(norm, sources[3], b1); sync()
+            B.it_experts_forward(full, x[:count], ids[:count], w[:count], out, ws); sync()
+            B.it_residual_norm(norm, sources[3], eight_scale); sync()
+            B.it_experts_forward(eight, x8[:count], ids[:count], w[:count], out8, ws, x_scale=xs[:count]); sync()
+            got += [out, out8]
+        return got
+
+    every = [[r(1, E), r(1, 64), r(E * a, 64), r(E, 64)] for _ in range(rounds)]
+    want = [calls(s, True) for s in every]
+    for _ in range(3):
+        got = [calls(s, False) for s in every]
+        torch.cuda.synchronize()
+        for a_, b_ in zip(got, want):
+            for p, q in zip(a_, b_):
+                assert torch.equal(p, q)
