@@ -29,6 +29,7 @@ __host__ __device__ constexpr int ex_staging(it_expert_store s) { return ex_dire
 struct ExMeta { int32_t place[TC_BM]; float weight[TC_BM]; float bias[256]; };
 struct ExMetaEight : ExMeta { float xs[TC_BM]; float scale[256]; };
 constexpr int EX_MAX_STAGES = 8;
+constexpr int EX_SLICE = 8;        // k-blocks of a slice (LONG_SUMS)
 constexpr int EX_EPI_BACKOFF = 64, EX_TMA_BACKOFF = 32;   // ns between polls
 
 struct ExParams {
@@ -36,9 +37,8 @@ struct ExParams {
   const void *A;
   int tiles_max;
   int n_splits, bn, cols_per_tile;   // column tiles; columns of an accumulator; columns of the result in a tile (gated: bn / 2)
-  int K, kb, passes;                 // k-blocks of a pass; passes: 1, or the six products of fp32 parts
+  int K, kb;                         // k-blocks
   int stages;
-  int halves;                        // 2: either half of K has an accumulator of its own, and a tile both of them (fp32)
   int box_panels;                    // panels of W that one copy fetches, or 0: a copy each
   int gather_div;                    // > 0: row of A = place / gather_div; 0: row = position
   int a_rows;                        // rows of one part of A
@@ -52,21 +52,25 @@ struct ExParams {
   int no_loads;
 };
 
-// the parts of A and W that pass i multiplies, smallest products first
-__device__ __forceinline__ void pass_parts(int passes, int i, int *pa, int *pb) {
+// the parts of A and W that pass i of the six multiplies, smallest products first
+__device__ __forceinline__ void pass_parts(int i, int *pa, int *pb) {
   constexpr uint32_t A = 0x001102u, B = 0x010120u;   // nibble i: (2,0) (0,2) (1,1) (1,0) (0,1) (0,0)
-  *pa = passes == 1 ? 0 : (int)((A >> (4 * i)) & 15u);
-  *pb = passes == 1 ? 0 : (int)((B >> (4 * i)) & 15u);
+  *pa = (int)((A >> (4 * i)) & 15u);
+  *pb = (int)((B >> (4 * i)) & 15u);
 }
 
 // TRI (fp32, K up to 512): a stage holds the three parts of a k-block of either operand, and an accumulator of its own takes the small products.
-template <bool EIGHT, it_expert_store STORE, bool GATED, bool TRI>
+// LONG_SUMS (fp32, K above 512): slice by slice of K, each with all its six products; the epilogue adds the slices up, rounding to nearest, in the second
+// accumulator's place.
+enum ExForm { EX_PLAIN, EX_TRI, EX_LONG_SUMS };
+template <bool EIGHT, it_expert_store STORE, bool GATED, ExForm FORM>
 __global__ void __launch_bounds__(EX_THREADS, 1)
 expert_gemm_kernel(const __grid_constant__ CUtensorMap map_a, const __grid_constant__ CUtensorMap map_w, const ExParams p) {
   extern __shared__ __align__(1024) unsigned char base[];   // (the swizzle goes by addresses: stages start at multiples of 1024)
   const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
   constexpr int BK = EIGHT ? 128 : 64;                  // elements of a k-block, and columns of a panel
   constexpr int PANEL = BK * TC_KBLOCK_BYTES;           // bytes of a panel of W: BK rows x 128 bytes
+  constexpr bool TRI = FORM == EX_TRI, LONG_SUMS = FORM == EX_LONG_SUMS;
   constexpr int P = TRI ? 3 : 1;                        // parts in a stage: of A, then of W
   const int b_bytes = p.bn * TC_KBLOCK_BYTES, stage_bytes = P * (EX_STAGE_A + b_bytes);
 
@@ -111,8 +115,10 @@ expert_gemm_kernel(const __grid_constant__ CUtensorMap map_a, const __grid_const
   int m_tiles = *p.n_tiles;
   m_tiles = m_tiles < p.tiles_max ? m_tiles : p.tiles_max;
   const uint32_t splits = (uint32_t)p.n_splits, n_tiles = (uint32_t)m_tiles * splits;   // (below 2^31)
-  const int passes = TRI ? 1 : p.passes, KB = p.kb * passes;
-  const uint32_t bufs = !TRI && p.halves == 2 ? 1u : 2u, acc_stride = (uint32_t)p.bn * (TRI ? 2u : 1u);   // accumulators of tiles in flight
+  constexpr int PASSES = LONG_SUMS ? 6 : 1;   // walks over the k-blocks
+  const int slices = LONG_SUMS ? (p.kb + EX_SLICE - 1) / EX_SLICE : 1;
+  constexpr uint32_t bufs = LONG_SUMS ? 1u : 2u;
+  const uint32_t acc_stride = (uint32_t)p.bn * (TRI ? 2u : 1u);   // accumulators of tiles in flight
 
   if (warp < EX_FETCH_WARPS) {
     // ------------------------------------------------------------------ producers: rows found by place by all four warps, 16 bytes a lane;
@@ -152,10 +158,11 @@ expert_gemm_kernel(const __grid_constant__ CUtensorMap map_a, const __grid_const
           real |= (r >= 0 ? 1u : 0u) << i;
         }
       }
-      for (int pass = 0; pass < passes && ok; ++pass) {
-        int pa, pb;
-        pass_parts(passes, pass, &pa, &pb);
-        for (int kb = 0; kb < p.kb; ++kb) {
+      for (int round = 0; round < slices * PASSES && ok; ++round) {
+        int pa = 0, pb = 0;
+        if constexpr (LONG_SUMS) pass_parts(round % PASSES, &pa, &pb);
+        const int kb0 = LONG_SUMS ? round / PASSES * EX_SLICE : 0, kb1 = LONG_SUMS && kb0 + EX_SLICE < p.kb ? kb0 + EX_SLICE : p.kb;
+        for (int kb = kb0; kb < kb1; ++kb) {
           if (lane == 0) {
             ok = mbar_wait(&empty[stage], phase ^ 1u, abort_flag, p.spin_limit, EX_TMA_BACKOFF);
             if (ok && warp == 0) mbar_arrive_expect_tx(&full[stage], tma_bytes);
@@ -202,12 +209,13 @@ expert_gemm_kernel(const __grid_constant__ CUtensorMap map_a, const __grid_const
     const uint32_t idesc = (1u << 4) | (fmt << 7) | (fmt << 10) | (1u << 16) | ((uint32_t)(p.bn >> 3) << 17) | ((uint32_t)(TC_BM >> 4) << 24);
     uint32_t stage = 0, phase = 0, acc = 0, acc_phase = 0;
     bool ok = true;
-    for (uint32_t tile = blockIdx.x; tile < n_tiles && ok; tile += gridDim.x) {
+    for (uint32_t tile = blockIdx.x; tile < n_tiles && ok; tile += gridDim.x)
+    for (int slice = 0; slice < slices; ++slice) {
+      const int kbs = LONG_SUMS && p.kb - slice * EX_SLICE > EX_SLICE ? EX_SLICE : p.kb - (LONG_SUMS ? slice * EX_SLICE : 0);   // k-blocks of a pass
       ok = ex_wait_warp(&acc_empty[acc], acc_phase ^ 1u, abort_flag, p.spin_limit);
       if (!ok) break;
       tc_fence_after();
-      int kb_in_pass = 0;
-      for (int kb = 0; kb < KB; ++kb) {
+      for (int kb = 0; kb < kbs * PASSES; ++kb) {
         ok = ex_wait_warp(&full[stage], phase, abort_flag, p.spin_limit);
         if (!ok) break;
         // gathered rows were written by the threads of the other warps: what follows reads them through the tensor core's path
@@ -218,7 +226,7 @@ expert_gemm_kernel(const __grid_constant__ CUtensorMap map_a, const __grid_const
 #pragma unroll
           for (int pass = 0; pass < 6; ++pass) {
             int pa, pb;
-            pass_parts(6, pass, &pa, &pb);
+            pass_parts(pass, &pa, &pb);
             const uint64_t a_d = make_desc(a_s + pa * EX_STAGE_A), b_d = make_desc_mn(a_s + 3 * EX_STAGE_A + (uint32_t)(pb * b_bytes), PANEL);
 #pragma unroll
             for (int k = 0; k < 4; ++k)
@@ -226,15 +234,10 @@ expert_gemm_kernel(const __grid_constant__ CUtensorMap map_a, const __grid_const
           }
         } else {
           const uint64_t a_d = make_desc(a_s), b_d = make_desc_mn(a_s + EX_STAGE_A, PANEL);
-          // (two halves: the first product into either of them is the first pass's)
-          const int half_at = p.kb / 2;
-          const bool second = p.halves == 2 && kb_in_pass >= half_at;
-          const uint32_t d_tmem = tmem_base + (p.halves == 2 ? (second ? (uint32_t)p.bn : 0u) : acc * acc_stride);
-          const bool begun = second ? kb > half_at : kb > 0;
+          const uint32_t d_tmem = tmem_base + acc * acc_stride;
 #pragma unroll
           for (int k = 0; k < 4; ++k)   // four steps of 32 bytes of K: a quarter of the k-block's rows of W
-            ex_mma<EIGHT>(lead, d_tmem, a_d + k * 2, b_d + k * (PANEL / 64), idesc, begun || k != 0);
-          if (++kb_in_pass == p.kb) kb_in_pass = 0;
+            ex_mma<EIGHT>(lead, d_tmem, a_d + k * 2, b_d + k * (PANEL / 64), idesc, kb > 0 || k != 0);
         }
         ex_commit(lead, &empty[stage]);
         if (++stage == (uint32_t)p.stages) { stage = 0; phase ^= 1u; }
@@ -282,6 +285,16 @@ expert_gemm_kernel(const __grid_constant__ CUtensorMap map_a, const __grid_const
         if (p.bias) bias[i] = *reinterpret_cast<const float4 *>(p.bias + at);
         if constexpr (EIGHT) scale[i] = *reinterpret_cast<const float4 *>(p.w_scale + at);
       }
+      if constexpr (LONG_SUMS) {   // (the slices before the last need nothing of this)
+        bool ok = true;
+        for (int slice = 0; slice + 1 < slices && ok; ++slice) {
+          ok = lane == 0 ? mbar_wait(&acc_empty[acc], acc_phase ^ 1u, abort_flag, p.spin_limit, EX_EPI_BACKOFF) : true;
+          ok = __shfl_sync(0xffffffffu, (int)ok, 0);
+          if (ok && lane == 0) mbar_arrive(&meta_full[acc]);
+          acc_phase ^= 1u;
+        }
+        if (!ok) break;
+      }
       bool ok = lane == 0 ? mbar_wait(&acc_empty[acc], acc_phase ^ 1u, abort_flag, p.spin_limit, EX_EPI_BACKOFF) : true;
       if (!__shfl_sync(0xffffffffu, (int)ok, 0)) break;
       Meta &k = meta[acc];
@@ -304,7 +317,6 @@ expert_gemm_kernel(const __grid_constant__ CUtensorMap map_a, const __grid_const
     constexpr bool F32_OUT = STORE == IT_EXPERT_SUMS || STORE == IT_EXPERT_OUT_F32, DIRECT = STORE == IT_EXPERT_OUT_BF16 || STORE == IT_EXPERT_OUT_F32;
     constexpr int ESIZE = F32_OUT ? 4 : 2, COLS = 64 / ESIZE;   // 64 bytes of a row are staged at a time
     constexpr int PLANES = STORE == IT_EXPERT_PARTS ? 3 : 1;
-    constexpr bool MAY_SPLIT = !EIGHT && (STORE == IT_EXPERT_PARTS || F32_OUT);
     constexpr int ROW = DIRECT ? 128 : 64, PIECES = ROW / 16, AT_ONCE = 32 / PIECES;   // staging tile: bytes of a row, its lanes, rows that a warp stores at once
     const uint32_t stage_s = smem_u32(staging) + (uint32_t)(warp - EX_EPI_WARP0) * ex_staging(STORE);
     // 16-byte pieces are swizzled: this lane's row as it writes it (piece i: put ^ 16 i), and its piece of every row that it stores
@@ -315,6 +327,38 @@ expert_gemm_kernel(const __grid_constant__ CUtensorMap map_a, const __grid_const
     uint32_t acc = 0, acc_phase = 0;
     for (uint32_t tile = blockIdx.x; tile < n_tiles; tile += gridDim.x) {
       const int m = (int)(tile / splits), c_tile = (int)(tile % splits) * p.cols_per_tile;
+      if constexpr (LONG_SUMS) {
+        // this warp's columns of every slice but the last: into the place of the sums, or added to what is there
+        const int cols = p.cols - c_tile < p.cols_per_tile ? p.cols - c_tile : p.cols_per_tile;
+        const int half = (cols + 32 * EX_EPI_SUBS - 1) / (32 * EX_EPI_SUBS) * 32, from = sub * half, upto = from + half < cols ? from + half : cols;
+        const uint32_t product = tmem_base + ((uint32_t)(quarter * 32) << 16), sums = product + (uint32_t)p.bn;
+        bool ok = true;
+        for (int slice = 0; slice + 1 < slices; ++slice) {
+          ok = mbar_wait(&meta_full[0], acc_phase, abort_flag, p.spin_limit, EX_EPI_BACKOFF) && mbar_wait(&acc_full[0], acc_phase, abort_flag, p.spin_limit, EX_EPI_BACKOFF);
+          ok = __all_sync(0xffffffffu, ok);
+          if (!ok) break;
+          tc_fence_after();
+#pragma unroll
+          for (int second = 0; second < (GATED ? 2 : 1); ++second)
+            for (int c = from + second * p.cols_per_tile; c < upto + second * p.cols_per_tile; c += 16) {
+              uint32_t r[16], q[16];
+              tmem_ld16(product + (uint32_t)c, r);
+              if (slice > 0) tmem_ld16(sums + (uint32_t)c, q);
+              tmem_ld_wait();
+              if (slice > 0) {
+#pragma unroll
+                for (int i = 0; i < 16; ++i) r[i] = __float_as_uint(__uint_as_float(r[i]) + __uint_as_float(q[i]));
+              }
+              tmem_st16(sums + (uint32_t)c, r);
+            }
+          tmem_st_wait();
+          tc_fence_before();
+          __syncwarp();
+          if (lane == 0) mbar_arrive(&acc_empty[0]);
+          acc_phase ^= 1u;
+        }
+        if (!ok) break;
+      }
       const int64_t pos0 = (int64_t)m * TC_BM + quarter * 32;
       const bool ok = mbar_wait(&meta_full[acc], acc_phase, abort_flag, p.spin_limit, EX_EPI_BACKOFF) &&
                       mbar_wait(&acc_full[acc], acc_phase, abort_flag, p.spin_limit, EX_EPI_BACKOFF);
@@ -447,7 +491,7 @@ expert_gemm_kernel(const __grid_constant__ CUtensorMap map_a, const __grid_const
       // (the next 32 columns read ahead would take registers that are not there: with them spilled the epilogue took twice as long)
       auto read = [&](int col, uint32_t (&r)[32]) {
         tmem_ld32(taddr + (uint32_t)col, r);
-        if (TRI || (MAY_SPLIT && p.halves == 2)) {
+        if constexpr (TRI || LONG_SUMS) {
           uint32_t q[32];
           tmem_ld32(taddr + (uint32_t)(p.bn + col), q);
           tmem_ld_wait();
@@ -482,10 +526,10 @@ expert_gemm_kernel(const __grid_constant__ CUtensorMap map_a, const __grid_const
 }
 
 // ----------------------------------------------------------------------------- host side
-template <bool EIGHT, it_expert_store STORE, bool GATED, bool TRI = false>
+template <bool EIGHT, it_expert_store STORE, bool GATED, ExForm FORM = EX_PLAIN>
 it_status launch(const CUtensorMap &ma, const CUtensorMap &mw, const ExParams &p, int grid, int smem, double bytes, double flops, cudaStream_t st) {
-  IT_CUDA_TRY(cudaFuncSetAttribute(expert_gemm_kernel<EIGHT, STORE, GATED, TRI>, cudaFuncAttributeMaxDynamicSharedMemorySize, smem));
-  IT_LAUNCH(IT_K_EXPERT_GEMM, bytes, flops, st, IT_CUDA_TRY(it_launch_pdl(expert_gemm_kernel<EIGHT, STORE, GATED, TRI>, dim3((unsigned)grid), dim3(EX_THREADS), smem, st, ma, mw, p)));
+  IT_CUDA_TRY(cudaFuncSetAttribute(expert_gemm_kernel<EIGHT, STORE, GATED, FORM>, cudaFuncAttributeMaxDynamicSharedMemorySize, smem));
+  IT_LAUNCH(IT_K_EXPERT_GEMM, bytes, flops, st, IT_CUDA_TRY(it_launch_pdl(expert_gemm_kernel<EIGHT, STORE, GATED, FORM>, dim3((unsigned)grid), dim3(EX_THREADS), smem, st, ma, mw, p)));
   return IT_OK;
 }
 
@@ -495,7 +539,7 @@ it_status it_launch_expert_gemm(const it_experts_args &a, const it_experts_plan 
   const int elem = g.eight ? 1 : 2, BK = TC_KBLOCK_BYTES / elem;
   ExParams p{};
   p.order = q.order; p.tile_expert = q.tile_expert; p.n_tiles = q.n_tiles; p.tiles_max = (int)q.tiles_max;
-  p.K = g.K; p.kb = (g.K + BK - 1) / BK; p.passes = g.parts == 3 ? 6 : 1;
+  p.K = g.K; p.kb = (g.K + BK - 1) / BK;
   p.A = g.A; p.gather_div = g.gather ? a.d.top_k : 0; p.a_rows = (int)g.a_rows;
   p.n_experts = a.d.n_experts; p.w_cols = g.w_cols; p.cols = g.cols; p.act = g.act; p.gated = g.gated;
   p.bias = g.bias; p.w_scale = g.w_scale; p.x_scale = g.x_scale; p.weights = a.weights; p.x_div = a.d.top_k;
@@ -510,10 +554,9 @@ it_status it_launch_expert_gemm(const it_experts_args &a, const it_experts_plan 
   p.cols_per_tile = ((g.cols + p.n_splits - 1) / p.n_splits + BK - 1) / BK * BK;
   p.n_splits = (g.cols + p.cols_per_tile - 1) / p.cols_per_tile;
   p.bn = g.gated ? 2 * p.cols_per_tile : p.cols_per_tile;
-  // A tensor core cuts off what it adds to an accumulator, which pulls long sums towards zero: fp32, 2-norm of the error for K = 256, 512, 1024, 2048
-  // 3.5e-7, 6.1e-7, 1.2e-6, 2.1e-6 (a library's fp32 product 3e-7 to 7e-7).  Above K = 512 either half of K has an accumulator of its own (K = 1024,
-  // 2048: 6.9e-7, 9.8e-7), and the parts go by one after the other, the smallest products first.
-  p.halves = g.parts == 3 && !tri ? 2 : 1;
+  // A tensor core cuts off what it adds to an accumulator, which pulls long sums towards zero: fp32, 2-norm of the error with one accumulator for all of K =
+  // 512, 1024, 2048 4.9e-7, 9.8e-7, 2.1e-6 (a library's fp32 product 4e-7 to 7e-7), and in proportion.  Above K = 512 the epilogue adds up slices of 512, rounding to
+  // nearest: 4.8e-7 for K = 1024 to 8192, 5.2e-7 for 65536, at no cost (40k x 2048 x 256 479 us; slices of 256 2.6e-7 and 487, of 1024 9.8e-7 and 476).
 
   const cuuint64_t da[2] = {(cuuint64_t)g.K, (cuuint64_t)(g.a_rows * g.parts)}, sa[1] = {(cuuint64_t)g.K * elem};
   const cuuint32_t ba[2] = {(cuuint32_t)BK, (cuuint32_t)TC_BM};
@@ -544,27 +587,27 @@ it_status it_launch_expert_gemm(const it_experts_args &a, const it_experts_plan 
   const int64_t places = a.n * a.d.top_k;
   const double flops = 2.0 * places * g.K * (double)g.w_cols, bytes = (double)places * (g.K * elem * g.parts + g.cols * 4.0);
 #define IT_EX_LAUNCH(EIGHT, STORE, GATED) return launch<EIGHT, STORE, GATED>(ma, mw, p, grid, smem, bytes, flops, st)
-#define IT_EX_TRI(STORE, GATED) if (tri) return launch<false, STORE, GATED, true>(ma, mw, p, grid, smem, bytes, flops, st)
+#define IT_EX_F32(STORE, GATED)                                                                 \
+  if (tri) return launch<false, STORE, GATED, EX_TRI>(ma, mw, p, grid, smem, bytes, flops, st); \
+  return launch<false, STORE, GATED, EX_LONG_SUMS>(ma, mw, p, grid, smem, bytes, flops, st)
   switch (g.store) {
     case IT_EXPERT_HIDDEN:
       if (g.eight) { if (g.gated) IT_EX_LAUNCH(true, IT_EXPERT_HIDDEN, true); else IT_EX_LAUNCH(true, IT_EXPERT_HIDDEN, false); }
       if (g.gated) IT_EX_LAUNCH(false, IT_EXPERT_HIDDEN, true);
       IT_EX_LAUNCH(false, IT_EXPERT_HIDDEN, false);
     case IT_EXPERT_PARTS:
-      if (g.gated) { IT_EX_TRI(IT_EXPERT_PARTS, true); IT_EX_LAUNCH(false, IT_EXPERT_PARTS, true); }
-      IT_EX_TRI(IT_EXPERT_PARTS, false);
-      IT_EX_LAUNCH(false, IT_EXPERT_PARTS, false);
+      if (g.gated) { IT_EX_F32(IT_EXPERT_PARTS, true); }
+      IT_EX_F32(IT_EXPERT_PARTS, false);
     case IT_EXPERT_SUMS:
       if (g.eight) IT_EX_LAUNCH(true, IT_EXPERT_SUMS, false);
-      IT_EX_TRI(IT_EXPERT_SUMS, false);
+      if (g.parts == 3) { IT_EX_F32(IT_EXPERT_SUMS, false); }
       IT_EX_LAUNCH(false, IT_EXPERT_SUMS, false);
     case IT_EXPERT_OUT_BF16:
       if (g.eight) IT_EX_LAUNCH(true, IT_EXPERT_OUT_BF16, false);
       IT_EX_LAUNCH(false, IT_EXPERT_OUT_BF16, false);
     default:
-      IT_EX_TRI(IT_EXPERT_OUT_F32, false);
-      IT_EX_LAUNCH(false, IT_EXPERT_OUT_F32, false);
+      IT_EX_F32(IT_EXPERT_OUT_F32, false);
   }
-#undef IT_EX_TRI
+#undef IT_EX_F32
 #undef IT_EX_LAUNCH
 }
