@@ -32,3 +32,59 @@ def test_long_sums_of_both_products(a, h, o, gated):
     """(gated: the relative errors of the two factors add up)"""
     c = experts_case(a + h, 700, 2, 2, a, h, o, F32, act="none", gated=gated, biased=False)
     assert error(c, run_experts(c)) <= bound(a, h) + (bound(a) if gated else 0)
+
+
+# ----------------------------------------------------------------------------- six products, none of them missing
+def split3(v):
+    """fp32 as three bf16 parts, cut off: 8 bits each."""
+    parts = []
+    for _ in range(3):
+        top = (v.view(torch.int32) & -65536).view(F32)
+        parts.append(top.double())
+        v = v - top
+    return parts
+
+
+def product_of_parts(x, w, missing=None):
+    """The sum of the six products in 64 bits, or of the five others."""
+    a, b = split3(x), split3(w)
+    return sum(a[i] @ b[j] for i, j in SIX if (i, j) != missing)
+
+
+SIX = [(2, 0), (0, 2), (1, 1), (1, 0), (0, 1), (0, 0)]
+SHORT = [(64, 0, 64), (256, 0, 128), (64, 256, 64), (128, 128, 128)]
+
+
+@pytest.mark.parametrize("shape", SHORT, ids=str)
+@pytest.mark.parametrize("missing", [None, *SIX], ids=str)
+def test_the_bound_tells_a_missing_product(shape, missing):
+    a, h, o = shape
+    c = experts_case(a + h, 400, 1, 1, a, h, o, F32, act="none", biased=False)
+    x = c["x"]
+    for first, w in enumerate((c["W1"], c["W2"])):
+        if w is None:
+            continue
+        want, got = x.double() @ w[0].double(), product_of_parts(x, w[0], missing)
+        rel = ((got - want).norm() / want.norm()).item()
+        if missing is None:
+            assert rel <= 4 * 2.0 ** -24
+        else:
+            assert rel > 1.5 * bound(*((a, h) if h else (a,))), rel
+        x = want.float()
+
+
+@pytest.mark.gpu
+@pytest.mark.parametrize("shape", SHORT, ids=str)
+@pytest.mark.parametrize("n,k", [(5, 2), (3000, 1), (2500, 3)])
+def test_short_sums_keep_every_product(shape, n, k):
+    a, h, o = shape
+    c = experts_case(a + h + n, n, 5, k, a, h, o, F32, act="none", biased=False)
+    assert error(c, run_experts(c)) <= bound(*((a, h) if h else (a,)))
+
+
+@pytest.mark.gpu
+@pytest.mark.parametrize("n", [5, 3000])
+def test_short_sums_keep_every_product_gated(n):
+    """Each of the two factors, and the second product."""
+    c = experts_case(n, n, 5, 2, 64, 128, 64, F32, act="none", gated=True, biased=False)
+    assert error(c, run_experts(c)) <= bound(64, 64, 128)
