@@ -280,12 +280,19 @@ expert_fused_kernel(const __grid_constant__ CUtensorMap map_w1, const __grid_con
             v[2 * i + 1] = hi;
           }
         };
-        auto pack = [&](const uint64_t (&v)[16], uint32_t (&w)[16], bool cut) {
+        // left: hidden columns from the first of these 32 on.  What lies behind the last one is 0: zeros for W1 times an infinite state would be NaN, and stay so
+        // times zeros for W2
+        auto pack = [&](const uint64_t (&v)[16], uint32_t (&w)[16], bool cut, int left) {
 #pragma unroll
           for (int i = 0; i < 16; ++i) {
             const float2 f = unpack2(v[i]);
             w[i] = bf16x2_of(f.x, f.y);
             if (cut) w[i] = max_bf16x2(w[i], floor2);
+          }
+          if (left < 32) {
+#pragma unroll
+            for (int i = 0; i < 16; ++i)
+              if (2 * i >= left) w[i] = 0u;
           }
         };
         if constexpr (GATED) {
@@ -299,7 +306,7 @@ expert_fused_kernel(const __grid_constant__ CUtensorMap map_w1, const __grid_con
           scaled(u, 32, q);
 #pragma unroll
           for (int i = 0; i < 16; ++i) v[i] = mul2(v[i], q[i]);
-          pack(v, w, false);
+          pack(v, w, false, 32);   // (gated, an infinite state has no finite row: 0 times what is gated is NaN)
           tmem_st16(st + (uint32_t)(sub * 32), w);
         } else {
           // (P of the first 32 columns takes the place of 16 of them, which have been read)
@@ -311,7 +318,7 @@ expert_fused_kernel(const __grid_constant__ CUtensorMap map_w1, const __grid_con
             tmem_ld_wait();
             scaled(r, h * 32, v);
             if (p.act != IT_ACT_RELU) expert_act(v, p.act);
-            pack(v, w, true);
+            pack(v, w, true, p.hidden - c * 128 - sub * 64 - h * 32);
             tmem_st16(st + (uint32_t)(sub * 64 + h * 16), w);
           }
         }

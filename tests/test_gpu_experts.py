@@ -258,3 +258,24 @@ def test_many_chunks_take_turns_in_two_buffers(kind, gated, a, h, o):
     check_experts(c, want, device="cuda")
     for _ in range(4):
         assert torch.equal(run_experts(c, desc=d, workspace=ws), want)
+
+
+@pytest.mark.parametrize("kind", ["bf16", "eight"])
+@pytest.mark.parametrize("a,h", [(64, 16), (64, 80), (64, 128), (64, 208), (520, 80)])
+@pytest.mark.parametrize("n", [20, 700])
+def test_an_infinite_state_whose_hidden_row_is_finite(kind, a, h, n):
+    """A state of plus infinity before negative weights: ReLU leaves a hidden row of zeros, and the result is the second bias, whatever fills up a tile of hidden columns."""
+    a = a // 16 * 16
+    c = experts_case(h + n, n, 3, 2, a, h, 64, BF16, act="relu", eight=kind == "eight")
+    c["W1"] = (-(c["W1"].float().abs() + 2.0 ** -6).clamp_max(448)).to(c["W1"].dtype)
+    if kind == "eight":   # (e4m3 has no infinity: the scale of a vertex has)
+        c["x"][1] = torch.full((a,), 2.0).to(c["x"].dtype)
+        c["x_scale"][1] = float("inf")
+    else:
+        c["x"][1] = float("inf")
+    got = run_experts(c)
+    assert torch.isfinite(got).all()
+    want = (c["weights"][1][:, None].double() * c["b2"][c["ids"][1].long()].double()).sum(0)
+    # (a rounding of the result, and two products and two sums in fp32, which may cancel)
+    off = c["weights"][1].double() @ c["b2"][c["ids"][1].long()].double().abs()
+    assert ((got[1].double().cpu() - want).abs() <= want.abs() * 2.0 ** -8 + off * 4 * 2.0 ** -24).all()
