@@ -306,7 +306,9 @@ it_status it_aggregate_finish(int64_t n, int32_t dim, it_dtype dtype, const floa
  * it_residual_norm - residual addition and root-mean-square norm of every row:
  *       s = x + residual                                        (residual may be NULL: s = x)
  *       y = s / sqrt( mean(s^2) + eps ) * weight                (weight fp32 [dim] or NULL: 1)
- *   s and the mean are held in fp32 (so |s| beyond 1e19 overflows the mean, and an infinity or NaN in a row makes the row NaN).
+ *   s and the mean are held in fp32: where squares overflow (|s| beyond 1.8e19) the mean is infinite and finite entries of the row become 0, an infinite one
+ *   NaN; a NaN makes the whole row NaN.  In 8 bits a row with an infinity or a NaN is all NaN, and so is its scale.  Squares below 2^-150 count as 0; a row whose
+ *   mean + eps is 0 becomes infinities, and NaN where s is 0.
  *   sum_out [n, dim] feat_dtype, or NULL: s, rounded; the next block's residual.  y is taken from the unrounded s.
  *   out [n, dim]: out_dtype = feat_dtype, or IT_E4M3 (dim a multiple of 16): y / scales[v] rounded to nearest even, with one fp32 scale
  *   per row, scales[v] = max( max|y| / 448, 2^-126 ).  scales must be NULL otherwise.

@@ -151,3 +151,30 @@ def test_no_rows():
     x = torch.empty(0, 64, dtype=BF16, device="cuda")
     assert B.it_residual_norm(B.NormDesc(dim=64, feat_dtype=BF16), x, torch.empty_like(x)).shape == (0, 64)
     assert math.isclose(HALF[BF16], torch.finfo(BF16).eps / 2)
+
+
+@pytest.mark.parametrize("dtype", [F32, BF16])
+@pytest.mark.parametrize("dim", [16, 256, 1040, 2064])
+@pytest.mark.parametrize("eight", [False, True])
+def test_rows_beyond_the_range_of_their_squares(dim, dtype, eight):
+    """What the header says of infinities, NaN, squares that overflow or vanish, and eps = 0."""
+    x, _, w = _inputs(12, 8, dim, dtype, residual=False)
+    w = w.abs() + 0.1
+    x[1, 3] = -float("inf")
+    x[2, dim - 1] = float("nan")
+    x[3, 7] = 3e19
+    x[4] = 1e-30
+    x[5] = 0
+    x[5, 2] = -1e-30
+    out, scales, _ = _run(x, None, w, eight=eight, want_sum=False, eps=0.0)
+    f = out.float()
+    others = [i for i in range(dim) if i != 3]
+    if eight:
+        assert f[1].isnan().all() and scales[1].isnan() and f[2].isnan().all() and scales[2].isnan()
+        assert (f[3] == 0).all() and scales[3] == 2.0 ** -126
+    else:
+        assert f[1, 3].isnan() and (f[1, others] == 0).all() and f[2].isnan().all() and (f[3] == 0).all()
+        assert (f[4] == float("inf")).all()
+        assert f[5, 2] == -float("inf") and f[5, others[3:]].isnan().all()
+    rows = [0, 6, 7]
+    _check(x[rows], None, w, out[rows], scales[rows] if eight else None, None, eps=0.0)
