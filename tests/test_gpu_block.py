@@ -125,3 +125,24 @@ def test_arrays_written_by_the_call_before(rounds):
         for a_, b_ in zip(got, want):
             for p, q in zip(a_, b_):
                 assert torch.equal(p, q)
+
+
+@pytest.mark.parametrize("field,value", [("act", 3), ("feat_dtype", 2), ("weight_dtype", 2), ("act_edge", 3)])
+def test_a_layer_refuses_what_only_the_block_takes(field, value):
+    """SiLU and 8-bit states: refused by the call itself, and nothing is written."""
+    indptr = torch.arange(0, 33, 4, dtype=torch.int64, device="cuda")
+    graph = B.it_graph_create(indptr, torch.zeros(32, dtype=torch.int32, device="cuda"))
+    B.it_split_hubs(graph, 0)
+    layer = B.LayerDesc(op="mean", act="none", in_dim=16, out_dim=16, W=torch.ones(32, 16, device="cuda"))
+    if field == "act_edge":
+        B.it_graph_set_edge_features(graph, torch.ones(32, 4, device="cuda"))
+        layer = B.LayerDesc(op="mean", act="none", in_dim=16, out_dim=16, W=torch.ones(32, 16, device="cuda"), edge_dim=4, msg_dim=16, W_edge=torch.ones(20, 16, device="cuda"))
+    ws = torch.empty(B.it_workspace_bytes(graph, [layer]), dtype=torch.uint8, device="cuda")
+    x, out = torch.ones(8, 16, device="cuda"), torch.full((8, 16), 7.0, device="cuda")
+    c = layer.to_c()
+    setattr(c, field, value)
+    with pytest.raises(B.ItError, match="IT_ERR_INVALID_ARG|IT_ERR_UNSUPPORTED"):
+        B.it_layer_forward(graph, c, x, out, ws)
+    assert (out == 7).all()
+    B.it_layer_forward(graph, layer, x, out, ws)
+    assert not (out == 7).all()
