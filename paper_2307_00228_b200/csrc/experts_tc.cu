@@ -29,7 +29,7 @@ __host__ __device__ constexpr int ex_staging(it_expert_store s) { return ex_dire
 struct ExMeta { int32_t place[TC_BM]; float weight[TC_BM]; float bias[256]; };
 struct ExMetaEight : ExMeta { float xs[TC_BM]; float scale[256]; };
 constexpr int EX_MAX_STAGES = 8;
-constexpr int EX_SLICE = 8;        // k-blocks of a slice (LONG_SUMS)
+constexpr int EX_SLICE = 4;        // k-blocks of a slice (LONG_SUMS)
 constexpr int EX_EPI_BACKOFF = 64, EX_TMA_BACKOFF = 32;   // ns between polls
 
 struct ExParams {
@@ -59,8 +59,8 @@ __device__ __forceinline__ void pass_parts(int i, int *pa, int *pb) {
   *pb = (int)((B >> (4 * i)) & 15u);
 }
 
-// TRI (fp32, K up to 512): a stage holds the three parts of a k-block of either operand, and an accumulator of its own takes the small products.
-// LONG_SUMS (fp32, K above 512): slice by slice of K, each with all its six products; the epilogue adds the slices up, rounding to nearest, in the second
+// TRI (fp32, K up to 256): a stage holds the three parts of a k-block of either operand, and an accumulator of its own takes the small products.
+// LONG_SUMS (fp32, K above 256): slice by slice of K, each with all its six products; the epilogue adds the slices up, rounding to nearest, in the second
 // accumulator's place.
 enum ExForm { EX_PLAIN, EX_TRI, EX_LONG_SUMS };
 template <bool EIGHT, it_expert_store STORE, bool GATED, ExForm FORM>
@@ -547,7 +547,7 @@ it_status it_launch_expert_gemm(const it_experts_args &a, const it_experts_plan 
   p.spin_limit = g.spin_limit ? g.spin_limit : TC_SPIN_LIMIT; p.no_loads = g.no_loads;
   // fp32: with the parts of a k-block in one stage they are fetched once instead of twice each, and the six products are issued behind one wait; two stages
   // and the second accumulator leave 128 columns (64 where rows are stored 128 bytes at a time).
-  const bool tri = g.parts == 3 && g.K <= 512;
+  const bool tri = g.parts == 3 && g.K <= EX_SLICE * 64;
   // columns in as few tiles as 256 accumulator columns allow, of equal width in whole panels
   const int most = (tri ? (ex_direct(g.store) ? 64 : 128) : 256) / (g.gated ? 2 : 1);
   p.n_splits = (g.cols + most - 1) / most;
@@ -555,8 +555,10 @@ it_status it_launch_expert_gemm(const it_experts_args &a, const it_experts_plan 
   p.n_splits = (g.cols + p.cols_per_tile - 1) / p.cols_per_tile;
   p.bn = g.gated ? 2 * p.cols_per_tile : p.cols_per_tile;
   // A tensor core cuts off what it adds to an accumulator, which pulls long sums towards zero: fp32, 2-norm of the error with one accumulator for all of K =
-  // 512, 1024, 2048 4.9e-7, 9.8e-7, 2.1e-6 (a library's fp32 product 4e-7 to 7e-7), and in proportion.  Above K = 512 the epilogue adds up slices of 512, rounding to
-  // nearest: 4.8e-7 for K = 1024 to 8192, 5.2e-7 for 65536, at no cost (40k x 2048 x 256 479 us; slices of 256 2.6e-7 and 487, of 1024 9.8e-7 and 476).
+  // 256, 512, 1024, 2048 2.5e-7, 4.9e-7, 9.8e-7, 2.1e-6 (a library's fp32 product 2.9e-7 to 7e-7), and in proportion; where products follow one another, and in the two
+  // factors of a gate, it adds up (512-1024-512 gated, in slices of 512, 1.4e-6, plain fp32 8.1e-7).  Above K = 256 the epilogue adds up slices of 256, rounding to nearest:
+  // 2.6e-7 for K = 512 to 4096, 512-1024-512 gated 7.7e-7.  Against slices of 512 and TRI up to there: 40k x 512 x 256 140 us / 142, 40k x 1024 x 256 256 / 252,
+  // 20k, 2 of 4, 256-1024-256 325 / 322, gated 512-1024-512 812 / 722, 128-512-128 144 / 117.  (Slices of 128, 1.7e-7: 143, 264, 331, 838, 146.)
 
   const cuuint64_t da[2] = {(cuuint64_t)g.K, (cuuint64_t)(g.a_rows * g.parts)}, sa[1] = {(cuuint64_t)g.K * elem};
   const cuuint32_t ba[2] = {(cuuint32_t)BK, (cuuint32_t)TC_BM};

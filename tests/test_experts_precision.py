@@ -88,3 +88,27 @@ def test_short_sums_keep_every_product_gated(n):
     """Each of the two factors, and the second product."""
     c = experts_case(n, n, 5, 2, 64, 128, 64, F32, act="none", gated=True, biased=False)
     assert error(c, run_experts(c)) <= bound(64, 64, 128)
+
+
+@pytest.mark.gpu
+@pytest.mark.parametrize("a,h,o,gated", [(512, 1024, 512, True), (512, 512, 64, True), (384, 384, 384, True), (320, 520, 136, True), (512, 512, 512, False), (512, 0, 256, False),
+                                         (264, 0, 64, False), (1024, 2048, 72, False)])
+@pytest.mark.parametrize("k", [1, 2])
+def test_as_exact_as_plain_fp32(a, h, o, gated, k):
+    """What the tensor cores cut off adds up over the factors of a gate and the products that follow one another, where roundings to nearest partly cancel: the result
+    stays within one and a half times the error of the same products in plain fp32."""
+    c = experts_case(a + h + o, 2000, 3, k, a, h, o, F32, act="none", gated=gated, biased=False)
+    x, ids, w, W1 = (c[i].cuda() for i in ("x", "ids", "weights", "W1"))
+    before, torch.backends.cuda.matmul.allow_tf32 = torch.backends.cuda.matmul.allow_tf32, False
+    plain = torch.zeros(2000, o, device="cuda")
+    for j in range(k):
+        for e in range(3):
+            v = (ids[:, j] == e).nonzero().flatten()
+            y = x[v] @ W1[e]
+            if gated:
+                y = y[:, :h] * y[:, h:]
+            if h:
+                y = y @ c["W2"][e].cuda()
+            plain[v] += w[v, j, None] * y
+    torch.backends.cuda.matmul.allow_tf32 = before
+    assert error(c, run_experts(c)) <= 1.5 * error(c, plain)
