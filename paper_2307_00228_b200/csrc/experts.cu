@@ -50,9 +50,20 @@ template <typename TW> __device__ __forceinline__ void w_to_f32(const uint4 &q, 
   }
 }
 
+// 16 bytes, or zeros: a load under a predicate, so that a thread's loads go out one behind the other without a branch in between (C++ for the same, with which
+// they did not: bf16 128-512-128 64 places 12.1 us / 10.7, fp32 512-64-512 64 places 13.0 / 11.7).
+__device__ __forceinline__ uint4 load_if(bool in, const void *from) {
+  uint4 q = make_uint4(0, 0, 0, 0);
+  asm volatile("{\n\t.reg .pred p;\n\tsetp.ne.b32 p, %5, 0;\n\t@p ld.global.v4.b32 {%0, %1, %2, %3}, [%4];\n\t}"
+               : "+r"(q.x), "+r"(q.y), "+r"(q.z), "+r"(q.w)
+               : "l"(from), "r"((int)in));
+  return q;
+}
+
+// (blocks an SM: fp32 256-1024-256 128 places 51.7 us with two, 48.3 with four; gated 768-1024-768 16 places 30.4 with two, 27.1 with three)
 // SECOND: the rows of W follow one another place by place of the vertex: row i is row i % K of the place i / K.
 template <typename TX, typename TW, bool SECOND, bool GATED, typename TO>
-__global__ void __launch_bounds__(ROWS_THREADS) expert_rows_kernel(const RowsParams p) {
+__global__ void __launch_bounds__(ROWS_THREADS, GATED ? 3 : 4) expert_rows_kernel(const RowsParams p) {
   constexpr int N = WVec<TW>::N, CB = ROWS_COL_LANES * N, PARTS = GATED ? 2 : 1;
   __shared__ float part[ROWS_WARPS][PARTS * CB];
   __shared__ float total[PARTS * CB];
@@ -107,7 +118,7 @@ __global__ void __launch_bounds__(ROWS_THREADS) expert_rows_kernel(const RowsPar
         xv[u] = in ? elem_f32(x + r) * f : 0.f;
 #pragma unroll
         for (int g = 0; g < PARTS; ++g)
-          q[g][u] = in ? *reinterpret_cast<const uint4 *>(w + (int64_t)r * p.w_cols + g * p.gated_at) : make_uint4(0, 0, 0, 0);
+          q[g][u] = load_if(in, w + (int64_t)r * p.w_cols + g * p.gated_at);
       }
 #pragma unroll
       for (int u = 0; u < ROWS_UNROLL; ++u) {
@@ -289,10 +300,10 @@ it_status check(const it_experts_desc *d, int64_t n) {
   return IT_OK;
 }
 
-// Few places keep the form by place, whose time grows with the weights that its places read.  By place against sorted, us (captured): bf16 64-256-64
-// 64 places 8.3 / 10.2, 128 10.8 / 10.7; 256-256 64 6.9 / 9.5, 128 10.6 / 9.7; 128-512-128 (64 experts) 64 11.3 / 14.2, 128 19.6 / 14.4; 256-1024-256
-// 64 22.4 / 24.1, 128 31.9 / 24.2; gated 768-1024-768 16 26.7 / 30.3, 32 40.6 / 33.0.  fp32, whose sorted form splits all weights first:
-// 64-256-64 256 21.9 / 30.9, 512 32.0 / 32.3; 256-1024-256 128 44.9 / 80.9, 256 78.6 / 82.2.
+// Few places keep the form by place, whose time grows with the weights that its places read: up to so many.  By place against sorted, us (captured): bf16 64-256-64
+// 64 places 8.6 / 10.5, 128 9.3 / 10.7; 256-256 64 6.2 / 9.7, 128 10.1 / 9.7; 128-512-128 (64 experts) 64 11.9 / 15.2, 128 18.6 / 15.5; 256-1024-256
+// 64 21.5 / 24.0, 128 33.5 / 24.0; gated 768-1024-768 16 27.1 / 30.0, 32 41.6 / 32.1.  fp32, whose sorted form splits all weights first:
+// 64-256-64 128 12.6 / 20.5, 192 19.7 / 20.6, 256 23.2 / 20.9, 448 32.3 / 21.8; 256-1024-256 192 72 / 76, 256 86 / 77; of many experts 512-64-512 (64) 256 23.3 / 47.1.
 int64_t most_few(const it_experts_desc &d) {
   const bool f32 = d.feat_dtype == IT_F32;
   const int64_t first = d.hidden_dim > 0 ? (int64_t)d.hidden_dim * (d.gated ? 2 : 1) : d.out_dim;
