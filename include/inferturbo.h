@@ -363,8 +363,8 @@ it_status it_route(const it_route_desc *d, int64_t n, const void *logits, int32_
  *   An id outside [0, n_experts) is no expert, whatever its weight; an expert may be named twice.
  *   in_dim, hidden_dim and out_dim are multiples of 8 (in_dim and the width of F's first product of 16 with IT_E4M3), n_experts <= 4096.  The
  *   places of all vertices, padded for every expert, are counted in 32 bits: n * top_k + 128 * n_experts < 2^31 (fp32: a third of that).
- *   The products run on the tensor cores with fp32 accumulators (fp32 operands as three bf16 parts, six products: an infinity in them gives
- *   NaN); the hidden row between the two products is rounded to feat_dtype, the places of a vertex are added in fp32, in their order, and
+ *   The products run on the tensor cores with fp32 accumulators (fp32 operands as three bf16 parts, six products, long sums in slices: an error like that of plain
+ *   fp32, 3e-7 a product in the 2-norm, at any width; an infinity in them gives NaN); the hidden row between the two products is rounded to feat_dtype, the places of a vertex are added in fp32, in their order, and
  *   rounded once.  Few places take products of their own, in fp32 throughout.  Which form a call takes depends on its sizes alone: the same call gives the
  *   same bits, but the last ones of a vertex may differ with the number of vertices beside it.
  *   workspace: device, 256-byte aligned, >= it_experts_workspace_bytes (which never falls as n grows: what serves n serves fewer); calls that can overlap on

@@ -173,7 +173,8 @@ __device__ __forceinline__ float route_unorder(unsigned o) { return __uint_as_fl
 
 // L lanes per row, C experts per lane; a round of the choice is a maximum over a lane's keys and over the lanes.  The scores of the chosen
 // are taken afterwards, a lane each.
-// (eight blocks an SM: 200k rows of 256 experts in groups 508 us with 94 registers a thread, 366 with 64)
+// (eight blocks an SM: 200k rows of 256 experts in groups 758 us with the 138 registers that it would take, 385 with 64 and some spills; 1M rows of 64 366 and 262,
+// with six blocks 278, with seven 271)
 template <typename T, int L, int C>
 __global__ void __launch_bounds__(ROUTE_THREADS, C == 8 ? 8 : 1) route_kernel(const RouteParams p) {
   it_allow_next();
